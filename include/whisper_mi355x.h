@@ -486,6 +486,135 @@ typedef enum {
 whisper_status whisper_test_kernel_choice(int32_t choice_of, int32_t dtype, const int64_t* sizes,
                                           int32_t n_sizes, int32_t* choice);
 
+/*
+ * Paged key/value cache: a cache of its own, for decoders that a program
+ * builds from operators (the engine's slots keep their caches themselves).
+ * The keys and values of up to max_seqs sequences live in pages of page_size
+ * positions; a sequence holds whole pages, and forked sequences share the
+ * pages that were full when they were forked.
+ *
+ * One chunk of new tokens at a time goes through the cache:
+ *   whisper_cache_extend makes room for the new positions of the listed
+ *     sequences (in the order of `seqs`, the rows of the following calls are
+ *     the tokens of the first sequence, then those of the second, ...);
+ *   whisper_cache_append writes a layer's keys and values of those tokens;
+ *   whisper_cache_attend computes a layer's causal attention of those tokens
+ *     over everything their sequences hold, the new positions included (after
+ *     the layer's append). A chunk of one token per sequence is a decode
+ *     step; longer ones are prompts or drafted tokens to verify.
+ *
+ * Streams: the calls enqueue work on the cache's stream (at first the device's
+ * default stream, see whisper_cache_set_stream) and return without waiting;
+ * host arrays are read before a call returns, device memory when the work
+ * runs (device pointers of a call that has no rows may be NULL). append and attend may be recorded into a graph, after an extend; each
+ * replay takes the chunk that is current when it runs (k, v, q and out need a
+ * row per token of it; a layer = -1 append as many tokens as at its
+ * recording). The other calls refuse a recording stream (WHISPER_E_STATE).
+ * All calls on one cache, replays too, share its workspace: order them on one
+ * stream.
+ * Device: calls run on the cache's device and leave the current device as it
+ * was. Device pointers are memory of that device.
+ * Results do not depend on which pages a sequence holds. A sequence's
+ * attention may round differently in another chunk (its positions may be cut
+ * over workgroups in another way).
+ * Threads: one thread at a time per cache.
+ */
+typedef struct whisper_cache whisper_cache;
+
+/* A handle without a device: the calls that only keep book (extend, truncate,
+ * fork, compact, info) work, append, attend and read return WHISPER_E_STATE. */
+#define WHISPER_NO_DEVICE (-1)
+
+/*
+ *   dtype          WHISPER_DTYPE_*: type of keys, values, queries and outputs;
+ *                  sums, maxima and softmax weights are fp32 (bf16: weights
+ *                  enter the product with the values rounded to bf16)
+ *   n_layer        1..256
+ *   n_head         query heads, 1..256
+ *   n_kv_head      key/value heads, a divisor of n_head: query head h reads
+ *                  key/value head h / (n_head / n_kv_head)
+ *   head_size      64 or 128
+ *   page_size      positions per page: 32, 64, 128 or 256
+ *   n_pages        pages of the cache, 1..2^22
+ *   max_seqs       sequences, 1..4096
+ *   max_positions  longest sequence, 1..2^24
+ *   max_tokens     most new tokens of a chunk, all sequences together, 1..2^20
+ */
+typedef struct {
+    int32_t dtype, n_layer, n_head, n_kv_head, head_size, page_size, n_pages, max_seqs, max_positions, max_tokens;
+} whisper_cache_params;
+
+/* Creates a cache on HIP device `device` (or WHISPER_NO_DEVICE), every
+ * sequence empty. *out is set only on success. Errors: E_INVAL, E_NOMEM,
+ * E_DEVICE; whisper_cache_error(NULL) then holds the message. */
+whisper_status whisper_cache_create(const whisper_cache_params* params, int device, whisper_cache** out);
+
+/* Waits for the cache's stream and frees what the cache owns. NULL is allowed. */
+void whisper_cache_destroy(whisper_cache* cache);
+
+/* Last error message of cache (or of the calling thread's last failed create
+ * when cache is NULL); valid until the next call on the same cache. */
+const char* whisper_cache_error(const whisper_cache* cache);
+
+/* Enqueues the cache's work on `hip_stream` from now on (a hipStream_t of its
+ * device; NULL: the device's default stream). Waits for the work on the stream
+ * chosen before, if that is another one; it must outlive its use. */
+whisper_status whisper_cache_set_stream(whisper_cache* cache, void* hip_stream);
+
+/*
+ * Adds counts[i] >= 0 positions to sequence seqs[i] (host arrays, n distinct
+ * sequences) and makes them the current chunk, until the next extend, or a
+ * truncate that takes positions from one of its sequences. A page that is
+ * shared and gets new positions is copied first. Errors: E_INVAL, E_CAPACITY
+ * (no such sequence, too few free pages, max_positions or max_tokens; nothing
+ * has changed then).
+ */
+whisper_status whisper_cache_extend(whisper_cache* cache, const int32_t* seqs, const int32_t* counts, int32_t n);
+
+/*
+ * Writes the chunk's keys and values of one layer: device rows k and v
+ * [tokens][n_kv_head][head_size], row strides in elements (0: rows without
+ * gaps). layer -1: all layers, k and v [n_layer][tokens] rows. Errors:
+ * E_INVAL, E_STATE (no chunk).
+ */
+whisper_status whisper_cache_append(whisper_cache* cache, int32_t layer, const void* k, const void* v, int64_t k_stride,
+                                    int64_t v_stride);
+
+/*
+ * Causal attention of the chunk in one layer. For new token i of a sequence
+ * that held `past` positions before the chunk, and query head h:
+ *   s[t] = scale * q . k[t], t = 0 .. past + i;  out = sum exp(s[t]) v[t] / sum exp(s[t])
+ * q and out: device rows [tokens][n_head][head_size], 16-byte aligned, row
+ * strides in elements (0: rows without gaps), multiples of 16 bytes. q and out may be
+ * the same memory only if their strides are equal. Later positions and
+ * positions beyond a sequence's end do not enter, whatever they hold.
+ * Errors: E_INVAL, E_STATE (no chunk).
+ */
+whisper_status whisper_cache_attend(whisper_cache* cache, int32_t layer, const void* q, void* out, int64_t q_stride,
+                                    int64_t out_stride, float scale);
+
+/* Shortens sequence seqs[i] to lengths[i] positions (0 frees it); pages that
+ * no sequence holds any more are free again. Errors: E_INVAL (longer than it
+ * is), E_CAPACITY (no such sequence). */
+whisper_status whisper_cache_truncate(whisper_cache* cache, const int32_t* seqs, const int32_t* lengths, int32_t n);
+
+/* Makes the n empty sequences dst copies of sequence src: full pages are
+ * shared, a partly filled last page is copied. Errors: E_INVAL, E_STATE (a
+ * destination is not empty), E_CAPACITY (no such sequence, too few free pages). */
+whisper_status whisper_cache_fork(whisper_cache* cache, int32_t src, const int32_t* dst, int32_t n);
+
+/* Moves the pages in use to the front of the cache's memory. */
+whisper_status whisper_cache_compact(whisper_cache* cache);
+
+/* Copies the keys and values of the n listed sequences, one after another, to
+ * device rows k and v (as in whisper_cache_append; layer -1: all layers, rows
+ * of layer l after those of layer l - 1). Errors: E_INVAL, E_CAPACITY. */
+whisper_status whisper_cache_read(whisper_cache* cache, int32_t layer, const int32_t* seqs, int32_t n, void* k, void* v,
+                                  int64_t k_stride, int64_t v_stride);
+
+/* Length and pages of sequence seq, and the cache's free pages (host; any may be NULL). */
+whisper_status whisper_cache_info(whisper_cache* cache, int32_t seq, int32_t* length, int32_t* pages, int32_t* free_pages);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,9 @@ EXPORTS = (
     "whisper_profile_enable", "whisper_profile_read", "whisper_time_kernel", "whisper_stats_read",
     "whisper_set_decoding", "whisper_test_batcher", "whisper_test_greedy_keys",
     "whisper_test_kernel_choice",
+    "whisper_cache_create", "whisper_cache_destroy", "whisper_cache_error", "whisper_cache_set_stream",
+    "whisper_cache_extend", "whisper_cache_append", "whisper_cache_attend", "whisper_cache_truncate",
+    "whisper_cache_fork", "whisper_cache_compact", "whisper_cache_read", "whisper_cache_info",
 )
 
 
@@ -57,6 +60,14 @@ class whisper_stats(C.Structure):
         "encode_passes", "segments_encoded", "decode_steps", "rows_decoded", "positions_attended",
         "refill_batches")] + [("batcher_host_ms", C.c_double), ("engine_host_ms", C.c_double)]
 
+
+class whisper_cache_params(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in (
+        "dtype", "n_layer", "n_head", "n_kv_head", "head_size", "page_size", "n_pages", "max_seqs", "max_positions",
+        "max_tokens")]
+
+
+NO_DEVICE = -1
 
 _lib = None
 
@@ -96,6 +107,18 @@ def load(path: str = LIB_PATH) -> C.CDLL:
                                       i32, i64, i64]),
         "whisper_test_greedy_keys": (i32, [C.POINTER(C.c_float), i32, i32, C.POINTER(C.c_uint32), pi32, pi32]),
         "whisper_test_kernel_choice": (i32, [i32, i32, C.POINTER(i64), i32, pi32]),
+        "whisper_cache_create": (i32, [C.POINTER(whisper_cache_params), C.c_int, C.POINTER(vp)]),
+        "whisper_cache_destroy": (None, [vp]),
+        "whisper_cache_error": (C.c_char_p, [vp]),
+        "whisper_cache_set_stream": (i32, [vp, vp]),
+        "whisper_cache_extend": (i32, [vp, pi32, pi32, i32]),
+        "whisper_cache_append": (i32, [vp, i32, vp, vp, i64, i64]),
+        "whisper_cache_attend": (i32, [vp, i32, vp, vp, i64, i64, C.c_float]),
+        "whisper_cache_truncate": (i32, [vp, pi32, pi32, i32]),
+        "whisper_cache_fork": (i32, [vp, i32, pi32, i32]),
+        "whisper_cache_compact": (i32, [vp]),
+        "whisper_cache_read": (i32, [vp, i32, pi32, i32, vp, vp, i64, i64]),
+        "whisper_cache_info": (i32, [vp, i32, pi32, pi32, pi32]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -113,6 +136,21 @@ class WhisperError(RuntimeError):
 
 def _ptr(a: np.ndarray, ctype):
     return a.ctypes.data_as(C.POINTER(ctype))
+
+
+def _ints(a) -> np.ndarray:
+    """Host integers as int32; values that do not fit are refused."""
+    x = np.asarray(list(a) if not isinstance(a, np.ndarray) else a)
+    if x.size == 0:
+        return np.zeros(0, np.int32)
+    if x.ndim != 1 or not np.issubdtype(x.dtype, np.integer) or x.min() < -2**31 or x.max() >= 2**31:
+        raise WhisperError(E_INVAL, "a list of 32-bit integers is needed")
+    return np.ascontiguousarray(x, dtype=np.int32)
+
+
+def _same_length(a, b):
+    if a.size != b.size:
+        raise WhisperError(E_INVAL, "lists of the same length are needed")
 
 
 def _check(st: int, ctx_handle=None):
@@ -273,6 +311,81 @@ class Context:
         st = whisper_stats()
         self._check(load().whisper_stats_read(self.h, C.byref(st), 1 if reset else 0))
         return {name: getattr(st, name) for name, _ in whisper_stats._fields_}
+
+
+class Cache:
+    """A paged key/value cache (whisper_cache_*). k, v, q and out are device
+    addresses; the calls enqueue work on the cache's stream and return
+    without waiting for it."""
+
+    def __init__(self, dtype: int, n_layer: int, n_head: int, n_kv_head: int, head_size: int, page_size: int,
+                 n_pages: int, max_seqs: int, max_positions: int, max_tokens: int, device: int = 0):
+        self.params = whisper_cache_params(dtype, n_layer, n_head, n_kv_head, head_size, page_size, n_pages, max_seqs,
+                                           max_positions, max_tokens)
+        h = C.c_void_p()
+        st = load().whisper_cache_create(C.byref(self.params), device, C.byref(h))
+        self.h = None
+        self._check(st)
+        self.h = h
+
+    def close(self):
+        if getattr(self, "h", None):
+            load().whisper_cache_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def _check(self, st):
+        if st != OK:
+            raise WhisperError(st, load().whisper_cache_error(self.h).decode())
+
+    def set_stream(self, stream_handle: int | None):
+        self._check(load().whisper_cache_set_stream(self.h, C.c_void_p(stream_handle or None)))
+
+    def extend(self, seqs, counts):
+        s, c = _ints(seqs), _ints(counts)
+        _same_length(s, c)
+        self._check(load().whisper_cache_extend(self.h, _ptr(s, C.c_int32), _ptr(c, C.c_int32), s.size))
+
+    def append(self, layer: int, k: int, v: int, k_stride: int = 0, v_stride: int = 0):
+        self._check(load().whisper_cache_append(self.h, layer, k, v, k_stride, v_stride))
+
+    def attend(self, layer: int, q: int, out: int, q_stride: int = 0, out_stride: int = 0, scale: float | None = None):
+        """scale defaults to head_size ** -0.5."""
+        self._check(load().whisper_cache_attend(self.h, layer, q, out, q_stride, out_stride,
+                                                self.params.head_size ** -0.5 if scale is None else scale))
+
+    def truncate(self, seqs, lengths):
+        s, c = _ints(seqs), _ints(lengths)
+        _same_length(s, c)
+        self._check(load().whisper_cache_truncate(self.h, _ptr(s, C.c_int32), _ptr(c, C.c_int32), s.size))
+
+    def fork(self, src: int, dst):
+        d = _ints(dst)
+        self._check(load().whisper_cache_fork(self.h, src, _ptr(d, C.c_int32), d.size))
+
+    def compact(self):
+        self._check(load().whisper_cache_compact(self.h))
+
+    def read(self, layer: int, seqs, k: int, v: int, k_stride: int = 0, v_stride: int = 0):
+        s = _ints(seqs)
+        self._check(load().whisper_cache_read(self.h, layer, _ptr(s, C.c_int32), s.size, k, v, k_stride, v_stride))
+
+    def info(self, seq: int):
+        """(length, pages) of a sequence and the cache's free pages."""
+        a, b, c = C.c_int32(), C.c_int32(), C.c_int32()
+        self._check(load().whisper_cache_info(self.h, seq, C.byref(a), C.byref(b), C.byref(c)))
+        return a.value, b.value, c.value
 
 
 def test_batcher(arrival_us, user_id, segment_id, max_new_tokens, slots, encode_batch, refill_min,

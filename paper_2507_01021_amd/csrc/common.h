@@ -144,6 +144,14 @@ __host__ __device__ inline float ord2f(uint32_t o) {
 // MFMA operand vectors.
 typedef __attribute__((__vector_size__(8 * sizeof(short)))) short bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+typedef __bf16 mfma_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float mfma_f32x4 __attribute__((ext_vector_type(4)));
+
+// s_waitcnt immediate that waits until at most n vector-memory ops are outstanding.
+#define WMI_VMCNT(n) ((((n) & 0xF)) | (((n) >> 4) << 14) | (0x7 << 4) | (0xF << 8))
+// The same, and for every LDS read of this wave. A barrier does not wait for
+// them, and after it other waves' direct loads refill the buffer read last.
+#define WMI_VMCNT_LDS(n) (WMI_VMCNT(n) & ~(0xF << 8))
 
 }  // namespace wmi
 

@@ -28,9 +28,6 @@
 
 namespace wmi {
 
-typedef __bf16 mfma_bf16x8 __attribute__((ext_vector_type(8)));
-typedef float mfma_f32x4 __attribute__((ext_vector_type(4)));
-
 // ------------------------------------------------------------------ bf16 MFMA
 
 namespace gb {
@@ -47,12 +44,6 @@ constexpr int LDS_BYTES = 2 * STAGE_BYTES;     // two buffers (128 KiB)
 // position c ^ ((r >> 1) & 3), so the 8 rows read together by a ds_read_b128
 // group hit distinct banks.
 __device__ inline int swz32(int r, int c) { return r * 64 + ((c ^ ((r >> 1) & 3)) << 4); }
-
-// s_waitcnt immediate that waits until at most n vector-memory ops are outstanding.
-#define WMI_VMCNT(n) ((((n) & 0xF)) | (((n) >> 4) << 14) | (0x7 << 4) | (0xF << 8))
-// The same, and for every LDS read of this wave. A barrier does not wait for
-// them, and after it other waves' direct loads refill the buffer read last.
-#define WMI_VMCNT_LDS(n) (WMI_VMCNT(n) & ~(0xF << 8))
 
 // Byte offset of 16-byte chunk c (0..7) of row r inside a [rows][64] bf16 LDS tile.
 __device__ inline int swz(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }

@@ -1,0 +1,505 @@
+// Kernels of a paged key/value cache: appending rows, copying pages, reading
+// sequences out, and causal attention of new tokens over the pages.
+//
+// Memory: page g of layer l holds, for every key/value head, P positions of
+// keys and P of values, D numbers each, both in the order in which a matrix
+// instruction takes them (16-byte pieces of 64 lanes, 1 KiB blocks), so that
+// an operand fragment is one contiguous load and needs no transposition:
+//   pages [page][layer][K, V][kv head][P * D]
+//   keys:   blocks of 16 positions x 16 bytes x 4 of dims (dec_off with row =
+//           position), as the A operand of S^T = K Q^T;
+//   values: blocks of 16 dims x 32 positions (bf16) or 16 (fp32), as the A
+//           operand of O^T += V^T P^T, whose positions are ordered so that a
+//           lane's scores are its own weights (val_off).
+// A page is one contiguous block over all layers, so copying one is one long
+// run.
+#pragma once
+
+#include "common.h"
+
+namespace wmi {
+
+// Element offset of (position p, dim c) in a head's values of D dims.
+template <class T>
+__host__ __device__ inline int val_off(int p, int c, int D) {
+    if constexpr (sizeof(T) == 2)
+        return ((p >> 5) * (D >> 4) + (c >> 4)) * 512 + (((p >> 2) & 3) * 16 + (c & 15)) * 8 + ((p & 16) >> 2) + (p & 3);
+    else
+        return ((p >> 4) * (D >> 4) + (c >> 4)) * 256 + (((p >> 2) & 3) * 16 + (c & 15)) * 4 + (p & 3);
+}
+
+// The pages of a cache as a kernel sees them. table[seq * ld + i] is the
+// i-th page of a sequence.
+struct PagedView {
+    unsigned char* pages;
+    const int* table;
+    int ld;
+    int shift;             // log2 of the positions per page
+    int n_layer, Hkv;
+    long long head_elems;  // P * D
+    template <class T>
+    __device__ T* head(int page, int layer, int kv, int h) const {
+        return reinterpret_cast<T*>(pages) + (((long long)page * n_layer + layer) * 2 + kv) * Hkv * head_elems +
+               (long long)h * head_elems;
+    }
+};
+
+// A run of up to 32 positions of one sequence inside one block of 32, and the
+// row of its first position in the caller's rows.
+struct PageTile {
+    int seq, pos, n;
+    int row;
+};
+
+// Head of a device list: what it holds and where (in ints from its start).
+// Kernels read it when they run and go through their part in strides of the
+// grid, so a recorded launch serves whatever list is current at its replay.
+struct ListHead {
+    int items, merges, tiles, merges_at, tiles_at, pad[3];
+};
+constexpr int HEAD_INTS = sizeof(ListHead) / sizeof(int);
+
+// ------------------------------------------------------------------ small lists
+//
+// Lists of up to PUT_INTS numbers reach the device as a kernel argument: no
+// copy engine, nothing to wait for, and the host may go on at once.
+constexpr int PUT_INTS = 960;
+struct PutInts {
+    int n;
+    int v[PUT_INTS];
+};
+__global__ __launch_bounds__(256) void put_ints_kernel(PutInts a, int* __restrict__ dst) {
+    for (int i = threadIdx.x; i < a.n; i += 256) dst[i] = a.v[i];
+}
+// table[at[2 i]] = at[2 i + 1]
+__global__ __launch_bounds__(256) void table_update_kernel(const int* __restrict__ at, int n, int* __restrict__ table) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) table[at[2 * i]] = at[2 * i + 1];
+}
+
+// ------------------------------------------------------------------ rows in and out
+//
+// Rows [layer][row][kv head][D] (layer stride layer_ld, row stride row_ld
+// elements). One workgroup per (tile, kv head, layer) moves a tile's keys and
+// values through LDS, so that memory is accessed in 16-byte pieces on both
+// sides; a tile that does not cover a whole value piece writes single
+// elements. VEC: rows are 16-byte aligned.
+template <class T, int D, bool VEC>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, const int* __restrict__ list, int layer0,
+                                                           const T* __restrict__ k, const T* __restrict__ v,
+                                                           long long k_ld, long long v_ld, long long k_layer,
+                                                           long long v_layer) {
+    constexpr int EL = 16 / sizeof(T);  // elements of a 16-byte piece
+    constexpr int CH = D / EL;          // pieces of a row
+    constexpr int LD = D + EL;          // LDS row
+    __shared__ __align__(16) T sv[32 * LD];
+    const ListHead head = *reinterpret_cast<const ListHead*>(list);
+    const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
+    const int h = blockIdx.y, layer = layer0 + blockIdx.z, tid = threadIdx.x;
+    for (int it = blockIdx.x; it < head.tiles; it += gridDim.x) {
+        const PageTile t = tiles[it];
+        const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
+        const int p0 = t.pos & ((1 << c.shift) - 1);
+        T* kd = c.head<T>(page, layer, 0, h);
+        T* vd = c.head<T>(page, layer, 1, h);
+        const T* ks = k + blockIdx.z * k_layer + (long long)t.row * k_ld + h * D;
+        const T* vs = v + blockIdx.z * v_layer + (long long)t.row * v_ld + h * D;
+        for (int i = tid; i < t.n * CH; i += 256) {
+            const int r = i / CH, ch = i - r * CH;
+            if constexpr (VEC) {
+                const u32x4 a = *reinterpret_cast<const u32x4*>(ks + r * k_ld + ch * EL);
+                const u32x4 b = *reinterpret_cast<const u32x4*>(vs + r * v_ld + ch * EL);
+                *reinterpret_cast<u32x4*>(kd + dec_off<T>(p0 + r, ch * EL, D)) = a;
+                *reinterpret_cast<u32x4*>(sv + ((p0 + r) & 31) * LD + ch * EL) = b;
+            } else {
+                for (int e = 0; e < EL; ++e) {
+                    kd[dec_off<T>(p0 + r, ch * EL + e, D)] = ks[r * k_ld + ch * EL + e];
+                    sv[((p0 + r) & 31) * LD + ch * EL + e] = vs[r * v_ld + ch * EL + e];
+                }
+            }
+        }
+        __syncthreads();
+        // value pieces of the tile's block of 32 positions: EL positions of one dim each
+        const int lo = p0 & 31, hi = lo + t.n;
+        T* vb = vd + val_off<T>(p0 & ~31, 0, D);
+        for (int i = tid; i < 32 * CH; i += 256) {
+            // piece i: block i / 64 (16 dims; in fp32 the 16-position halves come first), lane i % 64
+            const int blk = i >> 6, ln = i & 63;
+            const int half = sizeof(T) == 2 ? 0 : blk / (D >> 4);
+            const int dim = (blk - half * (D >> 4)) * 16 + (ln & 15), g = ln >> 4;
+            struct Elems { T e[EL]; } e;
+            bool all = true;
+#pragma unroll
+            for (int j = 0; j < EL; ++j) {
+                const int pos = sizeof(T) == 2 ? g * 4 + (j & 3) + (j >> 2) * 16 : half * 16 + g * 4 + j;
+                all = all && pos >= lo && pos < hi;
+                e.e[j] = sv[pos * LD + dim];
+            }
+            T* dst = vb + blk * (1024 / sizeof(T)) + ln * EL;
+            if (all) {
+                *reinterpret_cast<u32x4*>(dst) = __builtin_bit_cast(u32x4, e);
+            } else {
+#pragma unroll
+                for (int j = 0; j < EL; ++j) {
+                    const int pos = sizeof(T) == 2 ? g * 4 + (j & 3) + (j >> 2) * 16 : half * 16 + g * 4 + j;
+                    if (pos >= lo && pos < hi) dst[j] = e.e[j];
+                }
+            }
+        }
+        __syncthreads();  // the next tile's LDS
+    }
+}
+
+template <class T, int D, bool VEC>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedView c, const int* __restrict__ list, int layer0,
+                                                         T* __restrict__ k, T* __restrict__ v, long long k_ld,
+                                                         long long v_ld, long long k_layer, long long v_layer) {
+    constexpr int EL = 16 / sizeof(T);
+    constexpr int CH = D / EL;
+    constexpr int LD = D + EL;
+    __shared__ __align__(16) T sv[32 * LD];
+    const ListHead head = *reinterpret_cast<const ListHead*>(list);
+    const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
+    const int h = blockIdx.y, layer = layer0 + blockIdx.z, tid = threadIdx.x;
+    for (int it = blockIdx.x; it < head.tiles; it += gridDim.x) {
+        const PageTile t = tiles[it];
+        const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
+        const int p0 = t.pos & ((1 << c.shift) - 1);
+        const T* kd = c.head<T>(page, layer, 0, h);
+        const T* vb = c.head<T>(page, layer, 1, h) + val_off<T>(p0 & ~31, 0, D);
+        T* ks = k + blockIdx.z * k_layer + (long long)t.row * k_ld + h * D;
+        T* vs = v + blockIdx.z * v_layer + (long long)t.row * v_ld + h * D;
+        for (int i = tid; i < 32 * CH; i += 256) {
+            const int blk = i >> 6, ln = i & 63;
+            const int half = sizeof(T) == 2 ? 0 : blk / (D >> 4);
+            const int dim = (blk - half * (D >> 4)) * 16 + (ln & 15), g = ln >> 4;
+            const u32x4 a = *reinterpret_cast<const u32x4*>(vb + blk * (1024 / sizeof(T)) + ln * EL);
+            struct Elems { T e[EL]; };
+            const Elems e = __builtin_bit_cast(Elems, a);
+#pragma unroll
+            for (int j = 0; j < EL; ++j) {
+                const int pos = sizeof(T) == 2 ? g * 4 + (j & 3) + (j >> 2) * 16 : half * 16 + g * 4 + j;
+                sv[pos * LD + dim] = e.e[j];
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < t.n * CH; i += 256) {
+            const int r = i / CH, ch = i - r * CH;
+            if constexpr (VEC) {
+                *reinterpret_cast<u32x4*>(ks + r * k_ld + ch * EL) =
+                    *reinterpret_cast<const u32x4*>(kd + dec_off<T>(p0 + r, ch * EL, D));
+                *reinterpret_cast<u32x4*>(vs + r * v_ld + ch * EL) =
+                    *reinterpret_cast<const u32x4*>(sv + ((p0 + r) & 31) * LD + ch * EL);
+            } else {
+                for (int e = 0; e < EL; ++e) {
+                    ks[r * k_ld + ch * EL + e] = kd[dec_off<T>(p0 + r, ch * EL + e, D)];
+                    vs[r * v_ld + ch * EL + e] = sv[((p0 + r) & 31) * LD + ch * EL + e];
+                }
+            }
+        }
+        __syncthreads();  // the next tile's LDS
+    }
+}
+
+// Copies whole pages (all layers): pairs (source, destination), `bytes` each,
+// a multiple of 4096. Workgroups of a pair take 16 KiB each.
+constexpr int PAGE_RUN = 16384;
+__global__ __launch_bounds__(256) void paged_copy_kernel(unsigned char* __restrict__ pages,
+                                                         const int* __restrict__ pairs, long long bytes) {
+    const long long at = (long long)blockIdx.x * PAGE_RUN + threadIdx.x * 16;
+    const unsigned char* s = pages + pairs[2 * blockIdx.y] * bytes + at;
+    unsigned char* d = pages + pairs[2 * blockIdx.y + 1] * bytes + at;
+    u32x4 a[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (at + u * 4096 < bytes) a[u] = *reinterpret_cast<const u32x4*>(s + u * 4096);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (at + u * 4096 < bytes) *reinterpret_cast<u32x4*>(d + u * 4096) = a[u];
+}
+
+// ------------------------------------------------------------------ attention of few rows
+//
+// Query rows of a sequence and kv head: row j = token * G + g of the chunk's
+// `count` tokens and the G query heads that share the kv head. Token i of a
+// sequence that held `past` positions sees positions 0 .. past + i.
+// An item is 16 such rows and a range of positions [kv0, kv1); the ranges of
+// rows that are cut over several items are joined by paged_merge_kernel.
+struct AttnItem {
+    int seq, past, count;
+    int tok0;       // the sequence's first token row in q and out
+    int j0;         // first of up to 16 rows
+    int kv0, kv1;   // positions, kv0 a multiple of 32
+    int part;       // result slot of a cut range, or -1: the result itself
+};
+// Rows j0 .. of a sequence whose positions were cut into n parts, one after
+// another from slot `part`.
+struct MergeItem {
+    int count, tok0, j0, part, n;
+};
+struct AttnArgs {
+    PagedView c;
+    int layer, H, G;
+    const void* q;
+    void* out;
+    long long q_ld, out_ld;  // elements per token row
+    float scale;             // of the scores, times log2(e)
+    const int* plan;         // ListHead, then the items; merges at its merges_at
+    float* parts;            // [part][kv head][16][D + 2]: sums, maximum, weight
+};
+
+// Four consecutive outputs of a row, row-major or as the projections take
+// their activations (dec_off).
+template <class T, bool FRAG>
+__device__ inline void attn_store(const AttnArgs& a, int row, int h, int D, int dim, float x, float y, float z, float w) {
+    T* out = static_cast<T*>(a.out);
+    if constexpr (FRAG)
+        st4(out + dec_off<T>(row, h * D + dim, a.H * D), x, y, z, w);
+    else
+        st4(out + (long long)row * a.out_ld + h * D + dim, x, y, z, w);
+}
+
+// Fragments of 16 bytes and the products over them. bf16: one 16x16x32
+// instruction per fragment pair; fp32: four 16x16x4 ones.
+template <class T> struct Piece;
+template <> struct Piece<bf16> {
+    typedef mfma_bf16x8 V;
+    __device__ static inline mfma_f32x4 mul(V a, V b, mfma_f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Piece<float> {
+    typedef mfma_f32x4 V;
+    __device__ static inline mfma_f32x4 mul(V a, V b, mfma_f32x4 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// 16 rows per workgroup; its four waves take the item's blocks of 32 positions
+// in turn and join their results in LDS. Per wave and block
+//   S^T[position][row] = K Q^T, running maximum and sum per row (a lane holds
+//   8 positions of one row), O^T[dim][row] += V^T P^T with the lane's own
+//   weights as the B operand.
+// Scores, maxima, sums and outputs are fp32; the bf16 weights enter the product
+// rounded to bf16 (2^-9 of each weight at most), their sum does not.
+// Positions at or beyond kv1 may hold anything: their values are replaced by
+// zeros. A block some of whose positions only some rows see is multiplied row
+// by row if its values are not all finite, since 0 * inf is not 0.
+template <class T, int D, bool FRAG>
+__global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
+    typedef typename Piece<T>::V V;
+    constexpr int EL = 16 / sizeof(T), NK = D / KSTEP<T>, ND = D / 16, BLK = 1024 / sizeof(T);
+    constexpr int NV = sizeof(T) == 2 ? 1 : 2;  // value blocks per 32 positions and 16 dims
+    __shared__ float so[4][16][D + 4];
+    __shared__ float sm[4][16], sl[4][16];
+    const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
+    const AttnItem* items = reinterpret_cast<const AttnItem*>(a.plan + HEAD_INTS);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
+    for (int w0 = blockIdx.x; w0 < head.items * a.c.Hkv; w0 += gridDim.x) {
+        const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
+        const AttnItem t = items[it];
+        const int rows = t.count * a.G;
+        const int j = min(t.j0 + fr, rows - 1), tok = j / a.G, g = j - tok * a.G;
+        const int lim = t.past + tok + 1;            // positions this lane's row sees
+        const int all = t.past + t.j0 / a.G + 1;     // positions every row sees
+        const T* q = static_cast<const T*>(a.q) + (long long)(t.tok0 + tok) * a.q_ld + (h * a.G + g) * D + fc * EL;
+        V qf[NK];
+#pragma unroll
+        for (int s = 0; s < NK; ++s) qf[s] = *reinterpret_cast<const V*>(q + s * KSTEP<T>);
+        mfma_f32x4 o[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        const int* table = a.c.table + (long long)t.seq * a.c.ld;
+        const int pmask = (1 << a.c.shift) - 1;
+        for (int p = t.kv0 + wave * 32; p < t.kv1; p += 128) {
+            const int page = table[p >> a.c.shift], p0 = p & pmask;
+            const T* kb = a.c.template head<T>(page, a.layer, 0, h) + (p0 >> 4) * (NK * BLK) + lane * EL;
+            const T* vb = a.c.template head<T>(page, a.layer, 1, h) + val_off<T>(p0, 0, D) + lane * EL;
+            V kf[2][NK], vf[NV][ND];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int s = 0; s < NK; ++s) kf[b][s] = *reinterpret_cast<const V*>(kb + (b * NK + s) * BLK);
+#pragma unroll
+            for (int b = 0; b < NV; ++b)
+#pragma unroll
+                for (int d = 0; d < ND; ++d) vf[b][d] = *reinterpret_cast<const V*>(vb + (b * ND + d) * BLK);
+            mfma_f32x4 sc[2];
+            float mx = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                mfma_f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < NK; ++s) x = Piece<T>::mul(kf[b][s], qf[s], x);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] *= a.scale;
+                    if (p + 32 > all && p + b * 16 + fc * 4 + r >= lim) x[r] = -INFINITY;
+                    mx = fmaxf(mx, x[r]);
+                }
+                sc[b] = x;
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float mn = fmaxf(m, mx);
+            const float mu = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing yet
+            if (__any(mn > m)) {
+                const float alpha = exp2_softmax(m - mu);
+                l *= alpha;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
+                m = mn;
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sc[b][r] = exp2_softmax(sc[b][r] - mu);
+                    l += sc[b][r];
+                }
+            V pf[NV];
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    pf[0][r] = (__bf16)sc[0][r];
+                    pf[0][4 + r] = (__bf16)sc[1][r];
+                }
+            } else {
+                pf[0] = sc[0];
+                pf[1] = sc[1];
+            }
+            // position of element e of a value fragment
+            auto vpos = [&](int b, int e) { return p + fc * 4 + (sizeof(T) == 2 ? (e & 3) + (e >> 2) * 16 : b * 16 + e); };
+            bool by_row = false;
+            if (p + 32 > all) {
+                bool odd = false;
+#pragma unroll
+                for (int b = 0; b < NV; ++b)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int e = 0; e < EL; ++e) {
+                            if (vpos(b, e) >= t.kv1) vf[b][d][e] = 0.f;
+                            odd = odd || !(fabsf((float)vf[b][d][e]) < INFINITY);
+                        }
+                by_row = __any(odd);
+            }
+            if (!by_row) {
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int b = 0; b < NV; ++b) o[d] = Piece<T>::mul(vf[b][d], pf[b], o[d]);
+            } else {
+#pragma unroll 1
+                for (int r = 0; r < 16; ++r) {
+                    const int lr = __shfl(lim, r, 64);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        mfma_f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int b = 0; b < NV; ++b) {
+                            V y = vf[b][d];
+#pragma unroll
+                            for (int e = 0; e < EL; ++e)
+                                if (vpos(b, e) >= lr) y[e] = 0.f;
+                            x = Piece<T>::mul(y, pf[b], x);
+                        }
+                        if (fr == r) o[d] += x;
+                    }
+                }
+            }
+        }
+        // the lanes of a row hold different positions' weights
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (fc == 0) {
+            sm[wave][fr] = m;
+            sl[wave][fr] = l;
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) so[wave][fr][d * 16 + fc * 4 + r] = o[d][r];
+        __syncthreads();
+        // thread: row tid / 16, dims 4 (tid % 16) .. + 3 (and 64 further on)
+        const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 4;
+        if (t.j0 + row < rows) {
+        const float mt = fmaxf(fmaxf(sm[0][row], sm[1][row]), fmaxf(sm[2][row], sm[3][row]));
+        const float mu = mt == -INFINITY ? 0.f : mt;
+        float w[4], lt = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = exp2_softmax(sm[i][row] - mu);
+            lt += sl[i][row] * w[i];
+        }
+#pragma unroll
+        for (int d = d0; d < D; d += 64) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = so[0][row][d + e] * w[0] + so[1][row][d + e] * w[1] + so[2][row][d + e] * w[2] + so[3][row][d + e] * w[3];
+            if (t.part < 0) {
+                const int jr = t.j0 + row, tk = jr / a.G, gg = jr - tk * a.G;
+                const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+                attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+            } else {
+                float* ps = a.parts + ((long long)t.part * a.c.Hkv + h) * (16 * (D + 2)) + row * D + d;
+                st4(ps, x[0], x[1], x[2], x[3]);
+            }
+        }
+        if (t.part >= 0 && (threadIdx.x & 15) == 0) {
+            float* ps = a.parts + ((long long)t.part * a.c.Hkv + h) * (16 * (D + 2)) + 16 * D;
+            ps[row] = mt;
+            ps[16 + row] = lt;
+        }
+        }
+        __syncthreads();  // the next item's LDS
+    }
+}
+
+// Joins the parts of cut ranges, in their order: one workgroup per 16 rows and kv head.
+template <class T, int D, bool FRAG>
+__global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
+    const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
+    const MergeItem* merges = reinterpret_cast<const MergeItem*>(a.plan + head.merges_at);
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 4;
+    for (int w0 = blockIdx.x; w0 < head.merges * a.c.Hkv; w0 += gridDim.x) {
+        const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
+        const MergeItem t = merges[it];
+        const int j = t.j0 + row;
+        if (j >= t.count * a.G) continue;
+        const long long step = (long long)a.c.Hkv * (16 * (D + 2));
+        const float* ps = a.parts + ((long long)t.part * a.c.Hkv + h) * (16 * (D + 2));
+        float m = -INFINITY;
+        for (int i = 0; i < t.n; ++i) m = fmaxf(m, ps[i * step + 16 * D + row]);
+        const float mu = m == -INFINITY ? 0.f : m;
+        float l = 0.f, x[D / 16];
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) x[e] = 0.f;
+        for (int i = 0; i < t.n; ++i) {
+            const float w = exp2_softmax(ps[i * step + 16 * D + row] - mu);
+            l += w * ps[i * step + 16 * D + 16 + row];
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                const float4 y = ld4(ps + i * step + row * D + d0 + c * 64);
+                x[4 * c] += w * y.x;
+                x[4 * c + 1] += w * y.y;
+                x[4 * c + 2] += w * y.z;
+                x[4 * c + 3] += w * y.w;
+            }
+        }
+        const int tk = j / a.G, gg = j - tk * a.G;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)
+            attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d0 + c * 64, x[4 * c] * inv, x[4 * c + 1] * inv,
+                                x[4 * c + 2] * inv, x[4 * c + 3] * inv);
+    }
+}
+
+}  // namespace wmi
