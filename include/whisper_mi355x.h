@@ -615,6 +615,77 @@ whisper_status whisper_cache_read(whisper_cache* cache, int32_t layer, const int
 /* Length and pages of sequence seq, and the cache's free pages (host; any may be NULL). */
 whisper_status whisper_cache_info(whisper_cache* cache, int32_t seq, int32_t* length, int32_t* pages, int32_t* free_pages);
 
+/*
+ * Sampling options of one row.
+ *   temperature  0: the largest logit (lowest id on ties), the other options
+ *                and the uniform number unused; else logits are divided by it
+ *   top_k        0: off; else the top_k largest logits are kept (lowest ids
+ *                among equal ones)
+ *   top_p        1: off; else, of what top_k kept, the smallest set of largest
+ *                logits (lowest ids among equal ones) whose probability is at
+ *                least top_p of theirs together
+ *   min_p        0: off; else, of what is left, the ids with at least min_p
+ *                times the most likely one's probability
+ */
+typedef struct {
+    float temperature;
+    int32_t top_k;
+    float top_p;
+    float min_p;
+} whisper_sampling;
+
+/*
+ * Sampler: the choice of a token for every row of logits in device memory.
+ * Among the ids kept by a row's options, in the order of their numbers, the
+ * chosen one is the first whose running probability sum exceeds u times the
+ * sum of all of them, u the row's uniform number in [0, 1) (below 0 or NaN:
+ * the first kept id, 1 or more: the last). Suppressed ids, NaN and -inf are
+ * never kept; if the largest logit is +inf, only such ids are. Probabilities
+ * are taken as integers of 2^-43 of the largest, so a row's token depends on
+ * nothing but its logits, its options and u.
+ * Streams, device, threads: as for whisper_cache; whisper_sampler_run may be
+ * recorded into a graph and takes the options that are set when it runs
+ * (except that suppress lists stay on or off as they were).
+ */
+typedef struct whisper_sampler whisper_sampler;
+
+/* Creates a sampler for rows of n_vocab (1..2^20) logits, at most max_rows
+ * (1..65536) a call, on HIP device `device` (WHISPER_NO_DEVICE: for the checks
+ * of arguments; run returns WHISPER_E_STATE). Options at first: temperature 1,
+ * the filters off, nothing suppressed. Errors: E_INVAL, E_NOMEM, E_DEVICE;
+ * whisper_sampler_error(NULL) then holds the message. */
+whisper_status whisper_sampler_create(int32_t n_vocab, int32_t max_rows, int device, whisper_sampler** out);
+
+/* Waits for the sampler's stream and frees what the sampler owns. NULL is allowed. */
+void whisper_sampler_destroy(whisper_sampler* sampler);
+
+/* Last error message, as whisper_cache_error. */
+const char* whisper_sampler_error(const whisper_sampler* sampler);
+
+/* Stream of the following calls, as whisper_cache_set_stream. */
+whisper_status whisper_sampler_set_stream(whisper_sampler* sampler, void* hip_stream);
+
+/* Sets the options of rows 0 .. n - 1 (host array; the others keep theirs) and
+ * the n_suppress ids never chosen in any row (host array, replaces the
+ * former list). Waits for the sampler's stream. Errors: E_INVAL, E_STATE (the
+ * stream is recording a graph). */
+whisper_status whisper_sampler_options(whisper_sampler* sampler, const whisper_sampling* rows, int32_t n,
+                                       const int32_t* suppress, int32_t n_suppress);
+
+/*
+ * Enqueues the choice for rows 0 .. n_rows - 1 (device memory throughout):
+ *   logits      [n_rows][row_stride] of type dtype (WHISPER_DTYPE_*), row_stride
+ *               in elements (0: n_vocab); read only
+ *   uniforms    fp32 [n_rows]
+ *   tokens      int32 [n_rows]: the chosen ids, -1 for a row without any to choose
+ *   logprobs    NULL or fp32 [n_rows]: the chosen id's log-probability among
+ *               all ids that are not suppressed, at temperature 1 and without
+ *               the filters (-inf where the token is -1)
+ * Errors: E_INVAL.
+ */
+whisper_status whisper_sampler_run(whisper_sampler* sampler, const void* logits, int32_t dtype, int32_t n_rows,
+                                   int64_t row_stride, const float* uniforms, int32_t* tokens, float* logprobs);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,6 +31,8 @@ EXPORTS = (
     "whisper_cache_create", "whisper_cache_destroy", "whisper_cache_error", "whisper_cache_set_stream",
     "whisper_cache_extend", "whisper_cache_append", "whisper_cache_attend", "whisper_cache_truncate",
     "whisper_cache_fork", "whisper_cache_compact", "whisper_cache_read", "whisper_cache_info",
+    "whisper_sampler_create", "whisper_sampler_destroy", "whisper_sampler_error", "whisper_sampler_set_stream",
+    "whisper_sampler_options", "whisper_sampler_run",
 )
 
 
@@ -65,6 +67,10 @@ class whisper_cache_params(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "dtype", "n_layer", "n_head", "n_kv_head", "head_size", "page_size", "n_pages", "max_seqs", "max_positions",
         "max_tokens")]
+
+
+class whisper_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
 NO_DEVICE = -1
@@ -119,6 +125,12 @@ def load(path: str = LIB_PATH) -> C.CDLL:
         "whisper_cache_compact": (i32, [vp]),
         "whisper_cache_read": (i32, [vp, i32, pi32, i32, vp, vp, i64, i64]),
         "whisper_cache_info": (i32, [vp, i32, pi32, pi32, pi32]),
+        "whisper_sampler_create": (i32, [i32, i32, C.c_int, C.POINTER(vp)]),
+        "whisper_sampler_destroy": (None, [vp]),
+        "whisper_sampler_error": (C.c_char_p, [vp]),
+        "whisper_sampler_set_stream": (i32, [vp, vp]),
+        "whisper_sampler_options": (i32, [vp, C.POINTER(whisper_sampling), i32, pi32, i32]),
+        "whisper_sampler_run": (i32, [vp, vp, i32, i32, i64, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -386,6 +398,72 @@ class Cache:
         a, b, c = C.c_int32(), C.c_int32(), C.c_int32()
         self._check(load().whisper_cache_info(self.h, seq, C.byref(a), C.byref(b), C.byref(c)))
         return a.value, b.value, c.value
+
+
+def _sampling(n: int, temperature, top_k, top_p, min_p):
+    """whisper_sampling[n] from scalars or lists of n values."""
+    rows = (whisper_sampling * max(1, n))()
+    for name, x, kind in (("temperature", temperature, np.float32), ("top_k", top_k, np.int64),
+                          ("top_p", top_p, np.float32), ("min_p", min_p, np.float32)):
+        a = np.asarray(x)
+        if a.ndim > 1 or (a.ndim == 1 and a.size != n) or (kind == np.int64 and not np.issubdtype(a.dtype, np.integer)):
+            raise WhisperError(E_INVAL, f"{name}: one value, or one per row")
+        a = np.broadcast_to(a.astype(kind), (n,))
+        if kind == np.int64 and n and (a.min() < -2**31 or a.max() >= 2**31):
+            raise WhisperError(E_INVAL, f"{name}: a 32-bit integer is needed")
+        for i in range(n):
+            setattr(rows[i], name, a[i].item())
+    return rows
+
+
+class Sampler:
+    """Choice of tokens from logits in device memory (whisper_sampler_*).
+    Addresses are device addresses; run enqueues and returns."""
+
+    def __init__(self, n_vocab: int, max_rows: int, device: int = 0):
+        h = C.c_void_p()
+        st = load().whisper_sampler_create(n_vocab, max_rows, device, C.byref(h))
+        self.h = None
+        self._check(st)
+        self.h, self.n_vocab, self.max_rows = h, n_vocab, max_rows
+
+    def close(self):
+        if getattr(self, "h", None):
+            load().whisper_sampler_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def _check(self, st):
+        if st != OK:
+            raise WhisperError(st, load().whisper_sampler_error(self.h).decode())
+
+    def set_stream(self, stream_handle: int | None):
+        self._check(load().whisper_sampler_set_stream(self.h, C.c_void_p(stream_handle or None)))
+
+    def options(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, suppress=(), n_rows: int | None = None):
+        """Options of rows 0 .. n_rows - 1 (all rows when None): one value for
+        all of them, or lists of n_rows values; suppress for every row."""
+        sizes = [np.asarray(x).size for x in (temperature, top_k, top_p, min_p) if np.asarray(x).ndim == 1]
+        n = n_rows if n_rows is not None else sizes[0] if sizes else self.max_rows
+        rows = _sampling(n, temperature, top_k, top_p, min_p)
+        s = _ints(suppress)
+        self._check(load().whisper_sampler_options(self.h, rows, n, _ptr(s, C.c_int32), s.size))
+
+    def run(self, logits: int, dtype: int, n_rows: int, uniforms: int, tokens: int, logprobs: int = 0,
+            row_stride: int = 0):
+        self._check(load().whisper_sampler_run(self.h, logits, dtype, n_rows, row_stride, uniforms, tokens,
+                                               logprobs or None))
 
 
 def test_batcher(arrival_us, user_id, segment_id, max_new_tokens, slots, encode_batch, refill_min,

@@ -1,14 +1,18 @@
 // C ABI of the operators that work on a program's own device memory
-// (include/whisper_mi355x.h): the paged key/value cache. Argument checks,
+// (include/whisper_mi355x.h): the paged key/value cache and the sampler. Argument checks,
 // error codes and messages; every check runs before any device work.
 #include <hip/hip_runtime.h>
 
+#include <math.h>
+
 #include <memory>
 #include <new>
+#include <set>
 #include <string>
 #include <vector>
 
 #include "cache.h"
+#include "sampler.h"
 
 namespace {
 
@@ -19,6 +23,13 @@ thread_local std::string g_error;  // last failed create of this thread, calls w
 struct whisper_cache {
     whisper_cache_params p;
     std::unique_ptr<wmi::PagedCache> impl;
+    std::string err;
+    bool broken = false;
+};
+
+struct whisper_sampler {
+    int n_vocab, max_rows;
+    std::unique_ptr<wmi::Sampler> impl;
     std::string err;
     bool broken = false;
 };
@@ -84,6 +95,14 @@ std::string check_cache(const whisper_cache_params& p) {
     if (p.max_tokens < 1 || p.max_tokens > (1 << 20)) return "max_tokens must be in 1..1048576";
     if ((int64_t)p.max_seqs * ((p.max_positions + p.page_size - 1) / p.page_size) > (1 << 28))
         return "max_seqs x max_positions / page_size must not exceed 268435456";
+    return "";
+}
+
+std::string check_sampling(const whisper_sampling& o) {
+    if (!(o.temperature >= 0.f) || !isfinite(o.temperature)) return "temperature must be finite and >= 0";
+    if (o.top_k < 0) return "top_k must be >= 0";
+    if (!(o.top_p > 0.f && o.top_p <= 1.f)) return "top_p must be in (0, 1]";
+    if (!(o.min_p >= 0.f && o.min_p <= 1.f)) return "min_p must be in 0..1";
     return "";
 }
 
@@ -255,6 +274,81 @@ whisper_status whisper_cache_info(whisper_cache* cache, int32_t seq, int32_t* le
     if (pages) *pages = (int32_t)b.pages(seq).size();
     if (free_pages) *free_pages = b.free_pages();
     return WHISPER_OK;
+}
+
+whisper_status whisper_sampler_create(int32_t n_vocab, int32_t max_rows, int device, whisper_sampler** out) {
+    whisper_sampler* none = nullptr;
+    if (!out) return fail(none, WHISPER_E_INVAL, "out must not be NULL");
+    if (n_vocab < 1 || n_vocab > (1 << 20)) return fail(none, WHISPER_E_INVAL, "n_vocab must be in 1..1048576");
+    if (max_rows < 1 || max_rows > (1 << 16)) return fail(none, WHISPER_E_INVAL, "max_rows must be in 1..65536");
+    WMI_TRY(check_device(device));
+    std::unique_ptr<whisper_sampler> s(new (std::nothrow) whisper_sampler());
+    if (!s) return fail(none, WHISPER_E_NOMEM, "host allocation failed");
+    s->n_vocab = n_vocab;
+    s->max_rows = max_rows;
+    WMI_TRY(guarded(none, [&]() -> whisper_status {
+        s->impl = wmi::make_sampler(n_vocab, max_rows, device);
+        return WHISPER_OK;
+    }));
+    *out = s.release();
+    return WHISPER_OK;
+}
+
+void whisper_sampler_destroy(whisper_sampler* sampler) { delete sampler; }
+
+const char* whisper_sampler_error(const whisper_sampler* sampler) {
+    return sampler ? sampler->err.c_str() : g_error.c_str();
+}
+
+whisper_status whisper_sampler_set_stream(whisper_sampler* sampler, void* hip_stream) {
+    WMI_TRY(usable(sampler));
+    return guarded(sampler, [&]() -> whisper_status {
+        sampler->impl->set_stream(hip_stream);
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_sampler_options(whisper_sampler* sampler, const whisper_sampling* rows, int32_t n,
+                                       const int32_t* suppress, int32_t n_suppress) {
+    WMI_TRY(usable(sampler));
+    if (n < 0 || n > sampler->max_rows) return fail(sampler, WHISPER_E_INVAL, "n must be in 0..max_rows");
+    if ((n > 0 && !rows) || n_suppress < 0 || (n_suppress > 0 && !suppress))
+        return fail(sampler, WHISPER_E_INVAL, "rows and suppress must not be NULL");
+    for (int i = 0; i < n; ++i) {
+        const std::string bad = check_sampling(rows[i]);
+        if (!bad.empty()) return fail(sampler, WHISPER_E_INVAL, "row " + std::to_string(i) + ": " + bad);
+    }
+    std::set<int> ids;
+    for (int i = 0; i < n_suppress; ++i) {
+        if (suppress[i] < 0 || suppress[i] >= sampler->n_vocab)
+            return fail(sampler, WHISPER_E_INVAL, "suppressed id out of range");
+        ids.insert(suppress[i]);
+    }
+    if ((int)ids.size() >= sampler->n_vocab) return fail(sampler, WHISPER_E_INVAL, "every id would be suppressed");
+    return guarded(sampler, [&]() -> whisper_status {
+        sampler->impl->options(rows, n, suppress, n_suppress);
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_sampler_run(whisper_sampler* sampler, const void* logits, int32_t dtype, int32_t n_rows,
+                                   int64_t row_stride, const float* uniforms, int32_t* tokens, float* logprobs) {
+    WMI_TRY(usable(sampler));
+    if (dtype != WHISPER_DTYPE_F32 && dtype != WHISPER_DTYPE_BF16)
+        return fail(sampler, WHISPER_E_INVAL, "dtype must be 0 (fp32) or 1 (bf16)");
+    if (n_rows < 0 || n_rows > sampler->max_rows) return fail(sampler, WHISPER_E_INVAL, "n_rows must be in 0..max_rows");
+    if (row_stride != 0 && (row_stride < sampler->n_vocab || row_stride > ((int64_t)1 << 40)))
+        return fail(sampler, WHISPER_E_INVAL, "row_stride must be 0 or at least n_vocab");
+    if (n_rows == 0) return WHISPER_OK;
+    if (!logits || !uniforms || !tokens) return fail(sampler, WHISPER_E_INVAL, "device pointers must not be NULL");
+    const size_t es = dtype == WHISPER_DTYPE_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(uniforms) % 4 ||
+        reinterpret_cast<uintptr_t>(tokens) % 4 || reinterpret_cast<uintptr_t>(logprobs) % 4)
+        return fail(sampler, WHISPER_E_INVAL, "a device pointer is not aligned to its type");
+    return guarded(sampler, [&]() -> whisper_status {
+        sampler->impl->run(logits, dtype, n_rows, row_stride ? row_stride : sampler->n_vocab, uniforms, tokens, logprobs);
+        return WHISPER_OK;
+    });
 }
 
 }  // extern "C"

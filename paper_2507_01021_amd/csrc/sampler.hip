@@ -1,0 +1,83 @@
+// The sampler's device side: options in device memory and the launch.
+#include <string.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "device.h"
+#include "sampler.h"
+#include "sampling.h"
+
+namespace wmi {
+
+namespace {
+
+class SamplerImpl final : public Sampler {
+   public:
+    SamplerImpl(int n_vocab, int max_rows, int device) : V_(n_vocab), R_(max_rows), dev_(device) {
+        if (dev_ == WHISPER_NO_DEVICE) return;
+        DeviceScope scope(dev_);
+        const size_t words = (size_t)V_ / 32 + 1;
+        void* q = nullptr;
+        if (hipMalloc(&q, R_ * sizeof(SampleRow) + words * sizeof(unsigned)) != hipSuccess) {
+            (void)hipGetLastError();
+            throw ArgError(WHISPER_E_NOMEM, "device allocation of the sampler's options failed");
+        }
+        rows_ = static_cast<SampleRow*>(q);
+        never_ = reinterpret_cast<unsigned*>(rows_ + R_);
+        const std::vector<SampleRow> d(R_, SampleRow{1.f, 0, 1.f, 0.f});
+        WMI_HIP(hipMemcpy(rows_, d.data(), d.size() * sizeof(SampleRow), hipMemcpyHostToDevice));
+    }
+    ~SamplerImpl() override {
+        if (dev_ == WHISPER_NO_DEVICE) return;
+        int old = -1;
+        (void)hipGetDevice(&old);
+        (void)hipSetDevice(dev_);
+        (void)hipStreamSynchronize(st_);
+        if (rows_) (void)hipFree(rows_);
+        if (old >= 0) (void)hipSetDevice(old);
+    }
+    void set_stream(void* s) override {
+        if (dev_ == WHISPER_NO_DEVICE || s == st_) return;
+        DeviceScope scope(dev_);
+        WMI_HIP(hipStreamSynchronize(st_));
+        st_ = static_cast<hipStream_t>(s);
+    }
+    // Waits for the work enqueued so far: options change between steps rarely.
+    void options(const whisper_sampling* rows, int n, const int32_t* suppress, int n_suppress) override {
+        if (dev_ == WHISPER_NO_DEVICE) return;
+        DeviceScope scope(dev_);
+        if (capturing(st_)) throw ArgError(WHISPER_E_STATE, "the stream is recording a graph: only run may be recorded");
+        std::vector<SampleRow> h(n);
+        for (int i = 0; i < n; ++i) h[i] = SampleRow{rows[i].temperature, rows[i].top_k, rows[i].top_p, rows[i].min_p};
+        std::vector<unsigned> m((size_t)V_ / 32 + 1, 0u);
+        for (int i = 0; i < n_suppress; ++i) m[suppress[i] >> 5] |= 1u << (suppress[i] & 31);
+        WMI_HIP(hipStreamSynchronize(st_));
+        if (n) WMI_HIP(hipMemcpy(rows_, h.data(), h.size() * sizeof(SampleRow), hipMemcpyHostToDevice));
+        WMI_HIP(hipMemcpy(never_, m.data(), m.size() * sizeof(unsigned), hipMemcpyHostToDevice));
+        use_never_ = n_suppress > 0;
+    }
+    void run(const void* logits, int dtype, int n_rows, int64_t ld, const float* u, int32_t* tok, float* logp) override {
+        if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the sampler has no device");
+        DeviceScope scope(dev_);
+        const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp};
+        if (dtype == WHISPER_DTYPE_BF16) hipLaunchKernelGGL(sample_kernel<bf16>, dim3(n_rows), dim3(smp::THREADS), 0, st_, a);
+        else hipLaunchKernelGGL(sample_kernel<float>, dim3(n_rows), dim3(smp::THREADS), 0, st_, a);
+        WMI_HIP(hipGetLastError());
+    }
+
+   private:
+    int V_, R_, dev_;
+    hipStream_t st_ = nullptr;
+    SampleRow* rows_ = nullptr;
+    unsigned* never_ = nullptr;
+    bool use_never_ = false;
+};
+
+}  // namespace
+
+std::unique_ptr<Sampler> make_sampler(int n_vocab, int max_rows, int device) {
+    return std::unique_ptr<Sampler>(new SamplerImpl(n_vocab, max_rows, device));
+}
+
+}  // namespace wmi
