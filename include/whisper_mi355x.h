@@ -98,6 +98,13 @@ enum { WHISPER_DTYPE_F32 = 0, WHISPER_DTYPE_BF16 = 1 };
  *                     at encode time, so its first decode step returns its
  *                     first token. The tokens are the same either way.
  *                     CTC models: 0
+ *   paged             decoder models: 0 gives every slot a self-attention
+ *                     cache of n_text_ctx positions of its own; 1 keeps these
+ *                     caches in pages of 64 positions, as many as a segment's
+ *                     prompt and tokens need, so that a slot can be forked
+ *                     (whisper_slot_fork). The self-attention is then that of
+ *                     whisper_cache_attend, whose sums are grouped otherwise:
+ *                     logits agree within rounding, not to the bit. CTC models: 0
  */
 typedef struct {
     int32_t n_mels, n_audio_ctx, n_audio_state, n_audio_head, n_audio_layer;
@@ -112,6 +119,7 @@ typedef struct {
     int32_t max_wait_ms;
     int32_t ctc_beam;
     int32_t prefill;
+    int32_t paged;
 } whisper_params;
 
 /*
@@ -284,6 +292,54 @@ whisper_status whisper_batch_decode_step(whisper_ctx* ctx, const int32_t* slots,
  */
 whisper_status whisper_batch_decode_step_noalloc(whisper_ctx* ctx, const int32_t* slots, int32_t n,
                                                  int32_t* out_tokens_dev);
+
+/*
+ * Sampling options of one row.
+ *   temperature  0: the largest logit (lowest id on ties), the other options
+ *                and the uniform number unused; else logits are divided by it
+ *   top_k        0: off; else the top_k largest logits are kept (lowest ids
+ *                among equal ones)
+ *   top_p        1: off; else, of what top_k kept, the smallest set of largest
+ *                logits (lowest ids among equal ones) whose probability is at
+ *                least top_p of theirs together
+ *   min_p        0: off; else, of what is left, the ids with at least min_p
+ *                times the most likely one's probability
+ */
+typedef struct {
+    float temperature;
+    int32_t top_k;
+    float top_p;
+    float min_p;
+} whisper_sampling;
+
+/*
+ * One decoder step as whisper_batch_decode_step whose tokens are drawn: a
+ * generating slot's token is chosen from the step's logits by options[i] and
+ * the uniform number uniforms[i] in [0, 1) as whisper_sampler_run does, after
+ * the filters of whisper_set_decoding, and is the slot's next input.
+ *   options, uniforms  n entries (host), one per listed slot; a slot inside its
+ *                 prompt uses none
+ *   out_tokens    n int32 (host): the drawn tokens, -1 inside the prompt
+ *   out_logprobs  NULL or n fp32 (host): the drawn token's log-probability
+ *                 at temperature 1 among all ids the filters leave (the sum of
+ *                 these ranks candidates), 0 inside the prompt
+ * With temperature 0 in every row the tokens are whisper_batch_decode_step's.
+ * n = 0 is a no-op. Errors: E_INVAL, E_STATE (slot idle).
+ */
+whisper_status whisper_batch_decode_sample(whisper_ctx* ctx, const int32_t* slots, int32_t n,
+                                           const whisper_sampling* options, const float* uniforms, int32_t* out_tokens,
+                                           float* out_logprobs);
+
+/*
+ * Makes the n idle slots dst active copies of the active slot src: same
+ * prompt, tokens so far, position, limits and encoder result. They continue
+ * on their own (candidates of one segment, drawn apart by
+ * whisper_batch_decode_sample). The cross-attention cache is shared, and so
+ * are the self-attention cache's full pages; a partly filled page is copied.
+ * n = 0 is a no-op. Errors: E_STATE (src idle, a destination active, the
+ * context's params.paged is 0), E_INVAL, E_CAPACITY.
+ */
+whisper_status whisper_slot_fork(whisper_ctx* ctx, int32_t src, const int32_t* dst, int32_t n);
 
 /* Copies the tokens generated so far in `slot` (at most cap) to dst (host)
  * and their count to *n_out. */
@@ -614,25 +670,6 @@ whisper_status whisper_cache_read(whisper_cache* cache, int32_t layer, const int
 
 /* Length and pages of sequence seq, and the cache's free pages (host; any may be NULL). */
 whisper_status whisper_cache_info(whisper_cache* cache, int32_t seq, int32_t* length, int32_t* pages, int32_t* free_pages);
-
-/*
- * Sampling options of one row.
- *   temperature  0: the largest logit (lowest id on ties), the other options
- *                and the uniform number unused; else logits are divided by it
- *   top_k        0: off; else the top_k largest logits are kept (lowest ids
- *                among equal ones)
- *   top_p        1: off; else, of what top_k kept, the smallest set of largest
- *                logits (lowest ids among equal ones) whose probability is at
- *                least top_p of theirs together
- *   min_p        0: off; else, of what is left, the ids with at least min_p
- *                times the most likely one's probability
- */
-typedef struct {
-    float temperature;
-    int32_t top_k;
-    float top_p;
-    float min_p;
-} whisper_sampling;
 
 /*
  * Sampler: the choice of a token for every row of logits in device memory.

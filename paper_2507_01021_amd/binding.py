@@ -23,7 +23,7 @@ CHOICE_DEC_PROJ, CHOICE_PREFILL_CROSS, CHOICE_ENC_GEMM = 0, 1, 2
 EXPORTS = (
     "whisper_params_from_blob", "whisper_ctx_create", "whisper_ctx_destroy", "whisper_last_error",
     "whisper_ctx_set_stream", "whisper_batch_encode", "whisper_batch_decode_step",
-    "whisper_batch_decode_step_noalloc",
+    "whisper_batch_decode_step_noalloc", "whisper_batch_decode_sample", "whisper_slot_fork",
     "whisper_slot_tokens", "whisper_batch_transcribe", "whisper_batch_serve", "whisper_debug_copy",
     "whisper_profile_enable", "whisper_profile_read", "whisper_time_kernel", "whisper_stats_read",
     "whisper_set_decoding", "whisper_test_batcher", "whisper_test_greedy_keys",
@@ -41,7 +41,8 @@ class whisper_params(C.Structure):
         "n_mels", "n_audio_ctx", "n_audio_state", "n_audio_head", "n_audio_layer",
         "n_vocab", "n_text_ctx", "n_text_state", "n_text_head", "n_text_layer",
         "dtype", "max_slots", "max_encode_batch", "pad_mode", "refill_min", "batch_policy",
-        "step_cost_us", "max_wait_ms", "ctc_beam", "prefill")]
+        "step_cost_us", "max_wait_ms", "ctc_beam", "prefill",
+        "paged")]
 
 
 class whisper_segment(C.Structure):
@@ -97,6 +98,9 @@ def load(path: str = LIB_PATH) -> C.CDLL:
         "whisper_batch_encode": (i32, [vp, C.POINTER(whisper_segment), i32, pi32]),
         "whisper_batch_decode_step": (i32, [vp, pi32, i32, pi32, pi32, C.POINTER(C.c_float)]),
         "whisper_batch_decode_step_noalloc": (i32, [vp, pi32, i32, vp]),
+        "whisper_batch_decode_sample": (i32, [vp, pi32, i32, C.POINTER(whisper_sampling), C.POINTER(C.c_float), pi32,
+                                             C.POINTER(C.c_float)]),
+        "whisper_slot_fork": (i32, [vp, i32, pi32, i32]),
         "whisper_slot_tokens": (i32, [vp, i32, pi32, i32, pi32]),
         "whisper_batch_transcribe": (i32, [vp, C.POINTER(whisper_segment), i32, pi32, i64,
                                           C.POINTER(whisper_result)]),
@@ -209,13 +213,13 @@ class Context:
 
     def __init__(self, blob: np.ndarray, max_slots: int = 32, max_encode_batch: int = 0,
                  pad_mode: int = 0, refill_min: int = 0, device: int = 0, batch_policy: int = 0,
-                 step_cost_us: int = 0, max_wait_ms: int = 0, ctc_beam: int = 0, prefill: int = 0):
+                 step_cost_us: int = 0, max_wait_ms: int = 0, ctc_beam: int = 0, prefill: int = 0, paged: int = 0):
         lib = load()
         p = params_from_blob(blob)
         p.max_slots, p.max_encode_batch, p.pad_mode, p.refill_min = (
             max_slots, max_encode_batch, pad_mode, refill_min)
         p.batch_policy, p.step_cost_us, p.max_wait_ms = batch_policy, step_cost_us, max_wait_ms
-        p.ctc_beam, p.prefill = ctc_beam, prefill
+        p.ctc_beam, p.prefill, p.paged = ctc_beam, prefill, paged
         self.params = p
         h = C.c_void_p()
         _check(lib.whisper_ctx_create(C.byref(p), blob.ctypes.data, blob.nbytes, device, C.byref(h)))
@@ -268,6 +272,24 @@ class Context:
         sl = np.ascontiguousarray(slots, dtype=np.int32)
         self._check(load().whisper_batch_decode_step_noalloc(self.h, _ptr(sl, C.c_int32), sl.size,
                                                              C.c_void_p(out_tokens_dev or None)))
+
+    def decode_sample(self, slots, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        """One step with drawn tokens; options are one value or one per slot.
+        Returns (tokens, log-probabilities)."""
+        sl = np.ascontiguousarray(slots, dtype=np.int32)
+        u = np.ascontiguousarray(uniforms, dtype=np.float32)
+        if u.shape != sl.shape:
+            raise WhisperError(E_INVAL, "one uniform number per slot")
+        rows = _sampling(sl.size, temperature, top_k, top_p, min_p)
+        toks, lp = np.empty(sl.size, dtype=np.int32), np.empty(sl.size, dtype=np.float32)
+        self._check(load().whisper_batch_decode_sample(self.h, _ptr(sl, C.c_int32), sl.size, rows, _ptr(u, C.c_float),
+                                                       _ptr(toks, C.c_int32), _ptr(lp, C.c_float)))
+        return toks, lp
+
+    def fork(self, src: int, dst):
+        """Makes the idle slots dst copies of slot src (paged contexts)."""
+        d = _ints(dst)
+        self._check(load().whisper_slot_fork(self.h, src, _ptr(d, C.c_int32), d.size))
 
     def slot_tokens(self, slot: int, cap: int = 448):
         buf = np.empty(cap, dtype=np.int32)

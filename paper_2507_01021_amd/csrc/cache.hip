@@ -145,7 +145,7 @@ class PagedCacheT final : public PagedCache {
             no_capture();
         }
         std::vector<PageCopy> copies;
-        book_.fork(src, dst, n, copies);
+        book_.fork(src, book_.length(src), dst, n, copies);
         if (dev_ == WHISPER_NO_DEVICE) return;
         std::vector<int> upd;
         for (int i = 0; i < n; ++i) {

@@ -14,6 +14,7 @@
 #include "batcher.h"
 #include "common.h"
 #include "engine.h"
+#include "sampler.h"
 
 namespace {
 
@@ -107,6 +108,8 @@ std::string check_params(const whisper_params& p, const whisper_params& blob) {
     if (p.ctc_beam < 0 || p.ctc_beam > 16) return "ctc_beam must be in 0..16";
     if (p.prefill != 0 && p.prefill != 1) return "prefill must be 0 or 1";
     if (p.prefill != 0 && p.n_text_layer == 0) return "prefill needs a decoder model";
+    if (p.paged != 0 && p.paged != 1) return "paged must be 0 or 1";
+    if (p.paged != 0 && p.n_text_layer == 0) return "paged caches need a decoder model";
     if (p.ctc_beam > 1 && (p.n_text_layer != 0 || p.n_vocab > 4096))
         return "ctc_beam >= 2 needs a CTC model with n_vocab <= 4096";
     return "";
@@ -139,7 +142,8 @@ struct EngineBackend : wmi::BatchBackend {
         descs.resize(n);
         for (int k = 0; k < n; ++k) {
             const whisper_segment& s = segs[idx[k]];
-            descs[k] = wmi::SegmentDesc{s.audio, s.n_samples, s.audio_on_device == 1, s.prompt, s.n_prompt};
+            descs[k] = wmi::SegmentDesc{s.audio, s.n_samples, s.audio_on_device == 1, s.prompt, s.n_prompt,
+                                        s.max_new_tokens};
             steps[slots[k]] = c->p.prefill ? s.n_prompt - 1 : 0;  // prefilled prompt positions
         }
         c->eng->encode(descs.data(), n, slots, realtime);
@@ -265,7 +269,7 @@ struct CtcBackend : wmi::BatchBackend {
         std::vector<wmi::SegmentDesc> d(n);
         for (int k = 0; k < n; ++k) {
             const whisper_segment& s = segs[idx[k]];
-            d[k] = wmi::SegmentDesc{s.audio, s.n_samples, s.audio_on_device == 1, nullptr, 0};
+            d[k] = wmi::SegmentDesc{s.audio, s.n_samples, s.audio_on_device == 1, nullptr, 0, 0};
         }
         int mark = -1;
         const int ticket = c->eng->encode_ctc(d.data(), n, &mark);
@@ -413,7 +417,7 @@ whisper_status whisper_batch_encode(whisper_ctx* ctx, const whisper_segment* seg
         return guarded(ctx, [&]() -> whisper_status {
             std::vector<wmi::SegmentDesc> d(n);
             for (int i = 0; i < n; ++i)
-                d[i] = wmi::SegmentDesc{segs[i].audio, segs[i].n_samples, segs[i].audio_on_device == 1, nullptr, 0};
+                d[i] = wmi::SegmentDesc{segs[i].audio, segs[i].n_samples, segs[i].audio_on_device == 1, nullptr, 0, 0};
             ctx->eng->encode_ctc(d.data(), n, nullptr);
             ctx->eng->sync();
             ctx->stats.encode_passes += 1;
@@ -436,7 +440,7 @@ whisper_status whisper_batch_encode(whisper_ctx* ctx, const whisper_segment* seg
         std::vector<wmi::SegmentDesc> d(n);
         for (int i = 0; i < n; ++i)
             d[i] = wmi::SegmentDesc{segs[i].audio, segs[i].n_samples, segs[i].audio_on_device == 1, segs[i].prompt,
-                                    segs[i].n_prompt};
+                                    segs[i].n_prompt, segs[i].max_new_tokens};
         ctx->eng->encode(d.data(), n, slots, true);
         ctx->stats.encode_passes += (n + ctx->p.max_encode_batch - 1) / ctx->p.max_encode_batch;
         ctx->stats.segments_encoded += n;
@@ -514,6 +518,68 @@ whisper_status whisper_batch_decode_step_noalloc(whisper_ctx* ctx, const int32_t
             s.steps++;
             if (s.generated == s.max_new) s.active = false;
         }
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_batch_decode_sample(whisper_ctx* ctx, const int32_t* slots, int32_t n,
+                                           const whisper_sampling* options, const float* uniforms, int32_t* out_tokens,
+                                           float* out_logprobs) {
+    if (!ctx) return fail(nullptr, WHISPER_E_INVAL, "ctx is NULL");
+    if (ctx->broken) return fail(ctx, WHISPER_E_DEVICE, "context unusable after a device error");
+    if (ctx->p.n_text_layer == 0) return fail(ctx, WHISPER_E_STATE, "not available for an encoder-only CTC model");
+    if (n < 0 || n > ctx->p.max_slots) return fail(ctx, WHISPER_E_INVAL, "n must be in 0..max_slots");
+    if (n == 0) return WHISPER_OK;
+    if (!slots || !options || !uniforms || !out_tokens)
+        return fail(ctx, WHISPER_E_INVAL, "slots, options, uniforms and out_tokens must not be NULL");
+    std::set<int> seen;
+    for (int i = 0; i < n; ++i) {
+        if (slots[i] < 0 || slots[i] >= ctx->p.max_slots)
+            return fail(ctx, WHISPER_E_CAPACITY, "slot " + std::to_string(slots[i]) + " outside 0..max_slots-1");
+        if (!seen.insert(slots[i]).second) return fail(ctx, WHISPER_E_INVAL, "slots must be distinct");
+        if (!ctx->slots[slots[i]].active)
+            return fail(ctx, WHISPER_E_STATE, "slot " + std::to_string(slots[i]) + " is idle");
+        const char* bad = wmi::sampling_fault(options[i]);
+        if (bad) return fail(ctx, WHISPER_E_INVAL, "row " + std::to_string(i) + ": " + bad);
+    }
+    return guarded(ctx, [&]() -> whisper_status {
+        ctx->eng->decode_sample(slots, n, options, uniforms, out_tokens, out_logprobs);
+        ctx->stats.decode_steps += 1;
+        ctx->stats.rows_decoded += n;
+        for (int i = 0; i < n; ++i) {
+            SlotState& s = ctx->slots[slots[i]];
+            ctx->stats.positions_attended += s.steps + 1;
+            if (s.steps >= s.n_prompt - 1) s.generated++;
+            else if (out_logprobs) out_logprobs[i] = 0.f;
+            s.steps++;
+            if (s.generated == s.max_new) s.active = false;
+        }
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_slot_fork(whisper_ctx* ctx, int32_t src, const int32_t* dst, int32_t n) {
+    if (!ctx) return fail(nullptr, WHISPER_E_INVAL, "ctx is NULL");
+    if (ctx->broken) return fail(ctx, WHISPER_E_DEVICE, "context unusable after a device error");
+    if (ctx->p.n_text_layer == 0) return fail(ctx, WHISPER_E_STATE, "not available for an encoder-only CTC model");
+    if (!ctx->p.paged) return fail(ctx, WHISPER_E_STATE, "forking needs a context with paged caches (params.paged = 1)");
+    if (n < 0 || n > ctx->p.max_slots) return fail(ctx, WHISPER_E_INVAL, "n must be in 0..max_slots");
+    if (src < 0 || src >= ctx->p.max_slots) return fail(ctx, WHISPER_E_CAPACITY, "slot outside 0..max_slots-1");
+    if (!ctx->slots[src].active) return fail(ctx, WHISPER_E_STATE, "slot " + std::to_string(src) + " is idle");
+    if (n == 0) return WHISPER_OK;
+    if (!dst) return fail(ctx, WHISPER_E_INVAL, "dst must not be NULL");
+    std::set<int> seen;
+    for (int i = 0; i < n; ++i) {
+        if (dst[i] < 0 || dst[i] >= ctx->p.max_slots)
+            return fail(ctx, WHISPER_E_CAPACITY, "slot " + std::to_string(dst[i]) + " outside 0..max_slots-1");
+        if (!seen.insert(dst[i]).second) return fail(ctx, WHISPER_E_INVAL, "slots must be distinct");
+        if (ctx->slots[dst[i]].active)
+            return fail(ctx, WHISPER_E_STATE, "slot " + std::to_string(dst[i]) + " is active");
+    }
+    return guarded(ctx, [&]() -> whisper_status {
+        ctx->eng->fork_slot(src, ctx->slots[src].steps, dst, n);
+        ctx->eng->sync();
+        for (int i = 0; i < n; ++i) ctx->slots[dst[i]] = ctx->slots[src];
         return WHISPER_OK;
     });
 }

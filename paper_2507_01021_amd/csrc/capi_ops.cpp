@@ -3,8 +3,6 @@
 // error codes and messages; every check runs before any device work.
 #include <hip/hip_runtime.h>
 
-#include <math.h>
-
 #include <memory>
 #include <new>
 #include <set>
@@ -95,14 +93,6 @@ std::string check_cache(const whisper_cache_params& p) {
     if (p.max_tokens < 1 || p.max_tokens > (1 << 20)) return "max_tokens must be in 1..1048576";
     if ((int64_t)p.max_seqs * ((p.max_positions + p.page_size - 1) / p.page_size) > (1 << 28))
         return "max_seqs x max_positions / page_size must not exceed 268435456";
-    return "";
-}
-
-std::string check_sampling(const whisper_sampling& o) {
-    if (!(o.temperature >= 0.f) || !isfinite(o.temperature)) return "temperature must be finite and >= 0";
-    if (o.top_k < 0) return "top_k must be >= 0";
-    if (!(o.top_p > 0.f && o.top_p <= 1.f)) return "top_p must be in (0, 1]";
-    if (!(o.min_p >= 0.f && o.min_p <= 1.f)) return "min_p must be in 0..1";
     return "";
 }
 
@@ -315,8 +305,8 @@ whisper_status whisper_sampler_options(whisper_sampler* sampler, const whisper_s
     if ((n > 0 && !rows) || n_suppress < 0 || (n_suppress > 0 && !suppress))
         return fail(sampler, WHISPER_E_INVAL, "rows and suppress must not be NULL");
     for (int i = 0; i < n; ++i) {
-        const std::string bad = check_sampling(rows[i]);
-        if (!bad.empty()) return fail(sampler, WHISPER_E_INVAL, "row " + std::to_string(i) + ": " + bad);
+        const char* bad = wmi::sampling_fault(rows[i]);
+        if (bad) return fail(sampler, WHISPER_E_INVAL, "row " + std::to_string(i) + ": " + bad);
     }
     std::set<int> ids;
     for (int i = 0; i < n_suppress; ++i) {

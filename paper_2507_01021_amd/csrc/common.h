@@ -141,6 +141,12 @@ __host__ __device__ inline float ord2f(uint32_t o) {
     return __builtin_bit_cast(float, u);
 }
 
+// Key of the greedy choice: the largest key is the largest logit and, among
+// equal logits, the lowest id.
+__host__ __device__ inline unsigned long long amax_key(float v, int i) {
+    return ((unsigned long long)f2ord(v) << 32) | (unsigned long long)(0xffffffffu - (unsigned)i);
+}
+
 // MFMA operand vectors.
 typedef __attribute__((__vector_size__(8 * sizeof(short)))) short bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;

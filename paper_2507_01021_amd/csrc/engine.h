@@ -20,6 +20,7 @@ struct SegmentDesc {
     bool on_device;
     const int32_t* prompt;
     int n_prompt;
+    int max_new;  // tokens to generate (decoder models): with the prompt, the positions that paged caches reserve
 };
 
 class Engine {
@@ -33,6 +34,13 @@ class Engine {
     // sync = false leaves the work queued (outputs must then be null).
     virtual void decode_step(const int* slots, int n, const int* forced, int* out_tok, float* out_logits,
                              bool sync) = 0;
+    // One step that draws each row's token: options and uniform numbers per
+    // row (host), tokens and log-probabilities out (host, the latter or null).
+    virtual void decode_sample(const int* slots, int n, const whisper_sampling* options, const float* uniforms,
+                               int* out_tok, float* out_logp) = 0;
+    // Paged caches: makes the n slots dst copies of slot src, whose next input
+    // is at position pos; enqueued on the context's stream.
+    virtual void fork_slot(int src, int pos, const int* dst, int n) = 0;
     // One greedy step (no teacher forcing, no logits) that allocates nothing:
     // its per-step temporaries live in the library's static scratch array of
     // this device; only kernels are enqueued on the context's stream and the

@@ -41,6 +41,8 @@
 
 #include "engine.h"
 #include "kernels.h"
+#include "pages.h"
+#include "sampling.h"
 
 namespace wmi {
 
@@ -281,12 +283,15 @@ template <class T>
 class EngineT final : public Engine {
    public:
     EngineT(const whisper_params& p, const void* blob, size_t bytes, int device)
-        : P_(p), dev_(device) {
+        // every slot can hold the whole text context, whatever the others share
+        : P_(p), dev_(device),
+          book_(1 << PAGE_SHIFT, p.max_slots * ((447 >> PAGE_SHIFT) + 1), p.max_slots, 448) {
         d_ = p.n_audio_state; H_ = p.n_audio_head; Le_ = p.n_audio_layer; Ld_ = p.n_text_layer;
         V_ = p.n_vocab; nm_ = p.n_mels; S_ = p.max_slots;
         EB_ = p.max_encode_batch;
         ctc_ = Ld_ == 0;
         prefill_ = !ctc_ && p.prefill != 0;
+        paged_ = !ctc_ && p.paged != 0;
         WMI_HIP(hipSetDevice(dev_));
         WMI_HIP(hipStreamCreateWithFlags(&own_stream_, hipStreamNonBlocking));
         st_ = own_stream_;
@@ -440,6 +445,7 @@ class EngineT final : public Engine {
         join_chains();
         WMI_HIP(hipSetDevice(dev_));
         if (n > 1 && !sides_known_) pick_side_streams();
+        if (paged_) reserve(segs, n, slots);
         for (int s0 = 0; s0 < n; s0 += EB_) encode_pass(segs + s0, std::min(EB_, n - s0), slots + s0);
         WMI_HIP(hipGetLastError());
         if (sync_) WMI_HIP(hipStreamSynchronize(st_));
@@ -461,7 +467,7 @@ class EngineT final : public Engine {
     void decode_step(const int* slots, int n, const int* forced, int* out_tok, float* out_logits,
                      bool sync_) override {
         WMI_HIP(hipSetDevice(dev_));
-        const bool same_list = n == (int)list_host_.size() && std::equal(slots, slots + n, list_host_.begin());
+        const bool same_list = same_rows(slots, n);
         // timing of a decode kernel (or of the whole step) brackets each launch
         // with events: such steps run as plain launches, unsplit; encoder
         // timings leave the steps as they are
@@ -480,10 +486,7 @@ class EngineT final : public Engine {
             }
         }
         join_chains();
-        if (!same_list) {
-            list_host_.assign(slots, slots + n);
-            upload(0, list_, slots, n * sizeof(int));
-        }
+        if (!same_list) put_rows(slots, n);
         if (forced) upload(1, forced_, forced, n * sizeof(int));
         // Plain steps (no teacher forcing, no per-step outputs, no kernel
         // timing) replay captured graphs of the whole step; a graph only
@@ -534,6 +537,115 @@ class EngineT final : public Engine {
         }
     }
 
+    // The rows of the next step: their slots, and with paged caches the slots
+    // whose cross-attention caches they read (a fork reads its source's).
+    bool same_rows(const int* slots, int n) const {
+        if (n != (int)list_host_.size() || !std::equal(slots, slots + n, list_host_.begin())) return false;
+        for (int i = 0; paged_ && i < n; ++i)
+            if (region_[slots[i]] != xlist_host_[i]) return false;
+        return true;
+    }
+    void put_rows(const int* slots, int n) {
+        list_host_.assign(slots, slots + n);
+        upload(0, list_, slots, n * sizeof(int));
+        if (!paged_) return;
+        xlist_host_.resize(n);
+        for (int i = 0; i < n; ++i) xlist_host_[i] = region_[slots[i]];
+        upload(4, xlist_, xlist_host_.data(), n * sizeof(int));
+    }
+
+    // -------------------------------------------------------------- paged caches
+    //
+    // Slot s holds the pages of sequence s of book_, enough for its prompt and
+    // every token it will generate (a slot's first page list never changes
+    // while it is active, so steps need no host work), and the
+    // cross-attention caches of "slot" region_[s]: its own or, after a fork, its
+    // source's. There are as many regions as slots, so an encode always finds
+    // one that no slot reads.
+    void reserve(const SegmentDesc* segs, int n, const int* slots) {
+        for (int i = 0; i < n; ++i) drop_slot(slots[i]);
+        std::vector<PageCopy> none;
+        for (int i = 0; i < n; ++i) {
+            const int want = segs[i].n_prompt + segs[i].max_new;
+            book_.extend(slots + i, &want, 1, none);
+            int r = slots[i];
+            for (int k = 0; region_used_[r] > 0; ++k) r = k;
+            region_[slots[i]] = r;
+            ++region_used_[r];
+        }
+        put_table();
+    }
+    void drop_slot(int s) {
+        const int zero = 0;
+        book_.truncate(&s, &zero, 1);
+        if (region_[s] >= 0) --region_used_[region_[s]];
+        region_[s] = -1;
+    }
+    void put_table() {
+        const int ld = book_.max_list();
+        std::vector<int> t((size_t)S_ * ld, 0);
+        for (int s = 0; s < S_; ++s) std::copy(book_.pages(s).begin(), book_.pages(s).end(), t.begin() + (size_t)s * ld);
+        upload(5, table_, t.data(), t.size() * sizeof(int));
+    }
+    PagedView view() const {
+        return PagedView{reinterpret_cast<unsigned char*>(pages_), table_, book_.max_list(), PAGE_SHIFT, Ld_, H_,
+                         (long long)(64 << PAGE_SHIFT)};
+    }
+
+    void fork_slot(int src, int pos, const int* dst, int n) override {
+        if (!paged_) throw ArgError(WHISPER_E_STATE, "forking needs a context with paged caches");
+        join_chains();
+        WMI_HIP(hipSetDevice(dev_));
+        std::vector<PageCopy> copies;
+        for (int i = 0; i < n; ++i) drop_slot(dst[i]);
+        // positions 0 .. pos - 1 are there; the rest of the reservation is the fork's own
+        const std::vector<int> rest(n, book_.length(src) - pos);
+        book_.fork(src, pos, dst, n, copies);
+        std::vector<PageCopy> none;
+        for (int i = 0; i < n; ++i) {
+            // the copied page is the fork's alone, so nothing is copied again
+            book_.extend(dst + i, &rest[i], 1, none);
+            region_[dst[i]] = region_[src];
+            ++region_used_[region_[src]];
+        }
+        put_table();
+        std::vector<int> up(dst, dst + n);
+        for (auto& c : copies) up.insert(up.end(), {c.src, c.dst});
+        upload(1, forked_, up.data(), up.size() * sizeof(int));
+        if (!copies.empty()) {
+            const long long bytes = 2LL * Ld_ * H_ * (64 << PAGE_SHIFT) * (long long)sizeof(T);
+            hipLaunchKernelGGL(paged_copy_kernel, dim3((unsigned)((bytes + PAGE_RUN - 1) / PAGE_RUN), (unsigned)copies.size()),
+                               dim3(256), 0, st_, reinterpret_cast<unsigned char*>(pages_), forked_ + n, bytes);
+        }
+        hipLaunchKernelGGL(fork_slots_kernel, dim3(n), dim3(256), 0, st_, src, forked_, seq_, gen_, pos_, npr_, stop_at_);
+        WMI_HIP(hipGetLastError());
+    }
+
+    // One step whose tokens are drawn (sampling.h) instead of the largest
+    // logit's. The rows run as one chain, with plain launches: the logits are
+    // written out and the options come anew with every step.
+    void decode_sample(const int* slots, int n, const whisper_sampling* options, const float* uniforms, int* out_tok,
+                       float* out_logp) override {
+        WMI_HIP(hipSetDevice(dev_));
+        join_chains();
+        if (!same_rows(slots, n)) put_rows(slots, n);
+        std::vector<float> up((size_t)n * 5);
+        for (int i = 0; i < n; ++i) {
+            const SampleRow o{options[i].temperature, options[i].top_k, options[i].top_p, options[i].min_p};
+            memcpy(&up[4 * (size_t)i], &o, sizeof(o));
+            up[4 * (size_t)n + i] = uniforms[i];
+        }
+        upload(1, draw_, up.data(), up.size() * sizeof(float));
+        draw_rows_ = n;
+        launch_rows(0, n, false, true, st_, 0);
+        draw_rows_ = 0;
+        WMI_HIP(hipGetLastError());
+        WMI_HIP(hipMemcpyAsync(out_tok, outtok_, n * sizeof(int), hipMemcpyDeviceToHost, st_));
+        if (out_logp) WMI_HIP(hipMemcpyAsync(out_logp, draw_logp_, n * sizeof(float), hipMemcpyDeviceToHost, st_));
+        WMI_HIP(hipStreamSynchronize(st_));
+        check_decode_error();
+    }
+
     // Rows of a step of n rows cut into chains (independent launch
     // sequences on their own streams): one chain below 32 rows (or in fp32),
     // else up to chains_ chains of whole 16-row tiles, as even as the tiles
@@ -566,6 +678,7 @@ class EngineT final : public Engine {
     // partial sums.
     struct RowBufs {
         const int* list;
+        const int* xlist;   // whose cross-attention caches the rows read
         const int* rowpos;  // null: each row is at its slot's current position
         float* dx;
         T* dz;
@@ -578,6 +691,9 @@ class EngineT final : public Engine {
         // prefill rows: groups of up to XR consecutive rows of one slot (ngroups + 1 first rows)
         const int* groups = nullptr;
         int ngroups = 0;
+        // paged caches: the plan of the rows' self-attention and its items (0: made by the step, one a row)
+        int* plan = nullptr;
+        int nitems = 0;
         // room for a split cross-attention's chunk results, and the rows it holds
         float* xpart = nullptr;
         int xrows = 0;
@@ -594,23 +710,30 @@ class EngineT final : public Engine {
         const int ks4 = fc2_split_ == 8 && (4 * d / 32) % 8 == 0 ? 8 : split_k(4 * d);
         WMI_SWITCH_E(d, hipLaunchKernelGGL((embed_ln_kernel<T, E>), dim3(n), dim3(64), 0, s, tok_emb_, pos_emb_,
                                            b.list, pos_, b.rowpos, seq_, b.dx, b.dz, dec_[0].ln1g, dec_[0].ln1b));
+        if (paged_ && !b.nitems) hipLaunchKernelGGL(paged_rows_kernel, dim3(1), dim3(128), 0, s, b.list, pos_, n, b.plan);
         for (int l = 0; l < Ld_; ++l) {
             const DecLayerW<T>& L = dec_[l];
             const long long sl = (long long)l * S_ * H_ * 64;
-            proj(L.Wqkv, 3 * d, b.dz, n, d, 1,
-                 EpiDecQKV<T>{L.bq, L.bv, b.dq, kts_ + sl * TS, vs_ + sl * TS, b.list, pos_, b.rowpos, b.rowlen, d,
-                              H_},
-                 s);
+            if (paged_)
+                proj(L.Wqkv, 3 * d, b.dz, n, d, 1, EpiPagedQKV<T>{L.bq, L.bv, b.dq, view(), l, b.list, pos_, b.rowpos, d}, s);
+            else
+                proj(L.Wqkv, 3 * d, b.dz, n, d, 1,
+                     EpiDecQKV<T>{L.bq, L.bv, b.dq, kts_ + sl * TS, vs_ + sl * TS, b.list, pos_, b.rowpos, b.rowlen, d,
+                                  H_},
+                     s);
             if (b.groups && l + 1 == Ld_) return;
             DecAttnArgs sa{b.dq, kts_ + sl * TS, vs_ + sl * TS, b.datt, b.list, b.rowlen, TS, H_, d};
             prof_begin(WHISPER_K_SELF_ATTN, s);
-            if constexpr (std::is_same<T, bf16>::value)
+            if (paged_)  // the queries carry 1/8
+                hipLaunchKernelGGL((paged_attn_kernel<T, 64, true>), dim3((b.nitems ? b.nitems : n) * H_), dim3(256), 0, s,
+                                   AttnArgs{view(), l, H_, 1, b.dq, b.datt, d, d, LOG2E, b.plan, nullptr});
+            else if constexpr (std::is_same<T, bf16>::value)
                 hipLaunchKernelGGL(self_attn_bf16_kernel, dim3(H_, n), dim3(256), 0, s, sa);
             else
                 hipLaunchKernelGGL(self_attn_kernel<T>, dim3(H_, n), dim3(256), 0, s, sa);
             prof_end(WHISPER_K_SELF_ATTN, s);
             self_out_cross_q(L, n, b.datt, b.dq, b.dx, b.dz, b.pbuf, s);
-            DecAttnArgs ca{b.dq, ktc_ + sl * TC, vc_ + sl * TC, b.datt, b.list, nullptr, TC, H_, d,
+            DecAttnArgs ca{b.dq, ktc_ + sl * TC, vc_ + sl * TC, b.datt, b.xlist, nullptr, TC, H_, d,
                            b.stamps ? b.stamps + 2 * l : nullptr};
             prof_begin(WHISPER_K_CROSS_ATTN, s);
             const bool split = n <= b.xrows && cross_split(n);
@@ -646,9 +769,10 @@ class EngineT final : public Engine {
             stamps = stamps_ + (size_t)c * Ld_ * 2;
             hipLaunchKernelGGL(stamp_reset_kernel, dim3((Ld_ + 63) / 64), dim3(64), 0, s, stamps, Ld_);
         }
-        const StepBufs b{RowBufs{list_ + r0, nullptr, dx_ + (size_t)r0 * d, dz_ + (size_t)r0 * d,
+        const StepBufs b{RowBufs{list_ + r0, xlist_ + r0, nullptr, dx_ + (size_t)r0 * d, dz_ + (size_t)r0 * d,
                                  dq_ + (size_t)r0 * d, datt_ + (size_t)r0 * d, dh_ + (size_t)r0 * 4 * d,
                                  rowlen_ + r0, gpart_ + (size_t)c * KSMAX * S_ * d, stamps, nullptr, 0,
+                                 plan_ + (size_t)c * plan_ints(S_), 0,
                                  c == 0 ? xpart_ : nullptr, c == 0 ? std::min(S_, 16) : 0},
                          logits_ + (size_t)r0 * V_, keys_ + (size_t)r0 * nkeys_, outtok_ + r0,
                          forced ? forced_ + r0 : nullptr};
@@ -675,7 +799,14 @@ class EngineT final : public Engine {
         unsigned long long* keys = sb.keys;
         const TokenFilter tf{use_never_ ? never_mask_ : nullptr, use_first_ ? first_mask_ : nullptr, list, pos_, npr_};
         // the head kernel keeps one key per row and workgroup; logits only when asked for
-        const int nk = head_argmax(tok_emb_, V_, b.dz, n, d, HeadArgs{want_logits ? logits : nullptr, keys, V_, tf}, s);
+        int nk = head_argmax(tok_emb_, V_, b.dz, n, d, HeadArgs{want_logits ? logits : nullptr, keys, V_, tf}, s);
+        if (draw_rows_) {  // the drawn tokens take the place of the largest keys
+            const SampleRow* o = reinterpret_cast<const SampleRow*>(draw_);
+            hipLaunchKernelGGL(sample_kernel<float>, dim3(n), dim3(smp::THREADS), 0, s,
+                               SampleArgs{logits, V_, V_, o, tf.never, draw_ + 4 * (size_t)n, nullptr, draw_logp_, tf.first,
+                                          list, pos_, npr_, keys});
+            nk = 1;
+        }
         hipLaunchKernelGGL(argmax_step_kernel, dim3(n), dim3(64), 0, s, keys, nk, list, pos_, npr_, seq_, gen_,
                            sb.forced, sb.outtok, eot_, stop_at_, dec_err_);
     }
@@ -683,7 +814,7 @@ class EngineT final : public Engine {
     // Scratch layout of an allocation-free step of n rows (byte offsets,
     // each region 256-byte aligned); total() is what the array must hold.
     struct NoallocLayout {
-        size_t list, rowlen, outtok, dx, dz, dq, datt, dh, part, keys, logits, end;
+        size_t list, rowlen, outtok, dx, dz, dq, datt, dh, part, keys, logits, xlist, plan, end;
     };
     NoallocLayout noalloc_layout(int n) const {
         const size_t d = d_, n16 = (size_t)(n + 15) / 16 * 16;
@@ -703,6 +834,8 @@ class EngineT final : public Engine {
         // the capacity of the fp32 model counts the rows' logits: nothing writes
         // them any more, but sizes that were refused stay refused
         L.logits = std::is_same<T, bf16>::value ? o : take((size_t)n * V_ * sizeof(float));
+        L.xlist = paged_ ? take(WHISPER_NOALLOC_MAX_ROWS * sizeof(int)) : L.list;
+        L.plan = paged_ ? take(plan_ints(n) * sizeof(int)) : o;
         L.end = o;
         return L;
     }
@@ -726,10 +859,16 @@ class EngineT final : public Engine {
         for (int i = 0; i < n; ++i) rl.slot[i] = slots[i];
         int* list = reinterpret_cast<int*>(z + L.list);
         hipLaunchKernelGGL(put_list_kernel, dim3(1), dim3(WHISPER_NOALLOC_MAX_ROWS), 0, st_, rl, list);
-        const StepBufs b{RowBufs{list, nullptr, reinterpret_cast<float*>(z + L.dx), reinterpret_cast<T*>(z + L.dz),
+        int* xlist = reinterpret_cast<int*>(z + L.xlist);
+        if (paged_) {
+            for (int i = 0; i < n; ++i) rl.slot[i] = region_[slots[i]];
+            hipLaunchKernelGGL(put_list_kernel, dim3(1), dim3(WHISPER_NOALLOC_MAX_ROWS), 0, st_, rl, xlist);
+        }
+        const StepBufs b{RowBufs{list, xlist, nullptr, reinterpret_cast<float*>(z + L.dx), reinterpret_cast<T*>(z + L.dz),
                                  reinterpret_cast<T*>(z + L.dq), reinterpret_cast<T*>(z + L.datt),
                                  reinterpret_cast<T*>(z + L.dh), reinterpret_cast<int*>(z + L.rowlen),
                                  reinterpret_cast<float*>(z + L.part), nullptr, nullptr, 0,
+                                 reinterpret_cast<int*>(z + L.plan), 0,
                                  // in the MLP's activations, which are written after the merge
                                  reinterpret_cast<float*>(z + L.dh),
                                  (int)((L.part - L.dh) / (sizeof(float) * CROSS_PART_FLOATS * H_))},
@@ -778,7 +917,9 @@ class EngineT final : public Engine {
         for (int i = 0; i < nb; ++i)
             for (int p = 0; p + 1 < segs[i].n_prompt; ++p) { rl.push_back(slots[i]); rp.push_back(p); }
         const int R = (int)rl.size();
-        std::vector<int> up(3 * (size_t)pf_cap_ + 1);  // slots | positions | group starts
+        // slots | positions | group starts, and with paged caches | regions | plan
+        const size_t base = 3 * (size_t)pf_cap_ + 1, plan_at = (base + pf_cap_ + 15) / 16 * 16;
+        std::vector<int> up(paged_ ? plan_at + plan_ints(pf_cap_) : base);
         for (int c0 = 0; c0 < R; c0 += pf_cap_) {
             const int n = std::min(pf_cap_, R - c0);
             std::copy(rl.begin() + c0, rl.begin() + c0 + n, up.begin());
@@ -788,10 +929,30 @@ class EngineT final : public Engine {
             for (int r = 0; r < n; ++r)
                 if (r == 0 || up[r] != up[r - 1] || r - gs[ng - 1] == XR) gs[ng++] = r;
             gs[ng] = n;
+            int ni = 0;
+            if (paged_) {
+                for (int r = 0; r < n; ++r) up[base + r] = region_[up[r]];
+                // up to 16 rows of a slot per attention item
+                AttnItem* items = reinterpret_cast<AttnItem*>(up.data() + plan_at + HEAD_INTS);
+                for (int r = 0; r < n; ++r) {
+                    if (r && up[r] == up[r - 1] && items[ni - 1].count < 16) {
+                        ++items[ni - 1].count;
+                        ++items[ni - 1].kv1;
+                    } else {
+                        const int p = up[pf_cap_ + r];
+                        items[ni++] = AttnItem{up[r], p, 1, r, 0, 0, p + 1, -1};
+                    }
+                }
+                *reinterpret_cast<ListHead*>(up.data() + plan_at) = ListHead{ni, 0, 0, 0, 0, {}};
+            }
             upload(3, pf_list_, up.data(), up.size() * sizeof(int));
-            RowBufs b{pf_list_, pf_list_ + pf_cap_, pf_dx_, pf_dz_, pf_dq_, pf_datt_, pf_dh_, pf_rowlen_, pf_part_};
+            RowBufs b{pf_list_, paged_ ? pf_list_ + base : pf_list_, pf_list_ + pf_cap_, pf_dx_, pf_dz_, pf_dq_, pf_datt_, pf_dh_, pf_rowlen_, pf_part_};
             b.groups = pf_list_ + 2 * (size_t)pf_cap_;
             b.ngroups = ng;
+            if (paged_) {
+                b.plan = pf_list_ + plan_at;
+                b.nitems = ni;
+            }
             decoder_layers(b, n, st_);
         }
     }
@@ -922,9 +1083,10 @@ class EngineT final : public Engine {
             for (size_t i = 0; i < h.size(); ++i) out[i] = HostElem<T>::to_f(h.data(), i);
         } else if (tensor == WHISPER_T_CROSS_K || tensor == WHISPER_T_CROSS_V) {
             need(bytes, (size_t)Ld_ * H_ * N_CTX * 64 * 4, index < S_);
+            const int region = paged_ && index >= 0 && region_[index] >= 0 ? region_[index] : index;
             std::vector<T> h((size_t)H_ * 64 * TC);
             for (int l = 0; l < Ld_; ++l) {
-                const size_t base = (((size_t)l * S_ + index) * H_) * 64 * TC;
+                const size_t base = (((size_t)l * S_ + region) * H_) * 64 * TC;
                 WMI_HIP(hipMemcpy(h.data(), (tensor == WHISPER_T_CROSS_K ? ktc_ : vc_) + base, h.size() * sizeof(T),
                                   hipMemcpyDeviceToHost));
                 for (int hh = 0; hh < H_; ++hh)
@@ -1020,15 +1182,17 @@ class EngineT final : public Engine {
         if (n < 1 || n > S_ || reps < 1) throw ArgError(WHISPER_E_INVAL, "time_cross_attn: n in 1..max_slots, reps >= 1");
         std::vector<int> rows(n);
         for (int i = 0; i < n; ++i) rows[i] = i;
-        list_host_ = rows;
-        upload(0, list_, rows.data(), n * sizeof(int));
+        if (paged_)
+            for (int i = 0; i < n; ++i)
+                if (region_[i] < 0) throw ArgError(WHISPER_E_STATE, "time_cross_attn: a slot was never encoded");
+        put_rows(rows.data(), n);
         hipEvent_t e0, e1;
         WMI_HIP(hipEventCreate(&e0));
         WMI_HIP(hipEventCreate(&e1));
         WMI_HIP(hipEventRecord(e0, st_));
         for (int i = 0; i < reps; ++i) {
             const long long sl = (long long)(i % Ld_) * S_ * H_ * 64;
-            DecAttnArgs ca{dq_, ktc_ + sl * TC, vc_ + sl * TC, datt_, list_, nullptr, TC, H_, d_};
+            DecAttnArgs ca{dq_, ktc_ + sl * TC, vc_ + sl * TC, datt_, xlist_, nullptr, TC, H_, d_};
             hipLaunchKernelGGL(cross_attn_kernel<T>, dim3(H_, n), dim3(64 * CW), 0, st_, ca);
         }
         WMI_HIP(hipEventRecord(e1, st_));
@@ -1096,7 +1260,20 @@ class EngineT final : public Engine {
     int* stop_pin_[2] = {nullptr, nullptr};
     hipEvent_t stop_ev_[2] = {nullptr, nullptr};
     int64_t snapshots_ = 0;
-    T *kts_, *vs_, *ktc_, *vc_, *dz_, *dq_, *datt_, *dh_;
+    // paged self-attention caches: pages of 64 positions, the slots' lists of
+    // them, the plans of the chains' steps; cross-attention caches by slot
+    static constexpr int PAGE_SHIFT = 6;
+    static size_t plan_ints(int rows) { return HEAD_INTS + rows * (sizeof(AttnItem) / sizeof(int)); }
+    bool paged_ = false;
+    PageBook book_;
+    std::vector<int> region_, region_used_, xlist_host_;
+    T* pages_ = nullptr;
+    int *table_ = nullptr, *plan_ = nullptr, *xlist_ = nullptr, *forked_ = nullptr, *region_of_ = nullptr;
+    // options, uniform numbers and log-probabilities of a drawn step
+    float *draw_ = nullptr, *draw_logp_ = nullptr;
+    int draw_rows_ = 0;
+    T *kts_ = nullptr, *vs_ = nullptr;
+    T *ktc_, *vc_, *dz_, *dq_, *datt_, *dh_;
     float *dx_, *logits_, *gpart_, *xpart_;
     unsigned long long* keys_;  // greedy-choice keys [S][nkeys_]
     int nkeys_ = 16;
@@ -1149,7 +1326,7 @@ class EngineT final : public Engine {
     int enc_parts_ = 2;
     hipEvent_t fork_ev_ = nullptr, join_ev_[MAXC] = {};
     // host staging
-    Stage stage_[4];
+    Stage stage_[6];
     int32_t* tokpin_ = nullptr;
     size_t tokpin_cap_ = 0, tokpin_used_ = 0;
     std::vector<PendingRead> pending_;
@@ -1322,9 +1499,9 @@ class EngineT final : public Engine {
         const int d = d_, M = nb * N_CTX;
         // small per-pass arrays: sources, valid frames, slots, prompts
         std::vector<SegSrc> src(nb);
-        // nvalid | slot_of | n_prompt | prompts, each block EB entries long (the
-        // device pointers nvalid_, slot_of_, seat_np_, seat_prompts_ use that stride)
-        std::vector<int> small((size_t)EB_ * (3 + 448), 0);
+        // nvalid | slot_of | n_prompt | prompts | regions, each block EB entries long (the device
+        // pointers nvalid_, slot_of_, seat_np_, seat_prompts_, region_of_ use that stride)
+        std::vector<int> small((size_t)EB_ * (4 + 448), 0);
         int* nv = small.data();
         int* so = nv + EB_;
         int* npv = so + EB_;
@@ -1343,6 +1520,7 @@ class EngineT final : public Engine {
             // the audio (320 samples each), the frames greedy decoding reads
             so[i] = ctc_ ? std::min(N_CTX, (s.n_samples + 319) / 320) : slots[i];
             npv[i] = s.n_prompt;
+            pr[(size_t)EB_ * 448 + i] = paged_ ? region_[slots[i]] : so[i];
             memcpy(pr + (size_t)i * 448, s.prompt, s.n_prompt * sizeof(int));
         }
         upload(2, segsrc_, src.data(), nb * sizeof(SegSrc));
@@ -1415,8 +1593,8 @@ class EngineT final : public Engine {
             prof_end(WHISPER_K_ENC_PASS, st_);
             return;
         }
-        gemm(zb_, d, 0, WcK_, d, 0, M, Ld_ * d, d, 1, EpiCrossK<T>{ktc_, slot_of_, d, H_, S_, 1.0f / d});
-        gemm(WcV_, d, 0, zb_, d, 0, Ld_ * d, M, d, 1, EpiCrossV<T>{bcV_, vc_, slot_of_, d, H_, S_, 1.0f / d});
+        gemm(zb_, d, 0, WcK_, d, 0, M, Ld_ * d, d, 1, EpiCrossK<T>{ktc_, region_of_, d, H_, S_, 1.0f / d});
+        gemm(WcV_, d, 0, zb_, d, 0, Ld_ * d, M, d, 1, EpiCrossV<T>{bcV_, vc_, region_of_, d, H_, S_, 1.0f / d});
         hipLaunchKernelGGL(seat_kernel, dim3(nb), dim3(256), 0, st_, slot_of_, seat_np_, seat_prompts_, seq_, pos_, npr_,
                            stop_at_, prefill_ ? 1 : 0);
         prof_end(WHISPER_K_ENC_PASS, st_);
@@ -1558,10 +1736,11 @@ class EngineT final : public Engine {
         const size_t d = d_, H = H_, EB = EB_, S = S_, Ld = Ld_;
         stage_audio_ = dalloc<float>(EB * 480000);
         segsrc_ = dalloc<SegSrc>(EB);
-        nvalid_ = dalloc<int>(EB * (3 + 448));
+        nvalid_ = dalloc<int>(EB * (4 + 448));
         slot_of_ = nvalid_ + EB;
         seat_np_ = slot_of_ + EB;
         seat_prompts_ = seat_np_ + EB;
+        region_of_ = seat_prompts_ + EB * 448;
         xpad_ = dalloc<float>(EB * 480400);
         power_ = dalloc<float>(EB * 3000 * DFT_PS);
         logmel_ = dalloc<float>(EB * 3000 * nm_);
@@ -1586,8 +1765,21 @@ class EngineT final : public Engine {
         stop_at_ = dalloc<int>(S);
         never_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 1);
         first_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 1);
-        kts_ = dalloc<T>(Ld * S * H * 64 * TS);
-        vs_ = dalloc<T>(Ld * S * H * TS * 64);
+        draw_ = dalloc<float>(5 * S);
+        draw_logp_ = dalloc<float>(S);
+        xlist_ = list_;
+        if (paged_) {
+            pages_ = dalloc<T>((size_t)book_.free_pages() * 2 * Ld * H * (64 << PAGE_SHIFT));
+            table_ = dalloc<int>(S * book_.max_list());
+            plan_ = dalloc<int>(MAXC * plan_ints(S_));
+            xlist_ = dalloc<int>(S);
+            forked_ = dalloc<int>(3 * S);
+            region_.assign(S, -1);
+            region_used_.assign(S, 0);
+        } else {
+            kts_ = dalloc<T>(Ld * S * H * 64 * TS);
+            vs_ = dalloc<T>(Ld * S * H * TS * 64);
+        }
         ktc_ = dalloc<T>(Ld * S * H * 64 * TC);
         vc_ = dalloc<T>(Ld * S * H * TC * 64);
         // activations multiplied by projections: whole 16-row tiles (fragment-major)
@@ -1613,7 +1805,7 @@ class EngineT final : public Engine {
             // 2048 rows give every projection two or more workgroups per CU
             // (0.13 GB at d = 1280); no more than a pass can have
             pf_cap_ = std::min<int>(2048, ((int)EB * 447 + 15) / 16 * 16);
-            pf_list_ = dalloc<int>(3 * (size_t)pf_cap_ + 1);
+            pf_list_ = dalloc<int>(4 * (size_t)pf_cap_ + 32 + (paged_ ? plan_ints(pf_cap_) : 0));
             pf_rowlen_ = dalloc<int>(pf_cap_);
             pf_dx_ = dalloc<float>((size_t)pf_cap_ * d);
             pf_dz_ = dalloc<T>((size_t)pf_cap_ * d);

@@ -16,6 +16,7 @@
 #pragma once
 
 #include "common.h"
+#include "paged.h"
 
 namespace wmi {
 
@@ -230,6 +231,50 @@ struct EpiDecQKV {
         } else {
             const int f = i - 2 * d, h = f >> 6, jj = f & 63;
             st4(v + (((long long)s * H + h) * TS + ps) * 64 + jj, a + p.a.x, b + p.a.y, c + p.a.z, e + p.a.w);
+        }
+    }
+};
+
+// The same projection over paged caches: keys and values of position p go to
+// page table[slot * ld + p / P] (P = 2^shift positions) of the pages
+// (paged.h: keys in dec_off order, values in val_off order).
+template <class T>
+struct EpiPagedQKV {
+    const float* bq;
+    const float* bv;
+    T* q;
+    PagedView c;
+    int layer;
+    const int* list;
+    const int* pos;
+    const int* rowpos;
+    int d;
+    __device__ EpiPre pre(int i, int r, int) const {
+        EpiPre p{};
+        if (i < d) {
+            p.a = ld4(bq + i);
+        } else {
+            p.s = rowpos ? rowpos[r] : pos[list[r]];
+            if (i >= 2 * d) p.a = ld4(bv + (i - 2 * d));
+        }
+        return p;
+    }
+    __device__ void operator()(int i, int r, int, float a, float b, float x, float e, const EpiPre& p) const {
+        if (i < d) {
+            st4(q + (long long)r * d + i, (a + p.a.x) * 0.125f, (b + p.a.y) * 0.125f, (x + p.a.z) * 0.125f,
+                (e + p.a.w) * 0.125f);
+            return;
+        }
+        const int page = c.table[(long long)list[r] * c.ld + (p.s >> c.shift)], ps = p.s & ((1 << c.shift) - 1);
+        const int kv = i >= 2 * d, f = i - (1 + kv) * d, h = f >> 6, jj = f & 63;
+        T* dst = c.head<T>(page, layer, kv, h);
+        if (!kv) {
+            st4(dst + dec_off<T>(ps, jj, 64), a, b, x, e);
+        } else {
+            stf(dst + val_off<T>(ps, jj, 64), a + p.a.x);
+            stf(dst + val_off<T>(ps, jj + 1, 64), b + p.a.y);
+            stf(dst + val_off<T>(ps, jj + 2, 64), x + p.a.z);
+            stf(dst + val_off<T>(ps, jj + 3, 64), e + p.a.w);
         }
     }
 };

@@ -2331,9 +2331,6 @@ struct TokenFilter {
     const int* n_prompt;    // slot -> prompt length
 };
 
-__host__ __device__ inline unsigned long long amax_key(float v, int i) {
-    return ((unsigned long long)f2ord(v) << 32) | (unsigned long long)(0xffffffffu - (unsigned)i);
-}
 // The token of a row's largest key; a row without any key (k = 0) gets
 // token 0 and sets *bad.
 __host__ __device__ inline int key_token(unsigned long long k, int* bad) {
@@ -2495,6 +2492,21 @@ __global__ void seat_kernel(const int* __restrict__ slots, const int* __restrict
         pos[s] = prefilled ? np_in[e] - 1 : 0;
         n_prompt[s] = np_in[e];
         stop_at[s] = -1;
+    }
+}
+
+// Makes slot dst[blockIdx.x] continue where slot src stands.
+__global__ void fork_slots_kernel(int src, const int* __restrict__ dst, int* __restrict__ seq, int* __restrict__ gen,
+                                  int* __restrict__ pos, int* __restrict__ n_prompt, int* __restrict__ stop_at) {
+    const int s = dst[blockIdx.x];
+    for (int i = threadIdx.x; i < 448; i += blockDim.x) {
+        seq[s * 448 + i] = seq[src * 448 + i];
+        gen[s * 448 + i] = gen[src * 448 + i];
+    }
+    if (threadIdx.x == 0) {
+        pos[s] = pos[src];
+        n_prompt[s] = n_prompt[src];
+        stop_at[s] = stop_at[src];
     }
 }
 

@@ -68,11 +68,11 @@ struct PutInts {
     int n;
     int v[PUT_INTS];
 };
-__global__ __launch_bounds__(256) void put_ints_kernel(PutInts a, int* __restrict__ dst) {
+static __global__ __launch_bounds__(256) void put_ints_kernel(PutInts a, int* __restrict__ dst) {
     for (int i = threadIdx.x; i < a.n; i += 256) dst[i] = a.v[i];
 }
 // table[at[2 i]] = at[2 i + 1]
-__global__ __launch_bounds__(256) void table_update_kernel(const int* __restrict__ at, int n, int* __restrict__ table) {
+static __global__ __launch_bounds__(256) void table_update_kernel(const int* __restrict__ at, int n, int* __restrict__ table) {
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i < n) table[at[2 * i]] = at[2 * i + 1];
 }
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedView c, const int*
 // Copies whole pages (all layers): pairs (source, destination), `bytes` each,
 // a multiple of 4096. Workgroups of a pair take 16 KiB each.
 constexpr int PAGE_RUN = 16384;
-__global__ __launch_bounds__(256) void paged_copy_kernel(unsigned char* __restrict__ pages,
+static __global__ __launch_bounds__(256) void paged_copy_kernel(unsigned char* __restrict__ pages,
                                                          const int* __restrict__ pairs, long long bytes) {
     const long long at = (long long)blockIdx.x * PAGE_RUN + threadIdx.x * 16;
     const unsigned char* s = pages + pairs[2 * blockIdx.y] * bytes + at;
@@ -499,6 +499,19 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
         for (int c = 0; c < D / 64; ++c)
             attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d0 + c * 64, x[4 * c] * inv, x[4 * c + 1] * inv,
                                 x[4 * c + 2] * inv, x[4 * c + 3] * inv);
+    }
+}
+
+// A decode step's plan, made on the device: one item per row, of the slot
+// list[r] at its position pos[list[r]].
+static __global__ __launch_bounds__(128) void paged_rows_kernel(const int* __restrict__ list,
+                                                                const int* __restrict__ pos, int n,
+                                                                int* __restrict__ plan) {
+    const int r = threadIdx.x;
+    if (r == 0) *reinterpret_cast<ListHead*>(plan) = ListHead{n, 0, 0, 0, 0, {}};
+    if (r < n) {
+        const int s = list[r], p = pos[s];
+        reinterpret_cast<AttnItem*>(plan + HEAD_INTS)[r] = AttnItem{s, p, 1, r, 0, 0, p + 1, -1};
     }
 }
 

@@ -90,18 +90,19 @@ class PageBook {
         }
     }
 
-    // Makes each (empty) sequence dst[i] a copy of src: whole pages are
-    // shared, a partly filled last page is copied.
-    void fork(int src, const int* dst, int n, std::vector<PageCopy>& copies) {
-        const bool partial = len_[src] % P_ != 0;
+    // Makes each (empty) sequence dst[i] a copy of src's first len positions:
+    // whole pages are shared, a partly filled last page is copied.
+    void fork(int src, int len, const int* dst, int n, std::vector<PageCopy>& copies) {
+        const bool partial = len % P_ != 0;
         if (partial) require(n);
+        const std::vector<int> from(pages_[src].begin(), pages_[src].begin() + pages_for(len));
         for (int i = 0; i < n; ++i) {
             const int d = dst[i];
-            pages_[d] = pages_[src];
-            len_[d] = len_[src];
+            pages_[d] = from;
+            len_[d] = len;
             if (partial) {
                 pages_[d].back() = take();
-                copies.push_back({pages_[src].back(), pages_[d].back()});
+                copies.push_back({from.back(), pages_[d].back()});
             }
             for (size_t k = 0; k + (partial ? 1 : 0) < pages_[d].size(); ++k) ++ref_[pages_[d][k]];
         }

@@ -9,6 +9,15 @@
 
 namespace wmi {
 
+// What is wrong with a row's options, or null.
+inline const char* sampling_fault(const whisper_sampling& o) {
+    if (!(o.temperature >= 0.f && o.temperature <= 3.402823466e38f)) return "temperature must be finite and >= 0";
+    if (o.top_k < 0) return "top_k must be >= 0";
+    if (!(o.top_p > 0.f && o.top_p <= 1.f)) return "top_p must be in (0, 1]";
+    if (!(o.min_p >= 0.f && o.min_p <= 1.f)) return "min_p must be in 0..1";
+    return nullptr;
+}
+
 class Sampler {
    public:
     virtual ~Sampler() {}

@@ -60,7 +60,7 @@ class SamplerImpl final : public Sampler {
     void run(const void* logits, int dtype, int n_rows, int64_t ld, const float* u, int32_t* tok, float* logp) override {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the sampler has no device");
         DeviceScope scope(dev_);
-        const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp};
+        const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp, nullptr, nullptr, nullptr, nullptr, nullptr};
         if (dtype == WHISPER_DTYPE_BF16) hipLaunchKernelGGL(sample_kernel<bf16>, dim3(n_rows), dim3(smp::THREADS), 0, st_, a);
         else hipLaunchKernelGGL(sample_kernel<float>, dim3(n_rows), dim3(smp::THREADS), 0, st_, a);
         WMI_HIP(hipGetLastError());

@@ -24,6 +24,8 @@ struct SampleRow {  // whisper_sampling
     float top_p, min_p;
 };
 
+typedef unsigned long long u64;
+
 struct SampleArgs {
     const void* logits;
     long long ld;
@@ -31,14 +33,21 @@ struct SampleArgs {
     const SampleRow* rows;
     const unsigned* never;   // [V / 32 + 1] ids never chosen, or null
     const float* u;
-    int* tok;
+    int* tok;                // or null
     float* logp;             // or null
+    // decode steps: ids not chosen as a slot's first generated token (or
+    // null), the rows' slots and their positions and prompt lengths, and the
+    // choice as a greedy-choice key (0: none) for the step's last kernel
+    const unsigned* first;
+    const int* list;
+    const int* pos;
+    const int* n_prompt;
+    u64* keys;
 };
 
 namespace smp {
 constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048;
 constexpr double ONE = 8796093022208.0;  // 2^43, the weight of the largest logit
-typedef unsigned long long u64;
 
 // round(2^43 e^x) for x <= 0: e^x = 2^n e^r with |r| <= ln 2 / 2, e^r by its
 // Taylor series to r^11 (remainder below 1e-14), the integer from the low
@@ -74,12 +83,12 @@ __device__ inline u64 wave_sum64(u64 v) {
     return v;
 }
 
-// Calls f(id, logit) for the ids id0 .. id1 - 1 that the calling wave's lanes
-// take in turn; inadmissible ids come as -inf.
+// An id's logit; -inf for an inadmissible one.
 template <class T>
 __device__ inline float load_logit(const SampleArgs& a, const T* row, int id) {
     const float l = ldf(row + id);
     if (a.never && ((a.never[id >> 5] >> (id & 31)) & 1u)) return -INFINITY;
+    if (a.first && ((a.first[id >> 5] >> (id & 31)) & 1u)) return -INFINITY;
     return l == l ? l : -INFINITY;  // NaN is never chosen
 }
 }  // namespace smp
@@ -99,6 +108,10 @@ __global__ __launch_bounds__(smp::THREADS) void sample_kernel(SampleArgs a) {
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T* row = static_cast<const T*>(a.logits) + (long long)r * a.ld;
     const SampleRow o = a.rows[r];
+    if (a.first) {  // only for a row at its slot's first generated token
+        const int slot = a.list[r];
+        if (a.pos[slot] != a.n_prompt[slot] - 1) a.first = nullptr;
+    }
     const int V = a.V, C = ((V + WAVES - 1) / WAVES + 63) / 64 * 64;
     const int lo = min(V, wave * C), hi = min(V, lo + C);
 
@@ -122,7 +135,8 @@ __global__ __launch_bounds__(smp::THREADS) void sample_kernel(SampleArgs a) {
     __syncthreads();
     if (best == 0) {  // no admissible id
         if (tid == 0) {
-            a.tok[r] = -1;
+            if (a.tok) a.tok[r] = -1;
+            if (a.keys) a.keys[r] = 0;
             if (a.logp) a.logp[r] = -INFINITY;
         }
         return;
@@ -269,7 +283,8 @@ __global__ __launch_bounds__(smp::THREADS) void sample_kernel(SampleArgs a) {
     } else if (tid != 0) {
         return;
     }
-    a.tok[r] = token;
+    if (a.tok) a.tok[r] = token;
+    if (a.keys) a.keys[r] = amax_key(0.f, token);
     if (a.logp) {
         const float l = ldf(row + token);
         a.logp[r] = (float)((l == lmax ? 0.0 : (double)l - (double)lmax) - lse);
