@@ -802,9 +802,9 @@ class EngineT final : public Engine {
         int nk = head_argmax(tok_emb_, V_, b.dz, n, d, HeadArgs{want_logits ? logits : nullptr, keys, V_, tf}, s);
         if (draw_rows_) {  // the drawn tokens take the place of the largest keys
             const SampleRow* o = reinterpret_cast<const SampleRow*>(draw_);
-            hipLaunchKernelGGL(sample_kernel<float>, dim3(n), dim3(smp::THREADS), 0, s,
-                               SampleArgs{logits, V_, V_, o, tf.never, draw_ + 4 * (size_t)n, nullptr, draw_logp_, tf.first,
-                                          list, pos_, npr_, keys});
+            sample_rows<float>(SampleArgs{logits, V_, V_, o, tf.never, draw_ + 4 * (size_t)n, nullptr, draw_logp_, tf.first,
+                                          list, pos_, npr_, keys, draw_ws_, 0},
+                               n, s);
             nk = 1;
         }
         hipLaunchKernelGGL(argmax_step_kernel, dim3(n), dim3(64), 0, s, keys, nk, list, pos_, npr_, seq_, gen_,
@@ -1271,6 +1271,7 @@ class EngineT final : public Engine {
     int *table_ = nullptr, *plan_ = nullptr, *xlist_ = nullptr, *forked_ = nullptr, *region_of_ = nullptr;
     // options, uniform numbers and log-probabilities of a drawn step
     float *draw_ = nullptr, *draw_logp_ = nullptr;
+    unsigned char* draw_ws_ = nullptr;
     int draw_rows_ = 0;
     T *kts_ = nullptr, *vs_ = nullptr;
     T *ktc_, *vc_, *dz_, *dq_, *datt_, *dh_;
@@ -1763,10 +1764,11 @@ class EngineT final : public Engine {
         outtok_ = dalloc<int>(S);
         rowlen_ = dalloc<int>(S);
         stop_at_ = dalloc<int>(S);
-        never_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 1);
-        first_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 1);
+        never_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 2);  // a word to spare: 64 bits are read at once
+        first_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 2);
         draw_ = dalloc<float>(5 * S);
         draw_logp_ = dalloc<float>(S);
+        draw_ws_ = dalloc<unsigned char>(sample_ws_bytes(S_));
         xlist_ = list_;
         if (paged_) {
             pages_ = dalloc<T>((size_t)book_.free_pages() * 2 * Ld * H * (64 << PAGE_SHIFT));

@@ -17,14 +17,16 @@ class SamplerImpl final : public Sampler {
     SamplerImpl(int n_vocab, int max_rows, int device) : V_(n_vocab), R_(max_rows), dev_(device) {
         if (dev_ == WHISPER_NO_DEVICE) return;
         DeviceScope scope(dev_);
-        const size_t words = (size_t)V_ / 32 + 1;
+        const size_t words = (size_t)V_ / 32 + 2;
         void* q = nullptr;
-        if (hipMalloc(&q, R_ * sizeof(SampleRow) + words * sizeof(unsigned)) != hipSuccess) {
+        const size_t head = (R_ * sizeof(SampleRow) + words * sizeof(unsigned) + 255) / 256 * 256;
+        if (hipMalloc(&q, head + sample_ws_bytes(R_)) != hipSuccess) {
             (void)hipGetLastError();
             throw ArgError(WHISPER_E_NOMEM, "device allocation of the sampler's options failed");
         }
         rows_ = static_cast<SampleRow*>(q);
         never_ = reinterpret_cast<unsigned*>(rows_ + R_);
+        ws_ = static_cast<unsigned char*>(q) + head;
         const std::vector<SampleRow> d(R_, SampleRow{1.f, 0, 1.f, 0.f});
         WMI_HIP(hipMemcpy(rows_, d.data(), d.size() * sizeof(SampleRow), hipMemcpyHostToDevice));
     }
@@ -50,7 +52,7 @@ class SamplerImpl final : public Sampler {
         if (capturing(st_)) throw ArgError(WHISPER_E_STATE, "the stream is recording a graph: only run may be recorded");
         std::vector<SampleRow> h(n);
         for (int i = 0; i < n; ++i) h[i] = SampleRow{rows[i].temperature, rows[i].top_k, rows[i].top_p, rows[i].min_p};
-        std::vector<unsigned> m((size_t)V_ / 32 + 1, 0u);
+        std::vector<unsigned> m((size_t)V_ / 32 + 2, 0u);
         for (int i = 0; i < n_suppress; ++i) m[suppress[i] >> 5] |= 1u << (suppress[i] & 31);
         WMI_HIP(hipStreamSynchronize(st_));
         if (n) WMI_HIP(hipMemcpy(rows_, h.data(), h.size() * sizeof(SampleRow), hipMemcpyHostToDevice));
@@ -60,9 +62,9 @@ class SamplerImpl final : public Sampler {
     void run(const void* logits, int dtype, int n_rows, int64_t ld, const float* u, int32_t* tok, float* logp) override {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the sampler has no device");
         DeviceScope scope(dev_);
-        const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp, nullptr, nullptr, nullptr, nullptr, nullptr};
-        if (dtype == WHISPER_DTYPE_BF16) hipLaunchKernelGGL(sample_kernel<bf16>, dim3(n_rows), dim3(smp::THREADS), 0, st_, a);
-        else hipLaunchKernelGGL(sample_kernel<float>, dim3(n_rows), dim3(smp::THREADS), 0, st_, a);
+        const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp, nullptr, nullptr, nullptr, nullptr, nullptr, ws_, 0};
+        if (dtype == WHISPER_DTYPE_BF16) sample_rows<bf16>(a, n_rows, st_);
+        else sample_rows<float>(a, n_rows, st_);
         WMI_HIP(hipGetLastError());
     }
 
@@ -71,6 +73,7 @@ class SamplerImpl final : public Sampler {
     hipStream_t st_ = nullptr;
     SampleRow* rows_ = nullptr;
     unsigned* never_ = nullptr;
+    unsigned char* ws_ = nullptr;
     bool use_never_ = false;
 };
 

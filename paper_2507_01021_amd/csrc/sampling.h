@@ -4,14 +4,19 @@
 // With l_max the row's largest admissible logit, id i has the weight
 //   w_i = round(2^43 exp((l_i - l_max) / T)),
 // an integer, so that sums of weights are exact: they depend neither on the
-// order of the additions nor on how a row is cut over threads, and a row's
-// token is the same in every batch. (A weight is off by half a unit of
-// 2^-43 of the largest at most, less than the 2^-24 of fp32 sums by far; V is
-// at most 2^20, so a sum fits 64 bits.) Ids are ordered by (logit descending, id
-// ascending); each filter keeps a prefix of that order, so the filters
-// together keep the shortest: a cut, found by counting digits of the order's
-// 52-bit key (32 bits of the logit, 20 of the id), highest first, until one
-// digit decides.
+// order of the additions nor on how a row is cut over workgroups, and a row's
+// token is the same in every batch. (A weight is off by a unit or two of 2^-43
+// of the largest, far less than fp32 sums would be; V is at most 2^20, so a sum
+// fits 64 bits.) Ids are ordered by (logit descending, id ascending); each filter
+// keeps a prefix of that order, so the filters together keep the shortest.
+//
+// Three kernels. sample_max_kernel and sample_sum_kernel cut every row over
+// enough workgroups to fill the GPU: the largest logit; then the sum of the exponentials
+// and, over 2047 bins of distance from the largest logit, the ids (top-k) or
+// the weights (top-p) of every bin, or without both filters the weights' sums
+// by position. sample_pick_kernel, a workgroup per row, finds the bin of
+// the cut, lists the ids up to it (some dozens to thousands) and settles the rest
+// in that list, or if they are too many, by further passes over the row.
 #pragma once
 
 #include "common.h"
@@ -43,32 +48,38 @@ struct SampleArgs {
     const int* pos;
     const int* n_prompt;
     u64* keys;
+    // workspace of SAMPLE_ROWS rows at most, and the workgroups a row is cut over
+    unsigned char* ws;
+    int chunks;
 };
+constexpr int SAMPLE_ROWS = 1024;
 
 namespace smp {
 constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048;
+constexpr int CUT_WAVES = 4, MAX_CHUNKS = 64;  // waves of the first two kernels' workgroups, workgroups of a row
+// What the first two kernels leave of a row for the third.
+struct RowWork {
+    u64 bins[BINS];                       // by distance: ids, or weights
+    u64 sums[MAX_CHUNKS * CUT_WAVES];     // without top-k and top-p: a wave's kept weights
+    double exps[MAX_CHUNKS * CUT_WAVES];  // sums of exp(l - l_max)
+    float max[MAX_CHUNKS];
+    int id[MAX_CHUNKS];                   // lowest id with that maximum
+};
 constexpr double ONE = 8796093022208.0;  // 2^43, the weight of the largest logit
 
-// round(2^43 e^x) for x <= 0: e^x = 2^n e^r with |r| <= ln 2 / 2, e^r by its
-// Taylor series to r^11 (remainder below 1e-14), the integer from the low
-// bits of a sum with 2^52.
-__device__ inline u64 weight(double x) {
-    if (!(x > -32.0)) return 0;  // below half a unit (e^-32 2^43 < 0.12)
-    const double n = __builtin_rint(x * 1.4426950408889634074);
-    const double r = fma(n, -0.69314718055994530942, x);
-    double p = 1.0 / 39916800.0;
-    p = fma(p, r, 1.0 / 3628800.0);
-    p = fma(p, r, 1.0 / 362880.0);
-    p = fma(p, r, 1.0 / 40320.0);
-    p = fma(p, r, 1.0 / 5040.0);
-    p = fma(p, r, 1.0 / 720.0);
-    p = fma(p, r, 1.0 / 120.0);
-    p = fma(p, r, 1.0 / 24.0);
-    p = fma(p, r, 1.0 / 6.0);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    const double w = __builtin_amdgcn_ldexp(p, (int)n + 43) + 4503599627370496.0;
+// round(2^43 2^y) for y <= 0: y to the nearest 1/256 by the low bits of a
+// sum with 1.5 2^44, its power of two from a table, the rest (2^-9 at most) by
+// three terms of the exponential series (the fourth is below 2^-42), the
+// integer from the low bits of a sum with 2^52.
+__device__ __forceinline__ u64 weight(double y, const double* tab) {
+    if (!(y > -44.5)) return 0;  // below half a unit
+    const double t = y + 26388279066624.0;
+    const int k = (int)__builtin_bit_cast(u64, t);
+    const double f = y - (t - 26388279066624.0);
+    double p = fma(f, 0.055504108664821580, 0.24022650695910072);
+    p = fma(p, f, 0.69314718055994531);
+    p = fma(p, f, 1.0);
+    const double w = __builtin_amdgcn_ldexp(p * tab[k & 255], (k >> 8) + 43) + 4503599627370496.0;
     return __builtin_bit_cast(u64, w) & 0xfffffffffffffull;
 }
 
@@ -83,57 +94,277 @@ __device__ inline u64 wave_sum64(u64 v) {
     return v;
 }
 
-// An id's logit; -inf for an inadmissible one.
+// A row of logits in device memory as one workgroup reads it: 16-byte pieces
+// at 16-byte addresses, wave w taking the pieces of one contiguous range of
+// ids, so that sums in the order of ids are sums over waves first. The row
+// may begin at any element: `shift` elements of its first piece are not its own.
 template <class T>
-__device__ inline float load_logit(const SampleArgs& a, const T* row, int id) {
-    const float l = ldf(row + id);
-    if (a.never && ((a.never[id >> 5] >> (id & 31)) & 1u)) return -INFINITY;
-    if (a.first && ((a.first[id >> 5] >> (id & 31)) & 1u)) return -INFINITY;
-    return l == l ? l : -INFINITY;  // NaN is never chosen
+struct LogitRow {
+    static constexpr int EL = 16 / sizeof(T);
+    const T* row;
+    int V, shift, lo, hi;    // the wave's pieces lo .. hi - 1
+    int whole_lo, whole_hi;  // pieces all of whose ids are the row's
+    const unsigned *never, *first;
+
+    // The pieces of wave `wave` of `waves` that share row r.
+    __device__ __forceinline__ LogitRow(const SampleArgs& a, int r, int wave, int waves) {
+        row = static_cast<const T*>(a.logits) + (long long)r * a.ld;
+        V = a.V;
+        shift = (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(T);
+        whole_lo = shift ? 1 : 0;
+        whole_hi = (V + shift) / EL - 1;
+        take(wave, waves);
+        never = a.never;
+        first = a.first;
+        if (first) {  // only for a row at its slot's first generated token
+            const int slot = a.list[r];
+            if (a.pos[slot] != a.n_prompt[slot] - 1) first = nullptr;
+        }
+    }
+    __device__ __forceinline__ void take(int wave, int waves) {
+        const int n = (V + shift + EL - 1) / EL, per = ((n + waves - 1) / waves + 63) / 64 * 64;
+        lo = min(n, wave * per);
+        hi = min(n, lo + per);
+    }
+    // Piece v as loaded: its 16 bytes and the bits of ids that are left out.
+    // Loads of pieces that are not wholly the row's go to a whole one instead,
+    // so that a run of loads has no branches; unpack() then reads their ids one by one.
+    struct Raw {
+        u32x4 x;
+        unsigned m;
+    };
+    __device__ __forceinline__ Raw fetch(int v) const {
+        const int id0 = min(max(v, whole_lo), whole_hi) * EL - shift;
+        Raw r;
+        r.x = *reinterpret_cast<const u32x4*>(row + id0);
+        r.m = 0;
+        if (never) r.m |= bits(never, id0);
+        if (first) r.m |= bits(first, id0);
+        return r;
+    }
+    // Logits of piece v < end, inadmissible ids (filtered, NaN, outside the row) as -inf.
+    __device__ __forceinline__ void unpack(int v, int end, const Raw& r, float (&l)[EL]) const {
+#pragma unroll
+        for (int e = 0; e < EL; ++e) {
+            if constexpr (sizeof(T) == 4) l[e] = __uint_as_float(r.x[e]);
+            else l[e] = __uint_as_float(e & 1 ? r.x[e >> 1] & 0xffff0000u : r.x[e >> 1] << 16);
+            l[e] = ((r.m >> e) & 1u) || !(l[e] > -INFINITY) ? -INFINITY : l[e];
+        }
+        if (v < whole_lo || v > whole_hi || v >= end) {
+#pragma unroll
+            for (int e = 0; e < EL; ++e) {
+                const int i = v * EL - shift + e;
+                l[e] = -INFINITY;
+                if (v >= end || i < 0 || i >= V) continue;
+                const float y = ldf(row + i);
+                const bool out = (never && ((never[i >> 5] >> (i & 31)) & 1u)) || (first && ((first[i >> 5] >> (i & 31)) & 1u));
+                l[e] = out || !(y > -INFINITY) ? -INFINITY : y;
+            }
+        }
+    }
+    // The mask's bits from id0 on (masks have a word to spare behind the last).
+    __device__ __forceinline__ unsigned bits(const unsigned* m, int id0) const {
+        const u64 w = (u64)m[id0 >> 5] | (u64)m[(id0 >> 5) + 1] << 32;
+        return (unsigned)(w >> (id0 & 31));
+    }
+    // f(id of the first, logits) for every piece of the wave, lane by lane in
+    // turn. The next D pieces are on their way while one is worked on; the body
+    // is there once, so that it stays in the instruction cache.
+    template <int D, class F>
+    __device__ __forceinline__ void each(int lane, F&& f) const {
+        const bool any = whole_lo <= whole_hi;
+        Raw x[D];
+#pragma unroll
+        for (int u = 0; u < D; ++u) x[u] = any ? fetch(lo + lane + u * 64) : Raw{};
+#pragma unroll 1
+        for (int v0 = lo; v0 < hi; v0 += 64) {
+            const Raw now = x[0];
+#pragma unroll
+            for (int u = 0; u + 1 < D; ++u) x[u] = x[u + 1];
+            const int v = v0 + lane;
+            x[D - 1] = any ? fetch(v + D * 64) : Raw{};
+            float l[EL];
+            unpack(v, hi, now, l);
+            f(v * EL - shift, l);
+        }
+    }
+};
+
+// e^x for x <= 0 with an error of a few 2^-24: the rounding of x log2(e) is
+// made up for by a factor. 0 below e^-150, which no sum of 2^20 terms up to 1 feels.
+__device__ __forceinline__ float exp_neg(float x) {
+    x = fmaxf(x, -150.f);
+    const float t = x * 1.44269504f;
+    const float lo = fmaf(x, 1.44269504f, -t) + x * 1.925963e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, lo * 0.69314718f, e);
+}
+
+// What the options and the largest logit make of a logit.
+struct Scale {
+    float lmax, per_bin;
+    double per;  // log2 of a weight per logit
+    u64 least;   // min_p
+    const double* tab;
+    __device__ __forceinline__ Scale(const SampleRow& o, float m, const double* t) : lmax(m), tab(t) {
+        per = 1.4426950408889634074 / (double)o.temperature;
+        per_bin = 2047.f / 45.f * (float)per;
+        least = (u64)ceil((double)o.min_p * ONE);
+    }
+    // weight of an admissible logit; the largest (+inf too): 2^43
+    __device__ __forceinline__ u64 weigh(float l) const {
+        return l == lmax ? (u64)ONE : weight(((double)l - (double)lmax) * per, tab);
+    }
+    // bin by distance, as wide as 45 T ln 2 / 2047; 2047: weight 0
+    __device__ __forceinline__ int bin(float l) const { return l == lmax ? 0 : (int)fminf((lmax - l) * per_bin, 2047.f); }
+};
+__device__ __forceinline__ void fill_table(double* tab) {
+    if (threadIdx.x < 256) tab[threadIdx.x] = exp2((double)threadIdx.x / 256.0);
+}
+// The row's largest logit from its chunks (MAX_CHUNKS lanes).
+__device__ __forceinline__ float row_max(const RowWork& w, int chunks, int lane) {
+    return wave_max(lane < chunks ? w.max[lane] : -INFINITY);
+}
+// Inclusive sums over the lanes, and over all lanes.
+__device__ __forceinline__ u64 wave_scan64(u64 v, int lane) {
+#pragma unroll
+    for (int st = 1; st < 64; st <<= 1) {
+        const u64 x = __shfl_up(v, st, 64);
+        if (lane >= st) v += x;
+    }
+    return v;
 }
 }  // namespace smp
 
-// One workgroup per row. Every pass goes over the row again (it stays in the
-// L2 cache). Wave w owns the ids [w C, w C + C), so that sums in the order of
-// ids are sums over waves first.
 template <class T>
-__global__ __launch_bounds__(smp::THREADS) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_max_kernel(SampleArgs a) {
+    using namespace smp;
+    __shared__ float redf[CUT_WAVES];
+    __shared__ int redi[CUT_WAVES];
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const LogitRow<T> row(a, r, blockIdx.x * CUT_WAVES + wave, a.chunks * CUT_WAVES);
+    RowWork& ws = reinterpret_cast<RowWork*>(a.ws)[r];
+    constexpr int EL = LogitRow<T>::EL;
+    for (int i = blockIdx.x * 64 * CUT_WAVES + tid; i < BINS; i += a.chunks * 64 * CUT_WAVES) ws.bins[i] = 0;
+    float m = -INFINITY;
+    int id = 0x7fffffff;
+    row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
+        float mx = l[0];
+#pragma unroll
+        for (int e = 1; e < EL; ++e) mx = fmaxf(mx, l[e]);
+        if (mx > m) {
+            m = mx;
+#pragma unroll
+            for (int e = EL - 1; e >= 0; --e)
+                if (l[e] == mx) id = i0 + e;
+        }
+    });
+    const float wm = wave_max(m);
+    if (m != wm) id = 0x7fffffff;
+#pragma unroll
+    for (int st = 32; st > 0; st >>= 1) id = min(id, __shfl_xor(id, st, 64));
+    if (lane == 0) {
+        redf[wave] = wm;
+        redi[wave] = id;
+    }
+    __syncthreads();
+    if (tid != 0) return;
+    for (int w = 1; w < CUT_WAVES; ++w)
+        if (redf[w] > redf[0]) {  // ids rise from wave to wave: the first one's is the lowest
+            redf[0] = redf[w];
+            redi[0] = redi[w];
+        }
+    ws.max[blockIdx.x] = redf[0];
+    ws.id[blockIdx.x] = redi[0];
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_sum_kernel(SampleArgs a) {
     using namespace smp;
     __shared__ u64 hw[BINS];
-    __shared__ unsigned hc[BINS];
-    __shared__ u64 red[WAVES];
-    __shared__ double redd[WAVES];
-    __shared__ u64 sh_prefix, sh_need;
-    __shared__ int sh_done;
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const T* row = static_cast<const T*>(a.logits) + (long long)r * a.ld;
+    __shared__ double tab[256];
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int gw = blockIdx.x * CUT_WAVES + wave;
+    const LogitRow<T> row(a, r, gw, a.chunks * CUT_WAVES);
+    RowWork& ws = reinterpret_cast<RowWork*>(a.ws)[r];
+    constexpr int EL = LogitRow<T>::EL;
     const SampleRow o = a.rows[r];
-    if (a.first) {  // only for a row at its slot's first generated token
-        const int slot = a.list[r];
-        if (a.pos[slot] != a.n_prompt[slot] - 1) a.first = nullptr;
-    }
-    const int V = a.V, C = ((V + WAVES - 1) / WAVES + 63) / 64 * 64;
-    const int lo = min(V, wave * C), hi = min(V, lo + C);
-
-    // the largest key: its logit is l_max, its id the greedy choice
-    u64 best = 0;
-    for (int i = lo + lane; i < hi; i += 64) {
-        const float l = load_logit(a, row, i);
-        if (l > -INFINITY) {
-            const u64 k = order_key(l, i);
-            best = k > best ? k : best;
-        }
-    }
+    const float lmax = row_max(ws, a.chunks, lane);
+    const bool draws = o.temperature > 0.f && lmax > -INFINITY;
+    const bool log_sum = a.logp && lmax > -INFINITY;
+    if (!draws && !log_sum) return;
+    // top-k counts ids (1), top-p adds weights (2), neither: sums in the order of ids (0)
+    const int mode = !draws ? -1 : o.top_k > 0 ? 1 : o.top_p < 1.f ? 2 : 0;
+    fill_table(tab);
+    for (int i = tid; i < BINS; i += 64 * CUT_WAVES) hw[i] = 0;
+    __syncthreads();
+    const Scale sc(o, lmax, tab);
+    double se = 0.0;
+    u64 sum = 0;
+    row.template each<4>(lane, [&](int, const float (&l)[EL]) __attribute__((always_inline)) {
+        if (log_sum) {
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) {
-        const u64 c = __shfl_xor(best, s, 64);
-        best = c > best ? c : best;
+            for (int e = 0; e < EL; e += 4) {
+                float x = 0.f;
+#pragma unroll
+                for (int k = e; k < e + 4; ++k) x += l[k] == lmax ? 1.f : exp_neg(l[k] - lmax);
+                se += x;
+            }
+        }
+        if (mode == 0) {
+#pragma unroll
+            for (int e = 0; e < EL; ++e) {
+                const u64 w = sc.weigh(l[e]);
+                sum += w >= sc.least ? w : 0;
+            }
+        } else if (mode > 0) {
+#pragma unroll
+            for (int e = 0; e < EL; ++e) {
+                const int b = sc.bin(l[e]);
+                if (b < 2047) atomicAdd(&hw[b], mode == 1 ? 1ull : sc.weigh(l[e]));
+            }
+        }
+    });
+    if (log_sum) {
+#pragma unroll
+        for (int st = 32; st > 0; st >>= 1) se += __shfl_xor(se, st, 64);
+        if (lane == 0) ws.exps[gw] = se;
     }
-    if (lane == 0) red[wave] = best;
-    __syncthreads();
-    for (int w = 0; w < WAVES; ++w) best = red[w] > best ? red[w] : best;
-    __syncthreads();
-    if (best == 0) {  // no admissible id
+    if (mode == 0) {
+        sum = wave_sum64(sum);
+        if (lane == 0) ws.sums[gw] = sum;
+    } else if (mode > 0) {
+        __syncthreads();
+        // sums of integers: the order of the additions does not matter
+        for (int i = tid; i < BINS; i += 64 * CUT_WAVES)
+            if (hw[i]) atomicAdd(&ws.bins[i], hw[i]);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a) {
+    using namespace smp;
+    constexpr int BIN_IDS = THREADS;         // ids of a cut's bin that are ranked at once
+    constexpr int BLOCKS = 176, BLOCK = 64;  // the short list: blocks of ids of one wave each
+    __shared__ u64 hw[BINS];
+    __shared__ u64 lk[BIN_IDS], lw[BIN_IDS];
+    __shared__ u32x2 list[BLOCKS * BLOCK];   // id, logit
+    __shared__ unsigned char block_of[WAVES][BLOCKS];
+    __shared__ u64 red[WAVES];
+    __shared__ double tab[256];
+    __shared__ u64 sh_cut, sh_need;
+    __shared__ int sh_bin, n_ids, n_blocks;
+    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    LogitRow<T> row(a, r, wave, WAVES);
+    const RowWork& ws = reinterpret_cast<const RowWork*>(a.ws)[r];
+    const SampleRow o = a.rows[r];
+    const float u = a.u[r];
+    constexpr int EL = LogitRow<T>::EL;
+    constexpr int PER = MAX_CHUNKS * CUT_WAVES / 64;  // sums of the second kernel's waves per lane
+    const int cut_waves = a.chunks * CUT_WAVES;
+
+    const float lmax = row_max(ws, a.chunks, lane);
+    if (lmax == -INFINITY) {  // no admissible id
         if (tid == 0) {
             if (a.tok) a.tok[r] = -1;
             if (a.keys) a.keys[r] = 0;
@@ -141,153 +372,314 @@ __global__ __launch_bounds__(smp::THREADS) void sample_kernel(SampleArgs a) {
         }
         return;
     }
-    const float lmax = ord2f((uint32_t)(best >> 20));
-    // log of the sum of exp(l - l_max) over the admissible ids
-    double lse = 0.0;
+    double se = 0.0;
     if (a.logp) {
-        double s = 0.0;
-        for (int i = lo + lane; i < hi; i += 64) {
-            const float l = load_logit(a, row, i);
-            s += l == lmax ? 1.f : expf(l - lmax);
-        }
 #pragma unroll
-        for (int o2 = 32; o2 > 0; o2 >>= 1) s += __shfl_xor(s, o2, 64);
-        if (lane == 0) redd[wave] = s;
-        __syncthreads();
-        s = 0.0;
-        for (int w = 0; w < WAVES; ++w) s += redd[w];
-        __syncthreads();
-        lse = log(s);
+        for (int k = 0; k < PER; ++k) se += PER * lane + k < cut_waves ? ws.exps[PER * lane + k] : 0.0;
+#pragma unroll
+        for (int st = 32; st > 0; st >>= 1) se += __shfl_xor(se, st, 64);
     }
-    int token = 0xfffff - (int)(best & 0xfffff);
-    if (o.temperature > 0.f) {
-        const double invT = 1.0 / (double)o.temperature;
-        // weight of an admissible logit; +inf and ids equal to the largest: 2^43
-        auto weigh = [&](float l) { return l == lmax ? (u64)ONE : weight(((double)l - (double)lmax) * invT); };
-        // Kept so far: key >> shift >= prefix, for each filter (a later one's
-        // digits may stop short of telling what an earlier one left out).
-        struct Cut { u64 prefix; int shift; } cut[2] = {{0, 0}, {0, 0}};
-        // Finds the shortest prefix of the ids kept by cut[0] with `need` ids
-        // (by count), or with `share` of their weight, and puts it into `to`.
-        auto find = [&](bool by_count, double share, u64 need, Cut& to) {
-            int shift = 52, bits = 0;
-            u64 prefix = 0;
-            for (int pass = 0; pass < 5; ++pass) {
-                bits = pass < 2 ? 11 : 10;
-                shift -= bits;
-                for (int i = tid; i < BINS; i += THREADS) {
-                    hw[i] = 0;
-                    hc[i] = 0;
-                }
-                __syncthreads();
-                for (int i = lo + lane; i < hi; i += 64) {
-                    const float l = load_logit(a, row, i);
-                    if (!(l > -INFINITY)) continue;
-                    const u64 k = order_key(l, i);
-                    if ((k >> cut[0].shift) < cut[0].prefix || (k >> shift >> bits) != prefix) continue;
-                    const int d = (int)(k >> shift) & ((1 << bits) - 1);
-                    atomicAdd(&hc[d], 1u);
-                    if (!by_count) atomicAdd(&hw[d], weigh(l));
-                }
-                __syncthreads();
-                // thread t: digits BINS - 1 - 2 t and the next lower one
-                const int d1 = BINS - 1 - 2 * tid, d0 = d1 - 1;
-                const u64 m1 = by_count ? hc[d1] : hw[d1], m0 = by_count ? hc[d0] : hw[d0];
-                u64 s = m1 + m0;
+    // writes the row's results (one thread)
+    auto finish = [&](int token, float l) __attribute__((always_inline)) {
+        if (a.tok) a.tok[r] = token;
+        if (a.keys) a.keys[r] = amax_key(0.f, token);
+        if (a.logp) a.logp[r] = (float)((l == lmax ? 0.0 : (double)l - (double)lmax) - log(se));
+    };
+    if (!(o.temperature > 0.f)) {
+        // ids rise from chunk to chunk: the first that has the maximum
+        const unsigned long long has = __ballot(lane < a.chunks && ws.max[min(lane, a.chunks - 1)] == lmax);
+        if (tid == 0) finish(ws.id[__builtin_ctzll(has)], lmax);
+        return;
+    }
+    fill_table(tab);
+    if (tid == 0) n_blocks = 0;
+    const Scale sc(o, lmax, tab);
+    // where u falls: the first id whose running sum passes u * total, the last kept one at most
+    auto target_of = [&](u64 total) __attribute__((always_inline)) {
+        const double t = (double)u * (double)total;
+        const u64 x = t > 0.0 ? (u64)t : 0;  // an integer passes t if it passes t's integer part
+        return x < total ? x : total - 1;
+    };
+    float cut_l = -INFINITY;  // kept: larger logits, and equal ones up to id cut_id
+    int cut_id = -1;
+    auto kept = [&](int i, float l) __attribute__((always_inline)) { return l > cut_l || (l == cut_l && i <= cut_id); };
+
+    // All ids of the row, or once SHORT has listed those up to the first cut's
+    // bin, all of the list, are gone through once per stage: BIN adds up the
+    // bins (the first time they are there already), RANK lists the ids of the
+    // cut's bin, DIGIT adds up digits of their keys if they are too many, SUM
+    // adds the kept weights. Cut 0 is top-k's (every id measures 1), cut 1
+    // top-p's (an id measures its weight).
+    enum { BIN, SHORT, RANK, DIGIT, SUM };
+    int stage = BIN, cut = 0, digit = 0, shift = 52, nb = 0, bin = -1;
+    u64 prefix = 0, sum = 0;
+    bool fresh = true, listed = false;  // the bins are the second kernel's; the ids are in the list
+    int own = 0;                        // this wave's ids in the list
+    auto visit = [&](int i, float l) __attribute__((always_inline)) {
+        const int b = sc.bin(l);
+        if (!kept(i, l) || b == 2047 || ((stage == RANK || stage == DIGIT) && b != bin)) return;
+        if (stage == RANK) {
+            const int at = atomicAdd(&n_ids, 1);
+            if (at < BIN_IDS) lk[at] = order_key(l, i);
+            return;
+        }
+        const u64 w = cut == 0 ? 1 : sc.weigh(l);
+        if (stage == SUM) {
+            sum += w >= sc.least ? w : 0;
+        } else if (stage == BIN) {
+            atomicAdd(&hw[b], w);
+        } else {
+            const u64 k = order_key(l, i);
+            if ((k >> shift >> nb) == prefix) atomicAdd(&hw[(k >> shift) & ((1 << nb) - 1)], w);
+        }
+    };
+    for (;;) {
+        if (stage == BIN && cut == 0 && o.top_k <= 0) cut = 1;
+        if (stage == BIN && cut == 1 && !(o.top_p < 1.f)) cut = 2;
+        if (cut == 2) stage = SUM;
+        if (stage == SUM && fresh) break;  // the sums are there
+        nb = digit < 2 ? 11 : 10;
+        if (stage == DIGIT) shift -= nb;
+        if (stage == BIN || stage == DIGIT)
+            for (int i = tid; i < BINS; i += THREADS) hw[i] = stage == BIN && fresh ? ws.bins[i] : 0;
+        if (tid == 0) n_ids = 0;
+        bin = sh_bin;
+        __syncthreads();
+        if (stage == SHORT) {
+            // every wave lists its ids up to the bin in their order, in blocks of the workgroup's pool
+            int last = 0;  // the block that the wave is filling
+            row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
+                unsigned in = 0;
+#pragma unroll
+                for (int e = 0; e < EL; ++e)
+                    if (l[e] > -INFINITY && sc.bin(l[e]) <= bin) in |= 1u << e;
+                if (!__any(in)) return;
+                int c = __popc(in), before = c;
 #pragma unroll
                 for (int st = 1; st < 64; st <<= 1) {
-                    const u64 c = __shfl_up(s, st, 64);
-                    if (lane >= st) s += c;
+                    const int x = __shfl_up(before, st, 64);
+                    if (lane >= st) before += x;
                 }
-                if (lane == 63) red[wave] = s;
-                if (tid == 0) sh_done = -1;
-                __syncthreads();
-                u64 before = 0, total = 0;
-                for (int w = 0; w < WAVES; ++w) {
-                    if (w < wave) before += red[w];
-                    total += red[w];
+                const int n = __shfl(before, 63, 64);
+                before -= c;
+                // blocks first .. first + more - 1 of the wave are new: numbers base on
+                const int first = (own + BLOCK - 1) / BLOCK, more = (own + n + BLOCK - 1) / BLOCK - first;
+                int base = 0;
+                if (more) {
+                    if (lane == 0) base = atomicAdd(&n_blocks, more);
+                    base = __shfl(base, 0, 64);
+                    if (lane < more && base + lane < BLOCKS) block_of[wave][first + lane] = (unsigned char)(base + lane);
                 }
-                if (pass == 0) {
-                    if (by_count) {
-                        if (total <= need) {  // all of them are kept
-                            __syncthreads();
-                            return;
-                        }
-                    } else {
-                        need = (u64)ceil(share * (double)total);
-                        need = need < 1 ? 1 : need > total ? total : need;
-                    }
-                }
-                const u64 e1 = before + s - m0 - m1;  // measure of the digits above d1
-                if (e1 < need && e1 + m1 >= need) {
-                    sh_prefix = (prefix << bits) | d1;
-                    sh_need = need - e1;
-                    sh_done = hc[d1] == 1 || e1 + m1 == need ? 1 : 0;
-                } else if (e1 + m1 < need && e1 + m1 + m0 >= need) {
-                    sh_prefix = (prefix << bits) | d0;
-                    sh_need = need - e1 - m1;
-                    sh_done = hc[d0] == 1 || e1 + m1 + m0 == need ? 1 : 0;
-                }
-                __syncthreads();
-                prefix = sh_prefix;
-                need = sh_need;
-                const int done = sh_done;
-                __syncthreads();
-                if (done != 0) break;
-            }
-            to = Cut{prefix, shift};
-        };
-        if (o.top_k > 0) find(true, 0.0, (u64)o.top_k, cut[0]);
-        if (o.top_p < 1.f) find(false, (double)o.top_p, 0, cut[1]);
-        const double minw = (double)o.min_p * ONE;
-        // the kept weights, and the place of u times their sum among them
-        auto kept = [&](int i) -> u64 {
-            const float l = load_logit(a, row, i);
-            const u64 k = order_key(l, i);
-            if (!(l > -INFINITY) || (k >> cut[0].shift) < cut[0].prefix || (k >> cut[1].shift) < cut[1].prefix) return 0;
-            const u64 w = weigh(l);
-            return (double)w >= minw ? w : 0;
-        };
-        u64 s = 0;
-        for (int i = lo + lane; i < hi; i += 64) s += kept(i);
-        s = wave_sum64(s);
-        if (lane == 0) red[wave] = s;
-        __syncthreads();
-        u64 total = 0;
-        for (int w = 0; w < WAVES; ++w) total += red[w];
-        // the first id whose running sum passes u * total, the last kept one at most
-        const double u = a.u[r];
-        double t = u * (double)total;
-        u64 target = t > 0.0 ? (u64)t : 0;  // running sum > target  <=>  running sum > u * total
-        if (target >= total) target = total - 1;
-        u64 before = 0;
-        for (int w = 0; w < wave; ++w) before += red[w];
-        if (before > target || before + s <= target) return;  // another wave has it
-        for (int i0 = lo; i0 < hi; i0 += 64) {
-            const int i = i0 + lane;
-            const u64 w = i < hi ? kept(i) : 0;
-            u64 c = w;
 #pragma unroll
-            for (int st = 1; st < 64; st <<= 1) {
-                const u64 x = __shfl_up(c, st, 64);
-                if (lane >= st) c += x;
+                for (int e = 0; e < EL; ++e) {
+                    if (!((in >> e) & 1u)) continue;
+                    const int p = own + before++, q = p / BLOCK, at = q < first ? last : base + q - first;
+                    if (at < BLOCKS) list[at * BLOCK + p % BLOCK] = u32x2{(unsigned)(i0 + e), __float_as_uint(l[e])};
+                }
+                own += n;
+                if (more) last = base + more - 1;
+            });
+            __syncthreads();
+            listed = n_blocks <= BLOCKS;
+            stage = RANK;
+            continue;
+        }
+        if (!(stage == BIN && fresh)) {
+            if (listed) {
+                for (int p = lane; p - lane < own; p += BLOCK) {
+                    const u32x2 x = list[block_of[wave][p / BLOCK] * BLOCK + lane];
+                    if (p < own) visit((int)x.x, __uint_as_float(x.y));
+                }
+            } else {
+                row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int e = 0; e < EL; ++e) visit(i0 + e, l[e]);
+                });
             }
+            if (stage == SUM) break;
+            __syncthreads();
+        }
+        if (stage == RANK) {
+            const int n = n_ids;
+            __syncthreads();
+            if (n > BIN_IDS) {  // 11 11 10 bits of the logit, 10 10 of the id
+                stage = DIGIT;
+                digit = 0;
+                shift = 52;
+                prefix = 0;
+                continue;
+            }
+            // thread t has the bin's id t, and adds up what comes before it
+            const u64 k = tid < n ? lk[tid] : 0;
+            const u64 w = cut == 0 ? 1 : sc.weigh(ord2f((uint32_t)(k >> 20)));
+            lw[tid] = w;
+            __syncthreads();
+            if (tid < n) {
+                u64 before = 0;
+#pragma unroll 4
+                for (int j = 0; j < n; ++j) before += lk[j] > k ? lw[j] : 0;
+                if (before < sh_need && before + w >= sh_need) sh_cut = k;
+            }
+            __syncthreads();
+            prefix = sh_cut;
+        } else {
+            // bins by distance, digits highest first: thread t takes the places 2 t and 2 t + 1
+            const int p0 = stage == BIN ? 2 * tid : BINS - 1 - 2 * tid, p1 = stage == BIN ? p0 + 1 : p0 - 1;
+            const u64 m0 = hw[p0], m1 = hw[p1];
+            const u64 run = wave_scan64(m0 + m1, lane);
+            if (lane == 63) red[wave] = run;
+            if (tid == 0 && stage == BIN) sh_bin = -1;
+            __syncthreads();
+            u64 e = run - m0 - m1, total = 0;  // measure before place 2 t
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) e += red[w];
+                total += red[w];
+            }
+            u64 need = sh_need;
+            if (stage == BIN) need = cut == 0 ? (u64)o.top_k : max((u64)1, (u64)ceil((double)o.top_p * (double)total));
+            __syncthreads();
+            if (total > need || stage == DIGIT) {
+                const bool first = e < need && e + m0 >= need;
+                if (first || (e + m0 < need && e + m0 + m1 >= need)) {
+                    sh_need = first ? need - e : need - e - m0;  // still wanted from this place
+                    if (stage == BIN) sh_bin = first ? p0 : p1;
+                    else sh_cut = prefix << nb | (u64)(first ? p0 : p1);
+                }
+            }
+            __syncthreads();
+            if (stage == BIN) {
+                const bool was_fresh = fresh;
+                fresh = false;
+                if (sh_bin < 0) ++cut;  // nothing is cut off
+                else stage = was_fresh ? SHORT : RANK;
+                continue;
+            }
+            prefix = sh_cut;
+            if (++digit < 5) continue;
+        }
+        cut_l = ord2f((uint32_t)(prefix >> 20));
+        cut_id = 0xfffff - (int)(prefix & 0xfffff);
+        ++cut;
+        stage = BIN;
+        __syncthreads();
+    }
+
+    // The place of u times the sum of the kept weights. The waves' sums, in the
+    // order of their ids, say which wave's ids it is among.
+    const int waves = fresh ? cut_waves : WAVES;
+    if (!fresh) {
+        sum = wave_sum64(sum);
+        if (lane == 0) red[wave] = sum;
+    }
+    __syncthreads();
+    u64 part[PER], mine = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int w = PER * lane + k;
+        part[k] = w < waves ? fresh ? ws.sums[w] : red[w] : 0;
+        mine += part[k];
+    }
+    u64 run = wave_scan64(mine, lane);
+    const u64 target = target_of(__shfl(run, 63, 64));
+    const int at_lane = __builtin_ctzll(__ballot(run > target));
+    run -= mine;
+    int owner = PER * lane;
+#pragma unroll
+    for (int k = 0; k < PER - 1; ++k)
+        if (owner == PER * lane + k && run + part[k] <= target) {
+            run += part[k];
+            ++owner;
+        }
+    owner = __shfl(owner, at_lane, 64);
+    u64 before = __shfl(run, at_lane, 64);
+    if (listed) {
+        if (wave != owner) return;
+        for (int p = lane; p - lane < own; p += BLOCK) {
+            const u32x2 x = list[block_of[wave][p / BLOCK] * BLOCK + lane];
+            const float l = __uint_as_float(x.y);
+            u64 w = p < own && kept((int)x.x, l) ? sc.weigh(l) : 0;
+            if (w < sc.least) w = 0;
+            const u64 c = wave_scan64(w, lane);
             const unsigned long long hit = __ballot(before + c > target);
             if (hit) {
-                token = i0 + __builtin_ctzll(hit);
-                break;
+                if (lane == __builtin_ctzll(hit)) finish((int)x.x, l);
+                return;
             }
             before += __shfl(c, 63, 64);
         }
-        if (lane != 0) return;
-    } else if (tid != 0) {
         return;
     }
-    if (a.tok) a.tok[r] = token;
-    if (a.keys) a.keys[r] = amax_key(0.f, token);
-    if (a.logp) {
-        const float l = ldf(row + token);
-        a.logp[r] = (float)((l == lmax ? 0.0 : (double)l - (double)lmax) - lse);
+    // the owner's pieces, 64 at a time, are added up by all of this workgroup's waves
+    row.take(owner, waves);
+    const int lo = row.lo, hi = row.hi;
+    auto piece = [&](int v, float (&l)[EL], u64 (&w)[EL]) __attribute__((always_inline)) {
+        typename LogitRow<T>::Raw x{};
+        if (row.whole_lo <= row.whole_hi) x = row.fetch(v);
+        row.unpack(v, hi, x, l);
+        u64 c = 0;
+#pragma unroll
+        for (int e = 0; e < EL; ++e) {
+            w[e] = kept(v * EL + e - row.shift, l[e]) ? sc.weigh(l[e]) : 0;
+            if (w[e] < sc.least) w[e] = 0;
+            c += w[e];
+        }
+        return c;
+    };
+    float l[EL];
+    u64 w[EL];
+    for (int g = wave; lo + g * 64 < hi; g += WAVES) {
+        const u64 c = wave_sum64(piece(lo + g * 64 + lane, l, w));
+        if (lane == 0) hw[g] = c;
+    }
+    __syncthreads();
+    int g = 0;
+    for (; lo + (g + 1) * 64 < hi && before + hw[g] <= target; ++g) before += hw[g];
+    if (wave != g % WAVES) return;
+    const int v = lo + g * 64 + lane;
+    const u64 all = piece(v, l, w), c = wave_scan64(all, lane);
+    if (lane != __builtin_ctzll(__ballot(before + c > target))) return;
+    u64 at = before + c - all;
+    int e = 0;
+    float lt = l[0];
+#pragma unroll
+    for (int x = 0; x < EL; ++x) {
+        if (at <= target) {
+            e = x;
+            lt = l[x];
+        }
+        at += w[x];
+    }
+    finish(v * EL + e - row.shift, lt);
+}
+
+// Workgroups that a row of V logits is cut over when n rows are drawn at a
+// time: as many as fill 256 CUs four times, if every wave has 128 pieces of 16 bytes.
+template <class T>
+inline int sample_chunks(int n, int V) {
+    const int pieces = V / (16 / (int)sizeof(T)) + 1;
+    const int most = (pieces + 128 * smp::CUT_WAVES - 1) / (128 * smp::CUT_WAVES), want = (1024 + n - 1) / n;
+    const int c = want < most ? want : most;
+    return c < 1 ? 1 : c > smp::MAX_CHUNKS ? smp::MAX_CHUNKS : c;
+}
+inline size_t sample_ws_bytes(int rows) {
+    return sizeof(smp::RowWork) * (size_t)(rows < SAMPLE_ROWS ? rows : SAMPLE_ROWS);
+}
+// The choice for n rows; a.ws has sample_ws_bytes(n).
+template <class T>
+inline void sample_rows(SampleArgs a, int n, hipStream_t st) {
+    for (int r = 0; r < n; r += SAMPLE_ROWS) {
+        const int m = n - r < SAMPLE_ROWS ? n - r : SAMPLE_ROWS;
+        SampleArgs b = a;
+        b.logits = static_cast<const T*>(a.logits) + (long long)r * a.ld;
+        b.rows += r;
+        b.u += r;
+        if (b.tok) b.tok += r;
+        if (b.logp) b.logp += r;
+        b.chunks = sample_chunks<T>(m, a.V);
+        hipLaunchKernelGGL(sample_max_kernel<T>, dim3(b.chunks, m), dim3(64 * smp::CUT_WAVES), 0, st, b);
+        hipLaunchKernelGGL(sample_sum_kernel<T>, dim3(b.chunks, m), dim3(64 * smp::CUT_WAVES), 0, st, b);
+        hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(m), dim3(smp::THREADS), 0, st, b);
     }
 }
 
