@@ -804,7 +804,7 @@ class EngineT final : public Engine {
             const SampleRow* o = reinterpret_cast<const SampleRow*>(draw_);
             sample_rows<float>(SampleArgs{logits, V_, V_, o, tf.never, draw_ + 4 * (size_t)n, nullptr, draw_logp_, tf.first,
                                           list, pos_, npr_, keys, draw_ws_, 0},
-                               n, s);
+                               n, true, s);
             nk = 1;
         }
         hipLaunchKernelGGL(argmax_step_kernel, dim3(n), dim3(64), 0, s, keys, nk, list, pos_, npr_, seq_, gen_,

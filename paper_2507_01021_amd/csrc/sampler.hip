@@ -27,8 +27,8 @@ class SamplerImpl final : public Sampler {
         rows_ = static_cast<SampleRow*>(q);
         never_ = reinterpret_cast<unsigned*>(rows_ + R_);
         ws_ = static_cast<unsigned char*>(q) + head;
-        const std::vector<SampleRow> d(R_, SampleRow{1.f, 0, 1.f, 0.f});
-        WMI_HIP(hipMemcpy(rows_, d.data(), d.size() * sizeof(SampleRow), hipMemcpyHostToDevice));
+        host_.assign(R_, SampleRow{1.f, 0, 1.f, 0.f});
+        WMI_HIP(hipMemcpy(rows_, host_.data(), R_ * sizeof(SampleRow), hipMemcpyHostToDevice));
     }
     ~SamplerImpl() override {
         if (dev_ == WHISPER_NO_DEVICE) return;
@@ -58,13 +58,18 @@ class SamplerImpl final : public Sampler {
         if (n) WMI_HIP(hipMemcpy(rows_, h.data(), h.size() * sizeof(SampleRow), hipMemcpyHostToDevice));
         WMI_HIP(hipMemcpy(never_, m.data(), m.size() * sizeof(unsigned), hipMemcpyHostToDevice));
         use_never_ = n_suppress > 0;
+        std::copy(h.begin(), h.end(), host_.begin());
+        filters_ = false;
+        for (const SampleRow& x : host_) filters_ = filters_ || (x.temperature > 0.f && (x.top_k > 0 || x.top_p < 1.f));
     }
     void run(const void* logits, int dtype, int n_rows, int64_t ld, const float* u, int32_t* tok, float* logp) override {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the sampler has no device");
         DeviceScope scope(dev_);
         const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp, nullptr, nullptr, nullptr, nullptr, nullptr, ws_, 0};
-        if (dtype == WHISPER_DTYPE_BF16) sample_rows<bf16>(a, n_rows, st_);
-        else sample_rows<float>(a, n_rows, st_);
+        // a recorded run may meet other options at its replay
+        const bool filters = filters_ || capturing(st_);
+        if (dtype == WHISPER_DTYPE_BF16) sample_rows<bf16>(a, n_rows, filters, st_);
+        else sample_rows<float>(a, n_rows, filters, st_);
         WMI_HIP(hipGetLastError());
     }
 
@@ -74,7 +79,8 @@ class SamplerImpl final : public Sampler {
     SampleRow* rows_ = nullptr;
     unsigned* never_ = nullptr;
     unsigned char* ws_ = nullptr;
-    bool use_never_ = false;
+    bool use_never_ = false, filters_ = false;
+    std::vector<SampleRow> host_;  // the rows' options
 };
 
 }  // namespace

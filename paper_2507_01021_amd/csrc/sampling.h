@@ -10,13 +10,14 @@
 // fits 64 bits.) Ids are ordered by (logit descending, id ascending); each filter
 // keeps a prefix of that order, so the filters together keep the shortest.
 //
-// Three kernels. sample_max_kernel and sample_sum_kernel cut every row over
-// enough workgroups to fill the GPU: the largest logit; then the sum of the exponentials
-// and, over 2047 bins of distance from the largest logit, the ids (top-k) or
-// the weights (top-p) of every bin, or without both filters the weights' sums
-// by position. sample_pick_kernel, a workgroup per row, finds the bin of
-// the cut, lists the ids up to it (some dozens to thousands) and settles the rest
-// in that list, or if they are too many, by further passes over the row.
+// Four kernels. Three of them cut every row over enough workgroups to fill the
+// GPU: sample_max_kernel finds the largest logit; sample_sum_kernel the sum of
+// the exponentials and, over 2047 bins of distance from the largest logit, the
+// ids (top-k) or the weights (top-p) of every bin, or without both filters the
+// weights' sums by position; sample_list_kernel the bin in which the first
+// filter cuts, and lists the ids up to it (some dozens to thousands).
+// sample_pick_kernel, a workgroup per row, settles the rest in that list, or if
+// they were too many, by further passes over the row.
 #pragma once
 
 #include "common.h"
@@ -52,18 +53,24 @@ struct SampleArgs {
     unsigned char* ws;
     int chunks;
 };
-constexpr int SAMPLE_ROWS = 1024;
+constexpr int SAMPLE_ROWS = 512;
 
 namespace smp {
 constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048;
 constexpr int CUT_WAVES = 4, MAX_CHUNKS = 64;  // waves of the first two kernels' workgroups, workgroups of a row
-// What the first two kernels leave of a row for the third.
+constexpr int BLOCKS = 512, BLOCK = 64;        // a row's list: blocks of ids, each of one wave's
+// What the first three kernels leave of a row for the last.
 struct RowWork {
     u64 bins[BINS];                       // by distance: ids, or weights
     u64 sums[MAX_CHUNKS * CUT_WAVES];     // without top-k and top-p: a wave's kept weights
     double exps[MAX_CHUNKS * CUT_WAVES];  // sums of exp(l - l_max)
     float max[MAX_CHUNKS];
     int id[MAX_CHUNKS];                   // lowest id with that maximum
+    u64 need;                             // the first cut: what its bin has to give,
+    int bin;                              // the bin, or -1 if it keeps all
+    int n_blocks;                         // blocks of the list (more than BLOCKS: it is not whole)
+    unsigned block[BLOCKS];               // wave << 24 | number in the wave << 8 | ids
+    u32x2 list[BLOCKS * BLOCK];           // id, logit; a wave's blocks in the order of its ids
 };
 constexpr double ONE = 8796093022208.0;  // 2^43, the weight of the largest logit
 
@@ -203,17 +210,18 @@ __device__ __forceinline__ float exp_neg(float x) {
 // What the options and the largest logit make of a logit.
 struct Scale {
     float lmax, per_bin;
-    double per;  // log2 of a weight per logit
-    u64 least;   // min_p
+    double top, per;  // the largest logit; log2 of a weight per logit
+    u64 least;        // min_p
     const double* tab;
-    __device__ __forceinline__ Scale(const SampleRow& o, float m, const double* t) : lmax(m), tab(t) {
+    __device__ __forceinline__ Scale(const SampleRow& o, float m, const double* t) : lmax(m), top(m), tab(t) {
         per = 1.4426950408889634074 / (double)o.temperature;
         per_bin = 2047.f / 45.f * (float)per;
         least = (u64)ceil((double)o.min_p * ONE);
     }
-    // weight of an admissible logit; the largest (+inf too): 2^43
+    // weight of an admissible logit (0 for -inf); the largest, +inf too: 2^43
     __device__ __forceinline__ u64 weigh(float l) const {
-        return l == lmax ? (u64)ONE : weight(((double)l - (double)lmax) * per, tab);
+        if (lmax == INFINITY) return l == lmax ? (u64)ONE : 0;
+        return weight(((double)l - top) * per, tab);
     }
     // bin by distance, as wide as 45 T ln 2 / 2047; 2047: weight 0
     __device__ __forceinline__ int bin(float l) const { return l == lmax ? 0 : (int)fminf((lmax - l) * per_bin, 2047.f); }
@@ -246,6 +254,10 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_max_kernel(SampleA
     RowWork& ws = reinterpret_cast<RowWork*>(a.ws)[r];
     constexpr int EL = LogitRow<T>::EL;
     for (int i = blockIdx.x * 64 * CUT_WAVES + tid; i < BINS; i += a.chunks * 64 * CUT_WAVES) ws.bins[i] = 0;
+    if (blockIdx.x == 0 && tid == 0) {
+        ws.bin = -1;
+        ws.n_blocks = 0;
+    }
     float m = -INFINITY;
     int id = 0x7fffffff;
     row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
@@ -315,7 +327,7 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_sum_kernel(SampleA
 #pragma unroll
             for (int e = 0; e < EL; ++e) {
                 const u64 w = sc.weigh(l[e]);
-                sum += w >= sc.least ? w : 0;
+                sum += !sc.least || w >= sc.least ? w : 0;
             }
         } else if (mode > 0) {
 #pragma unroll
@@ -341,19 +353,111 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_sum_kernel(SampleA
     }
 }
 
+// Bin of the first cut among the summed bins (every workgroup finds it by
+// itself), and the ids up to it: each wave lists its own in their order, in
+// blocks that it takes from the row's pool.
+template <class T>
+__global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(SampleArgs a) {
+    using namespace smp;
+    constexpr int PER = BINS / (64 * CUT_WAVES);
+    __shared__ u64 red[CUT_WAVES];
+    __shared__ u64 sh_need;
+    __shared__ int sh_bin;
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int gw = blockIdx.x * CUT_WAVES + wave;
+    const SampleRow o = a.rows[r];
+    RowWork& ws = reinterpret_cast<RowWork*>(a.ws)[r];
+    if (!(o.temperature > 0.f) || (o.top_k <= 0 && !(o.top_p < 1.f))) return;
+    const LogitRow<T> row(a, r, gw, a.chunks * CUT_WAVES);
+    constexpr int EL = LogitRow<T>::EL;
+    const float lmax = row_max(ws, a.chunks, lane);
+    if (lmax == -INFINITY) return;
+    u64 m[PER], run = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        m[k] = ws.bins[PER * tid + k];
+        run += m[k];
+    }
+    u64 e = wave_scan64(run, lane);
+    if (lane == 63) red[wave] = e;
+    if (tid == 0) sh_bin = -1;
+    __syncthreads();
+    e -= run;
+    u64 total = 0;
+#pragma unroll
+    for (int w = 0; w < CUT_WAVES; ++w) {
+        if (w < wave) e += red[w];
+        total += red[w];
+    }
+    const u64 need = o.top_k > 0 ? (u64)o.top_k : max((u64)1, (u64)ceil((double)o.top_p * (double)total));
+    if (total > need) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (e < need && e + m[k] >= need) {
+                sh_bin = PER * tid + k;
+                sh_need = need - e;
+            }
+            e += m[k];
+        }
+    }
+    __syncthreads();
+    const int bin = sh_bin;
+    if (bin < 0) return;  // (ws.bin is -1)
+    if (blockIdx.x == 0 && tid == 0) {
+        ws.bin = bin;
+        ws.need = sh_need;
+    }
+    const Scale sc(o, lmax, nullptr);
+    int own = 0, last = 0;  // the wave's ids so far, the block it is filling
+    row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
+        unsigned in = 0;
+#pragma unroll
+        for (int x = 0; x < EL; ++x)
+            if (l[x] > -INFINITY && sc.bin(l[x]) <= bin) in |= 1u << x;
+        if (!__any(in)) return;
+        const int c = __popc(in);
+        int before = c;
+#pragma unroll
+        for (int st = 1; st < 64; st <<= 1) {
+            const int x = __shfl_up(before, st, 64);
+            if (lane >= st) before += x;
+        }
+        const int n = __shfl(before, 63, 64);
+        before -= c;
+        // blocks first .. first + more - 1 of the wave are new: numbers base on
+        const int first = (own + BLOCK - 1) / BLOCK, more = (own + n + BLOCK - 1) / BLOCK - first;
+        int base = 0;
+        if (more) {
+            if (lane == 0) base = atomicAdd(&ws.n_blocks, more);
+            base = __shfl(base, 0, 64);
+        }
+#pragma unroll
+        for (int x = 0; x < EL; ++x) {
+            if (!((in >> x) & 1u)) continue;
+            const int p = own + before++, q = p / BLOCK, at = q < first ? last : base + q - first;
+            if (at < BLOCKS) ws.list[at * BLOCK + p % BLOCK] = u32x2{(unsigned)(i0 + x), __float_as_uint(l[x])};
+        }
+        own += n;
+        // how full every block is that this run has touched
+        const int q = max(first - 1, 0) + lane, at = q < first ? last : base + q - first;
+        if (q * BLOCK < own && at < BLOCKS)
+            ws.block[at] = (unsigned)gw << 24 | (unsigned)(q & 0xffff) << 8 | (unsigned)min(BLOCK, own - q * BLOCK);
+        if (more) last = base + more - 1;
+    });
+}
+
 template <class T>
 __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a) {
     using namespace smp;
     constexpr int BIN_IDS = THREADS;         // ids of a cut's bin that are ranked at once
-    constexpr int BLOCKS = 176, BLOCK = 64;  // the short list: blocks of ids of one wave each
     __shared__ u64 hw[BINS];
     __shared__ u64 lk[BIN_IDS], lw[BIN_IDS];
-    __shared__ u32x2 list[BLOCKS * BLOCK];   // id, logit
-    __shared__ unsigned char block_of[WAVES][BLOCKS];
+    __shared__ unsigned block[BLOCKS];
+    __shared__ int in_order[BLOCKS];  // the list's blocks in the order of ids: number << 8 | ids
     __shared__ u64 red[WAVES];
     __shared__ double tab[256];
     __shared__ u64 sh_cut, sh_need;
-    __shared__ int sh_bin, n_ids, n_blocks;
+    __shared__ int sh_bin, n_ids;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     LogitRow<T> row(a, r, wave, WAVES);
     const RowWork& ws = reinterpret_cast<const RowWork*>(a.ws)[r];
@@ -392,7 +496,6 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
         return;
     }
     fill_table(tab);
-    if (tid == 0) n_blocks = 0;
     const Scale sc(o, lmax, tab);
     // where u falls: the first id whose running sum passes u * total, the last kept one at most
     auto target_of = [&](u64 total) __attribute__((always_inline)) {
@@ -404,17 +507,39 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
     int cut_id = -1;
     auto kept = [&](int i, float l) __attribute__((always_inline)) { return l > cut_l || (l == cut_l && i <= cut_id); };
 
-    // All ids of the row, or once SHORT has listed those up to the first cut's
-    // bin, all of the list, are gone through once per stage: BIN adds up the
-    // bins (the first time they are there already), RANK lists the ids of the
+    // All ids of the row, or if there is a whole list, of the list, are gone
+    // through once per stage: BIN adds up the bins, RANK lists the ids of the
     // cut's bin, DIGIT adds up digits of their keys if they are too many, SUM
     // adds the kept weights. Cut 0 is top-k's (every id measures 1), cut 1
-    // top-p's (an id measures its weight).
-    enum { BIN, SHORT, RANK, DIGIT, SUM };
-    int stage = BIN, cut = 0, digit = 0, shift = 52, nb = 0, bin = -1;
+    // top-p's (an id measures its weight); the first of them has its bin already.
+    enum { BIN, RANK, DIGIT, SUM };
+    int cut = o.top_k > 0 ? 0 : o.top_p < 1.f ? 1 : 2;
+    const bool summed = cut == 2;  // no filters: the sums are there
+    int stage = BIN, digit = 0, shift = 52, nb = 0, bin = -1;
     u64 prefix = 0, sum = 0;
-    bool fresh = true, listed = false;  // the bins are the second kernel's; the ids are in the list
-    int own = 0;                        // this wave's ids in the list
+    const int n_blocks = ws.n_blocks;
+    const bool listed = !summed && ws.bin >= 0 && n_blocks <= BLOCKS;
+    if (!summed) {
+        if (ws.bin >= 0) stage = RANK;
+        else ++cut;  // it keeps all
+        if (tid == 0) {
+            sh_bin = ws.bin;
+            sh_need = ws.need;
+        }
+    }
+    if (listed) {
+        // the list's blocks in the order of their waves and numbers
+        for (int i = tid; i < n_blocks; i += THREADS) block[i] = ws.block[i];
+        __syncthreads();
+        for (int i = wave; i < n_blocks; i += WAVES) {
+            int before = 0;
+            for (int j = lane; j < n_blocks; j += 64) before += block[j] < block[i];
+            before = (int)wave_sum64((u64)before);
+            if (lane == 0) in_order[before] = i << 8 | (int)(block[i] & 0xff);
+        }
+    }
+    // this wave's blocks
+    const int b_lo = n_blocks * wave / WAVES, b_hi = n_blocks * (wave + 1) / WAVES;
     auto visit = [&](int i, float l) __attribute__((always_inline)) {
         const int b = sc.bin(l);
         if (!kept(i, l) || b == 2047 || ((stage == RANK || stage == DIGIT) && b != bin)) return;
@@ -433,72 +558,57 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
             if ((k >> shift >> nb) == prefix) atomicAdd(&hw[(k >> shift) & ((1 << nb) - 1)], w);
         }
     };
+    // f(id, logit) for this wave's listed ids, 64 at a time (-inf: a lane
+    // without one), until it returns true; the next blocks are on their way meanwhile
+    auto each_listed = [&](auto&& f) __attribute__((always_inline)) {
+        constexpr int D = 4;
+        u32x2 x[D];
+        int n[D];
+        auto fetch = [&](int b, u32x2& y, int& m) __attribute__((always_inline)) {
+            const int q = b < b_hi ? in_order[b] : 0;
+            m = q & 0xff;
+            y = ws.list[(q >> 8) * BLOCK + lane];
+        };
+#pragma unroll
+        for (int u = 0; u < D; ++u) fetch(b_lo + u, x[u], n[u]);
+#pragma unroll 1
+        for (int b = b_lo; b < b_hi; ++b) {
+            const u32x2 y = x[0];
+            const int m = n[0];
+#pragma unroll
+            for (int u = 0; u + 1 < D; ++u) {
+                x[u] = x[u + 1];
+                n[u] = n[u + 1];
+            }
+            fetch(b + D, x[D - 1], n[D - 1]);
+            if (f((int)y.x, lane < m ? __uint_as_float(y.y) : -INFINITY)) break;
+        }
+    };
     for (;;) {
         if (stage == BIN && cut == 0 && o.top_k <= 0) cut = 1;
         if (stage == BIN && cut == 1 && !(o.top_p < 1.f)) cut = 2;
         if (cut == 2) stage = SUM;
-        if (stage == SUM && fresh) break;  // the sums are there
+        if (summed) break;
         nb = digit < 2 ? 11 : 10;
         if (stage == DIGIT) shift -= nb;
         if (stage == BIN || stage == DIGIT)
-            for (int i = tid; i < BINS; i += THREADS) hw[i] = stage == BIN && fresh ? ws.bins[i] : 0;
+            for (int i = tid; i < BINS; i += THREADS) hw[i] = 0;
         if (tid == 0) n_ids = 0;
-        bin = sh_bin;
         __syncthreads();
-        if (stage == SHORT) {
-            // every wave lists its ids up to the bin in their order, in blocks of the workgroup's pool
-            int last = 0;  // the block that the wave is filling
-            row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
-                unsigned in = 0;
-#pragma unroll
-                for (int e = 0; e < EL; ++e)
-                    if (l[e] > -INFINITY && sc.bin(l[e]) <= bin) in |= 1u << e;
-                if (!__any(in)) return;
-                int c = __popc(in), before = c;
-#pragma unroll
-                for (int st = 1; st < 64; st <<= 1) {
-                    const int x = __shfl_up(before, st, 64);
-                    if (lane >= st) before += x;
-                }
-                const int n = __shfl(before, 63, 64);
-                before -= c;
-                // blocks first .. first + more - 1 of the wave are new: numbers base on
-                const int first = (own + BLOCK - 1) / BLOCK, more = (own + n + BLOCK - 1) / BLOCK - first;
-                int base = 0;
-                if (more) {
-                    if (lane == 0) base = atomicAdd(&n_blocks, more);
-                    base = __shfl(base, 0, 64);
-                    if (lane < more && base + lane < BLOCKS) block_of[wave][first + lane] = (unsigned char)(base + lane);
-                }
-#pragma unroll
-                for (int e = 0; e < EL; ++e) {
-                    if (!((in >> e) & 1u)) continue;
-                    const int p = own + before++, q = p / BLOCK, at = q < first ? last : base + q - first;
-                    if (at < BLOCKS) list[at * BLOCK + p % BLOCK] = u32x2{(unsigned)(i0 + e), __float_as_uint(l[e])};
-                }
-                own += n;
-                if (more) last = base + more - 1;
+        bin = sh_bin;
+        if (listed) {
+            each_listed([&](int i, float l) __attribute__((always_inline)) {
+                if (l > -INFINITY) visit(i, l);
+                return false;
             });
-            __syncthreads();
-            listed = n_blocks <= BLOCKS;
-            stage = RANK;
-            continue;
-        }
-        if (!(stage == BIN && fresh)) {
-            if (listed) {
-                for (int p = lane; p - lane < own; p += BLOCK) {
-                    const u32x2 x = list[block_of[wave][p / BLOCK] * BLOCK + lane];
-                    if (p < own) visit((int)x.x, __uint_as_float(x.y));
-                }
-            } else {
-                row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
+        } else {
+            row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int e = 0; e < EL; ++e) visit(i0 + e, l[e]);
-                });
-            }
-            if (stage == SUM) break;
-            __syncthreads();
+                for (int e = 0; e < EL; ++e) visit(i0 + e, l[e]);
+            });
         }
+        if (stage == SUM) break;
+        __syncthreads();
         if (stage == RANK) {
             const int n = n_ids;
             __syncthreads();
@@ -549,10 +659,8 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
             }
             __syncthreads();
             if (stage == BIN) {
-                const bool was_fresh = fresh;
-                fresh = false;
                 if (sh_bin < 0) ++cut;  // nothing is cut off
-                else stage = was_fresh ? SHORT : RANK;
+                else stage = RANK;
                 continue;
             }
             prefix = sh_cut;
@@ -567,8 +675,8 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
 
     // The place of u times the sum of the kept weights. The waves' sums, in the
     // order of their ids, say which wave's ids it is among.
-    const int waves = fresh ? cut_waves : WAVES;
-    if (!fresh) {
+    const int waves = summed ? cut_waves : WAVES;
+    if (!summed) {
         sum = wave_sum64(sum);
         if (lane == 0) red[wave] = sum;
     }
@@ -577,7 +685,7 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int w = PER * lane + k;
-        part[k] = w < waves ? fresh ? ws.sums[w] : red[w] : 0;
+        part[k] = w < waves ? summed ? ws.sums[w] : red[w] : 0;
         mine += part[k];
     }
     u64 run = wave_scan64(mine, lane);
@@ -595,19 +703,15 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
     u64 before = __shfl(run, at_lane, 64);
     if (listed) {
         if (wave != owner) return;
-        for (int p = lane; p - lane < own; p += BLOCK) {
-            const u32x2 x = list[block_of[wave][p / BLOCK] * BLOCK + lane];
-            const float l = __uint_as_float(x.y);
-            u64 w = p < own && kept((int)x.x, l) ? sc.weigh(l) : 0;
+        each_listed([&](int i, float l) __attribute__((always_inline)) {
+            u64 w = l > -INFINITY && kept(i, l) ? sc.weigh(l) : 0;
             if (w < sc.least) w = 0;
             const u64 c = wave_scan64(w, lane);
             const unsigned long long hit = __ballot(before + c > target);
-            if (hit) {
-                if (lane == __builtin_ctzll(hit)) finish((int)x.x, l);
-                return;
-            }
+            if (hit && lane == __builtin_ctzll(hit)) finish(i, l);
             before += __shfl(c, 63, 64);
-        }
+            return hit != 0;
+        });
         return;
     }
     // the owner's pieces, 64 at a time, are added up by all of this workgroup's waves
@@ -665,9 +769,10 @@ inline int sample_chunks(int n, int V) {
 inline size_t sample_ws_bytes(int rows) {
     return sizeof(smp::RowWork) * (size_t)(rows < SAMPLE_ROWS ? rows : SAMPLE_ROWS);
 }
-// The choice for n rows; a.ws has sample_ws_bytes(n).
+// The choice for n rows; a.ws has sample_ws_bytes(n). `filters`: some row may
+// have top-k or top-p.
 template <class T>
-inline void sample_rows(SampleArgs a, int n, hipStream_t st) {
+inline void sample_rows(SampleArgs a, int n, bool filters, hipStream_t st) {
     for (int r = 0; r < n; r += SAMPLE_ROWS) {
         const int m = n - r < SAMPLE_ROWS ? n - r : SAMPLE_ROWS;
         SampleArgs b = a;
@@ -679,6 +784,7 @@ inline void sample_rows(SampleArgs a, int n, hipStream_t st) {
         b.chunks = sample_chunks<T>(m, a.V);
         hipLaunchKernelGGL(sample_max_kernel<T>, dim3(b.chunks, m), dim3(64 * smp::CUT_WAVES), 0, st, b);
         hipLaunchKernelGGL(sample_sum_kernel<T>, dim3(b.chunks, m), dim3(64 * smp::CUT_WAVES), 0, st, b);
+        if (filters) hipLaunchKernelGGL(sample_list_kernel<T>, dim3(b.chunks, m), dim3(64 * smp::CUT_WAVES), 0, st, b);
         hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(m), dim3(smp::THREADS), 0, st, b);
     }
 }
