@@ -16,7 +16,11 @@ namespace {
 // fewer: four per CU.
 constexpr int ATTN_WGS = 1024;
 // Fewest positions of a cut range: two blocks of 32 per wave.
-constexpr int ATTN_PART = 256;
+constexpr int ATTN_PART = 512;
+// Rows of a sequence and key/value head from which the kernel of 128 rows per
+// workgroup takes them (bf16), the workgroups it is cut into where the rows
+// give fewer (one per CU), and the fewest positions of a part.
+constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
 
 template <class T>
 class PagedCacheT final : public PagedCache {
@@ -26,6 +30,7 @@ class PagedCacheT final : public PagedCache {
         G_ = p.n_head / p.n_kv_head;
         // parts of cut ranges: ATTN_WGS / n_kv_head whole ones and a partial one for each of as many ranges
         max_parts_ = 2 * (ATTN_WGS / p.n_kv_head + 1);
+        if (big_rows(p.max_tokens)) max_parts_ += BIG_ROWS / 16 * 2 * (BIG_WGS / p.n_kv_head + 1);
         if (dev_ == WHISPER_NO_DEVICE) return;
         DeviceScope scope(dev_);
         head_elems_ = (long long)p.page_size * p.head_size;
@@ -36,7 +41,7 @@ class PagedCacheT final : public PagedCache {
         // room for the longest plan, so that recorded launches keep their addresses
         const long long T0 = p.max_tokens, S0 = p.max_seqs;
         max_tiles_ = (int)std::min(T0, T0 / 32 + 2 * S0);
-        plan_.cap = HEAD_INTS + 8 * (T0 * G_ / 16 + S0 + max_parts_) + 5LL * max_parts_ + 4LL * max_tiles_ +
+        plan_.cap = HEAD_INTS + 8 * (T0 * G_ / 16 + S0 + max_parts_) + 6LL * max_parts_ + 4LL * max_tiles_ +
                     2 * (std::min(T0, T0 / p.page_size + S0) + 2 * S0);
         plan_.dev = dalloc<int>(plan_.cap);
         parts_ = dalloc<float>((size_t)max_parts_ * p.n_kv_head * 16 * (p.head_size + 2));
@@ -116,7 +121,7 @@ class PagedCacheT final : public PagedCache {
         need_chunk();
         DeviceScope scope(dev_);
         const bool rec = capturing(st_);
-        if (n_items_ == 0 && !rec) return;
+        if (n_items_ + n_bigs_ == 0 && !rec) return;
         AttnArgs a{view(), layer, P_.n_head, G_, q, out, q_ld, out_ld, scale * 1.4426950408889634f, plan_.dev,
                    parts_};
         if (P_.head_size == 64) launch_attn<64>(a, rec);
@@ -182,7 +187,7 @@ class PagedCacheT final : public PagedCache {
         int row = 0;
         for (int i = 0; i < n; ++i) row = add_tiles(t, seqs[i], 0, book_.length(seqs[i]), row);
         if (row == 0) return;
-        const ListHead head{0, 0, (int)(t.size() - HEAD_INTS) / 4, 0, HEAD_INTS, {}};
+        const ListHead head{0, 0, (int)(t.size() - HEAD_INTS) / 4, 0, HEAD_INTS, 0, 0, 0};
         memcpy(t.data(), &head, sizeof(head));
         put(list_, t);
         move<false>(layer, list_.dev, head.tiles, k, v, k_ld, v_ld, row);
@@ -213,7 +218,7 @@ class PagedCacheT final : public PagedCache {
     // the chunk: its sequences, new tokens and the lengths of its lists
     std::vector<int> chunk_, blob_;
     bool plan_ok_ = false;
-    int tokens_ = 0, n_items_ = 0, n_merges_ = 0, n_tiles_ = 0;
+    int tokens_ = 0, n_items_ = 0, n_bigs_ = 0, n_merges_ = 0, n_tiles_ = 0;
     int max_tiles_ = 0;
 
     template <class U>
@@ -306,6 +311,10 @@ class PagedCacheT final : public PagedCache {
         copy_pages(list_.dev + upd.size(), (int)copies.size());
     }
 
+    // Whether a chunk's `count` tokens of one sequence go to the kernel of many rows.
+    bool big_rows(int count) const { return sizeof(T) == 2 && (long long)count * G_ >= BIG_FROM; }
+    bool max_bigs() const { return big_rows(P_.max_tokens); }
+
     // Positions [first, first + n) of a sequence as tiles; returns the row after its last.
     static int add_tiles(std::vector<int>& t, int seq, int first, int n, int row) {
         for (int p = first; p < first + n;) {
@@ -324,43 +333,53 @@ class PagedCacheT final : public PagedCache {
         std::vector<AttnItem> items, cut;
         std::vector<MergeItem> merges;
         std::vector<int> tiles;
-        int row = 0;
-        long long work = 0;
-        for (int i = 0; i < n; ++i) {
-            const int s = seqs[i], past = book_.length(s) - counts[i], rows = counts[i] * G_;
-            for (int j = 0; j < rows; j += 16) {
-                const int end = past + (std::min(j + 16, rows) - 1) / G_ + 1;
-                items.push_back(AttnItem{s, past, counts[i], row, j, 0, end, -1});
-                work += end;
+        int row = 0, np = 0;
+        // items of `step` rows of the sequences that kernel `big` takes, cut
+        // into about `wgs` workgroups, a part's positions a multiple of 128
+        auto plan = [&](bool big, int step, int wgs, int least) {
+            items.clear();
+            cut.clear();
+            long long work = 0;
+            int tok0 = 0;
+            for (int i = 0; i < n; tok0 += counts[i++]) {
+                const int s = seqs[i], past = book_.length(s) - counts[i], rows = counts[i] * G_;
+                if (big_rows(counts[i]) != big) continue;
+                for (int j = 0; j < rows; j += step) {
+                    const int end = past + (std::min(j + step, rows) - 1) / G_ + 1;
+                    items.push_back(AttnItem{s, past, counts[i], tok0, j, 0, end, -1});
+                    work += end;
+                }
             }
-            row = add_tiles(tiles, s, past, counts[i], row);
-        }
-        const long long part =
-            std::max<long long>(ATTN_PART, (work * P_.n_kv_head / ATTN_WGS + 127) / 128 * 128);
-        int np = 0;
-        for (const AttnItem& t : items) {
-            const int k = (int)((t.kv1 + part - 1) / part);
-            if (k < 2) {
-                cut.push_back(t);
-                continue;
+            const long long part = std::max<long long>(least, (work * P_.n_kv_head / wgs + 127) / 128 * 128);
+            for (const AttnItem& t : items) {
+                const int k = (int)((t.kv1 + part - 1) / part);
+                if (k < 2) {
+                    cut.push_back(t);
+                    continue;
+                }
+                const int len = ((t.kv1 + k - 1) / k + 127) / 128 * 128, slots = step / 16, first = np;
+                for (int p = 0; p < t.kv1; p += len) {
+                    AttnItem c = t;
+                    c.kv0 = p;
+                    c.kv1 = std::min(p + len, t.kv1);
+                    c.part = np;
+                    np += slots;
+                    cut.push_back(c);
+                }
+                for (int g = 0; g < slots && t.j0 + 16 * g < t.count * G_; ++g)
+                    merges.push_back(MergeItem{t.count, t.tok0, t.j0 + 16 * g, first + g, (np - first) / slots, slots});
             }
-            const int len = ((t.kv1 + k - 1) / k + 127) / 128 * 128;
-            MergeItem m{t.count, t.tok0, t.j0, np, 0};
-            for (int p = 0; p < t.kv1; p += len) {
-                AttnItem c = t;
-                c.kv0 = p;
-                c.kv1 = std::min(p + len, t.kv1);
-                c.part = np++;
-                ++m.n;
-                cut.push_back(c);
-            }
-            merges.push_back(m);
-        }
-        if (np > max_parts_) throw DeviceError("paged cache: more parts than planned for");
-        // long ranges first, so that none starts last
-        std::stable_sort(cut.begin(), cut.end(),
-                         [](const AttnItem& a, const AttnItem& b) { return a.kv1 - a.kv0 > b.kv1 - b.kv0; });
+            if (np > max_parts_) throw DeviceError("paged cache: more parts than planned for");
+            // long ranges first, so that none starts last
+            std::stable_sort(cut.begin(), cut.end(),
+                             [](const AttnItem& a, const AttnItem& b) { return a.kv1 - a.kv0 > b.kv1 - b.kv0; });
+        };
+        for (int i = 0; i < n; ++i) row = add_tiles(tiles, seqs[i], book_.length(seqs[i]) - counts[i], counts[i], row);
+        plan(true, BIG_ROWS, BIG_WGS, BIG_PART);
+        const std::vector<AttnItem> bigs = cut;
+        plan(false, 16, ATTN_WGS, ATTN_PART);
         n_items_ = (int)cut.size();
+        n_bigs_ = (int)bigs.size();
         n_merges_ = (int)merges.size();
         n_tiles_ = (int)tiles.size() / 4;
         blob_.assign(HEAD_INTS, 0);
@@ -373,7 +392,8 @@ class PagedCacheT final : public PagedCache {
         add(cut.data(), cut.size() * (sizeof(AttnItem) / sizeof(int)));
         const size_t ma = add(merges.data(), merges.size() * (sizeof(MergeItem) / sizeof(int)));
         const size_t ta = add(tiles.data(), tiles.size());
-        const ListHead head{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, {}};
+        const size_t ba = add(bigs.data(), bigs.size() * (sizeof(AttnItem) / sizeof(int)));
+        const ListHead head{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, 0};
         memcpy(blob_.data(), &head, sizeof(head));
     }
 
@@ -382,7 +402,11 @@ class PagedCacheT final : public PagedCache {
         // a recorded launch may meet a longer list at its replay: the kernels go through it in strides
         const unsigned ni = rec ? 2 * ATTN_WGS : (unsigned)n_items_ * P_.n_kv_head;
         const unsigned nm = rec ? ATTN_WGS : (unsigned)n_merges_ * P_.n_kv_head;
-        hipLaunchKernelGGL((paged_attn_kernel<T, D, false>), dim3(ni), dim3(256), 0, st_, a);
+        if constexpr (sizeof(T) == 2) {
+            const unsigned nb = rec ? (max_bigs() ? 2 * BIG_WGS : 0) : (unsigned)n_bigs_ * P_.n_kv_head;
+            if (nb) hipLaunchKernelGGL(paged_attn_big_kernel<D>, dim3(nb), dim3(BIG_THREADS), 0, st_, a);
+        }
+        if (ni) hipLaunchKernelGGL((paged_attn_kernel<T, D, false>), dim3(ni), dim3(256), 0, st_, a);
         if (nm) hipLaunchKernelGGL((paged_merge_kernel<T, D, false>), dim3(nm), dim3(256), 0, st_, a);
     }
 

@@ -943,7 +943,7 @@ class EngineT final : public Engine {
                         items[ni++] = AttnItem{up[r], p, 1, r, 0, 0, p + 1, -1};
                     }
                 }
-                *reinterpret_cast<ListHead*>(up.data() + plan_at) = ListHead{ni, 0, 0, 0, 0, {}};
+                *reinterpret_cast<ListHead*>(up.data() + plan_at) = ListHead{ni, 0, 0, 0, 0, 0, 0, 0};
             }
             upload(3, pf_list_, up.data(), up.size() * sizeof(int));
             RowBufs b{pf_list_, paged_ ? pf_list_ + base : pf_list_, pf_list_ + pf_cap_, pf_dx_, pf_dz_, pf_dq_, pf_datt_, pf_dh_, pf_rowlen_, pf_part_};

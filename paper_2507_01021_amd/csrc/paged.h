@@ -15,6 +15,8 @@
 // run.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace wmi {
@@ -44,6 +46,11 @@ struct PagedView {
     }
 };
 
+// An entry of a list that no running kernel writes, at an address that is the
+// same in all lanes: a scalar load, which does not queue behind vector loads.
+typedef const int __attribute__((address_space(4))) * ScalarList;
+__device__ __forceinline__ int list_at(const int* list, int i) { return ((ScalarList)(uintptr_t)list)[i]; }
+
 // A run of up to 32 positions of one sequence inside one block of 32, and the
 // row of its first position in the caller's rows.
 struct PageTile {
@@ -55,7 +62,7 @@ struct PageTile {
 // Kernels read it when they run and go through their part in strides of the
 // grid, so a recorded launch serves whatever list is current at its replay.
 struct ListHead {
-    int items, merges, tiles, merges_at, tiles_at, pad[3];
+    int items, merges, tiles, merges_at, tiles_at, bigs, bigs_at, pad;
 };
 constexpr int HEAD_INTS = sizeof(ListHead) / sizeof(int);
 
@@ -232,10 +239,10 @@ struct AttnItem {
     int kv0, kv1;   // positions, kv0 a multiple of 32
     int part;       // result slot of a cut range, or -1: the result itself
 };
-// Rows j0 .. of a sequence whose positions were cut into n parts, one after
-// another from slot `part`.
+// Rows j0 .. j0 + 15 of a sequence whose positions were cut into n parts, in
+// slots part, part + step, ...
 struct MergeItem {
-    int count, tok0, j0, part, n;
+    int count, tok0, j0, part, n, step;
 };
 struct AttnArgs {
     PagedView c;
@@ -296,7 +303,8 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
     __shared__ float sm[4][16], sl[4][16];
     const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
     const AttnItem* items = reinterpret_cast<const AttnItem*>(a.plan + HEAD_INTS);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
+    const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int w0 = blockIdx.x; w0 < head.items * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const AttnItem t = items[it];
@@ -314,8 +322,10 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
         float m = -INFINITY, l = 0.f;
         const int* table = a.c.table + (long long)t.seq * a.c.ld;
         const int pmask = (1 << a.c.shift) - 1;
+        int next = list_at(table, min(t.kv0 + wave * 32, t.kv1 - 1) >> a.c.shift);  // pages are looked up a block ahead
         for (int p = t.kv0 + wave * 32; p < t.kv1; p += 128) {
-            const int page = table[p >> a.c.shift], p0 = p & pmask;
+            const int page = next, p0 = p & pmask;
+            next = list_at(table, min(p + 128, t.kv1 - 1) >> a.c.shift);
             const T* kb = a.c.template head<T>(page, a.layer, 0, h) + (p0 >> 4) * (NK * BLK) + lane * EL;
             const T* vb = a.c.template head<T>(page, a.layer, 1, h) + val_off<T>(p0, 0, D) + lane * EL;
             V kf[2][NK], vf[NV][ND];
@@ -462,43 +472,315 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
     }
 }
 
-// Joins the parts of cut ranges, in their order: one workgroup per 16 rows and kv head.
+// Joins the parts of cut ranges: one workgroup per 16 rows and kv head. Wave w
+// adds up parts w, w + 4, ..., its lane dims D/4 (lane % 4) .. of row lane / 4,
+// weighted by the largest maximum of all parts; the waves' sums are added in order.
 template <class T, int D, bool FRAG>
 __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
+    constexpr int N = D / 16;  // 16-byte pieces of a lane
+    __shared__ float so[3][16][D + 4];
+    __shared__ float sl[4][16], sm[4][16];
     const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
     const MergeItem* merges = reinterpret_cast<const MergeItem*>(a.plan + head.merges_at);
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane >> 2, q4 = lane & 3;
     for (int w0 = blockIdx.x; w0 < head.merges * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const MergeItem t = merges[it];
         const int j = t.j0 + row;
-        if (j >= t.count * a.G) continue;
-        const long long step = (long long)a.c.Hkv * (16 * (D + 2));
+        const bool live = j < t.count * a.G;
+        const long long step = (long long)t.step * a.c.Hkv * (16 * (D + 2));
         const float* ps = a.parts + ((long long)t.part * a.c.Hkv + h) * (16 * (D + 2));
+        // the largest maximum: every lane takes every 16th part of its row
         float m = -INFINITY;
-        for (int i = 0; i < t.n; ++i) m = fmaxf(m, ps[i * step + 16 * D + row]);
+        for (int i = wave * 4 + q4; i < t.n; i += 16) m = fmaxf(m, live ? ps[i * step + 16 * D + row] : -INFINITY);
+        m = fmaxf(m, __shfl_xor(m, 1, 64));
+        m = fmaxf(m, __shfl_xor(m, 2, 64));
+        if (q4 == 0) sm[wave][row] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(sm[0][row], sm[1][row]), fmaxf(sm[2][row], sm[3][row]));
         const float mu = m == -INFINITY ? 0.f : m;
-        float l = 0.f, x[D / 16];
+        float l = 0.f;
+        mfma_f32x4 x[N];
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) x[e] = 0.f;
-        for (int i = 0; i < t.n; ++i) {
-            const float w = exp2_softmax(ps[i * step + 16 * D + row] - mu);
-            l += w * ps[i * step + 16 * D + 16 + row];
+        for (int c = 0; c < N; ++c) x[c] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+        if (live) {
+#pragma unroll 4
+            for (int i = wave; i < t.n; i += 4) {
+                const float* p = ps + i * step;
+                const float w = exp2_softmax(p[16 * D + row] - mu);
+                l += w * p[16 * D + 16 + row];
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-                const float4 y = ld4(ps + i * step + row * D + d0 + c * 64);
-                x[4 * c] += w * y.x;
-                x[4 * c + 1] += w * y.y;
-                x[4 * c + 2] += w * y.z;
-                x[4 * c + 3] += w * y.w;
+                for (int c = 0; c < N; ++c) x[c] += w * *reinterpret_cast<const mfma_f32x4*>(p + row * D + (c * 4 + q4) * 4);
             }
         }
-        const int tk = j / a.G, gg = j - tk * a.G;
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        if (q4 == 0) sl[wave][row] = l;
+        if (wave > 0) {
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c)
-            attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d0 + c * 64, x[4 * c] * inv, x[4 * c + 1] * inv,
-                                x[4 * c + 2] * inv, x[4 * c + 3] * inv);
+            for (int c = 0; c < N; ++c) *reinterpret_cast<mfma_f32x4*>(&so[wave - 1][row][(c * 4 + q4) * 4]) = x[c];
+        }
+        __syncthreads();
+        if (wave == 0 && live) {
+            l = sl[0][row] + sl[1][row] + sl[2][row] + sl[3][row];
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            const int tk = j / a.G, gg = j - tk * a.G;
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                const int d = (c * 4 + q4) * 4;
+#pragma unroll
+                for (int w = 0; w < 3; ++w) x[c] += *reinterpret_cast<const mfma_f32x4*>(&so[w][row][d]);
+                attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d, x[c][0] * inv, x[c][1] * inv, x[c][2] * inv, x[c][3] * inv);
+            }
+        }
+        __syncthreads();  // the next item's LDS
+    }
+}
+
+// ------------------------------------------------------------------ attention of many rows (bf16)
+//
+// 128 rows per workgroup, 32 per wave in two tiles of 16, and blocks of 64 positions that all waves read from LDS: two or three buffers,
+// filled by direct global->LDS loads of whole 1 KiB fragments, so that every
+// LDS access is a linear 16 bytes per lane. Two waves share a SIMD: the matrix
+// products of one run beside the other's softmax. A row's reference moves only
+// when a score is more than 2^8 above it, so the sums are rescaled rarely.
+// An item's rows may be fewer than 128 (its waves and tiles without rows do
+// nothing but help loading) and its positions a part of a cut range; slot
+// part + i then holds the i-th 16 rows.
+__device__ __forceinline__ void load_to_lds(const bf16* src, unsigned char* dst) {
+    __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
+}
+constexpr int BIG_ROWS = 128;
+constexpr int BIG_TILES = 2;  // tiles of 16 rows per wave
+constexpr int BIG_THREADS = BIG_ROWS / 16 / BIG_TILES * 64;
+template <int D>
+__global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs a) {
+    typedef mfma_bf16x8 V;
+    constexpr int NK = D / 32, ND = D / 16, UT = BIG_TILES, NW = BIG_THREADS / 64;
+    constexpr int HALF = 64 * D;           // bytes of the keys, or of the values, of 32 positions
+    constexpr int TILE = 4 * HALF;         // a block: keys, keys, values, values
+    constexpr int NB = D == 64 ? 3 : 2;    // buffers: two workgroups per CU at least
+    __shared__ __align__(16) unsigned char lds[NB * TILE];
+    const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
+    const AttnItem* items = reinterpret_cast<const AttnItem*>(a.plan + head.bigs_at);
+    const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int pmask = (1 << a.c.shift) - 1;
+    for (int w0 = blockIdx.x; w0 < head.bigs * a.c.Hkv; w0 += gridDim.x) {
+        const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
+        const AttnItem t = items[it];
+        const int rows = t.count * a.G;
+        const int r0 = t.j0 + wave * 16 * UT;
+        const int nu = min(UT, max(0, (min(rows, t.j0 + BIG_ROWS) - r0 + 15) / 16));  // this wave's tiles
+        int lim[UT];  // positions of the range that the lane's row of each tile sees
+        V qf[UT][NK];
+#pragma unroll
+        for (int u = 0; u < UT; ++u) {
+            const int j = min(r0 + u * 16 + fr, rows - 1), tok = j / a.G, g = j - tok * a.G;
+            lim[u] = min(t.past + tok + 1, t.kv1);
+            const bf16* q = static_cast<const bf16*>(a.q) + (long long)(t.tok0 + tok) * a.q_ld + (h * a.G + g) * D + fc * 8;
+#pragma unroll
+            for (int s = 0; s < NK; ++s) qf[u][s] = *reinterpret_cast<const V*>(q + s * 32);
+        }
+        // positions that every row of the wave sees, and the last one does (a wave without rows: none)
+        const int all = nu ? t.past + r0 / a.G + 1 : 0;
+        const int end = nu ? min(t.kv1, t.past + (min(r0 + 16 * UT, rows) - 1) / a.G + 1) : 0;
+        mfma_f32x4 o[ND][UT];
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int u = 0; u < UT; ++u) o[d][u] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+        float m[UT], l[UT];
+#pragma unroll
+        for (int u = 0; u < UT; ++u) {
+            m[u] = -INFINITY;
+            l[u] = 0.f;
+        }
+        // positions p .. p + 63 into buffer b: a quarter of the waves load each
+        // of the halves' keys and values. A half behind the range's last block of
+        // 32 loads that block again (its scores are masked).
+        const int* table = a.c.table + (long long)t.seq * a.c.ld;
+        const int last = (t.kv1 - 1) & ~31;
+        constexpr int WP = NW / 4, N = HALF / 1024 / WP;  // waves per quarter, loads per wave
+        const int part = wave / WP, sub = wave % WP;
+        auto place = [&](int p) __attribute__((always_inline)) { return min(p + (part & 1) * 32, last); };
+        auto issue = [&](int p, int page, int b) __attribute__((always_inline)) {
+            const int pp = place(p);
+            const bf16* src = a.c.template head<bf16>(page, a.layer, part >> 1, h) +
+                              ((pp & pmask) >> 5) * (HALF / 2) + sub * N * 512 + lane * 8;
+            unsigned char* dst = lds + b * TILE + part * HALF + sub * N * 1024;
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_to_lds(src + i * 512, dst + i * 1024);
+        };
+        // One block of 64 positions from LDS. MASKED: not every row sees all of
+        // them. Values behind the range may be anything and count as 0, and so
+        // do values that are not finite: 0 * inf would reach rows that do not
+        // see them (what they are to the others is added at the end).
+        bool odd = false;
+        auto block = [&](auto is_masked, int p, const unsigned char* tk) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(is_masked)::value;
+            const unsigned char* tv = tk + 2 * HALF;
+            mfma_f32x4 sc[UT][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                V kf[NK];
+#pragma unroll
+                for (int s = 0; s < NK; ++s) kf[s] = *reinterpret_cast<const V*>(tk + (b * NK + s) * 1024);
+#pragma unroll
+                for (int u = 0; u < UT; ++u) {
+                    mfma_f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < NK; ++s) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s], qf[u][s], x, 0, 0, 0);
+                    if constexpr (MASKED) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (b * 16 + r >= lim[u] - p - fc * 4) x[r] = -INFINITY;
+                    }
+                    sc[u][b] = x;
+                }
+            }
+            V pf[UT][2];
+#pragma unroll
+            for (int u = 0; u < UT; ++u) {
+                mfma_f32x4 (&cur)[4] = sc[u];
+                float mx = cur[0][0];
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, cur[b][r]);
+                mx *= a.scale;
+                if (__any(mx > m[u] + 8.f)) {  // (m starts at -inf)
+                    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    const float mn = mx > m[u] + 8.f ? mx : m[u];
+                    const float alpha = mn == m[u] ? 1.f : exp2_softmax(m[u] - mn);
+                    m[u] = mn;
+                    l[u] *= alpha;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[d][u][r] *= alpha;
+                }
+                float mu = m[u];
+                if constexpr (MASKED) mu = mu == -INFINITY ? 0.f : mu;  // a row that has seen nothing yet
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        cur[b][r] = exp2_softmax(fmaf(cur[b][r], a.scale, -mu));
+                        l[u] += cur[b][r];
+                    }
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        pf[u][s][r] = (__bf16)cur[2 * s][r];
+                        pf[u][s][4 + r] = (__bf16)cur[2 * s + 1][r];
+                    }
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    V vf = *reinterpret_cast<const V*>(tv + (s * ND + d) * 1024);
+                    if constexpr (MASKED) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool in = s * 32 + (e & 3) + (e >> 2) * 16 < t.kv1 - p - fc * 4;
+                            const bool fin = fabsf((float)vf[e]) < INFINITY;
+                            odd = odd || (in && !fin);
+                            if (!in || !fin) vf[e] = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < UT; ++u)
+                        o[d][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][s], o[d][u], 0, 0, 0);
+                }
+        };
+        int buf = 0;
+        auto page_of = [&](int p) __attribute__((always_inline)) { return list_at(table, place(p) >> a.c.shift); };
+        constexpr int AHEAD = (NB - 1) * 64;
+#pragma unroll
+        for (int i = 0; i < NB - 1; ++i)
+            if (t.kv0 + 64 * i < t.kv1) issue(t.kv0 + 64 * i, page_of(t.kv0 + 64 * i), i);
+        int page = page_of(t.kv0 + AHEAD);  // of the block that is issued next
+        for (int p = t.kv0; p < t.kv1; p += 64) {
+            // this block is in LDS (the later ones' loads may be on their way), and
+            // every wave is done with the one before
+            if (NB == 3 && p + 64 < t.kv1) __builtin_amdgcn_s_waitcnt(WMI_VMCNT_LDS(N));
+            else __builtin_amdgcn_s_waitcnt(WMI_VMCNT_LDS(0));
+            __builtin_amdgcn_s_barrier();
+            if (p + AHEAD < t.kv1) {
+                issue(p + AHEAD, page, buf == 0 ? NB - 1 : buf - 1);
+                page = page_of(p + 64 + AHEAD);
+            }
+            const unsigned char* tk = lds + buf * TILE + lane * 16;
+            buf = buf + 1 == NB ? 0 : buf + 1;
+            if (p + 64 <= all && p + 64 <= t.kv1) block(std::false_type{}, p, tk);
+            else if (p < end) block(std::true_type{}, p, tk);
+        }
+        // values of masked blocks that are not finite: what they add to the rows
+        // that see them, inf, -inf or NaN, by products of indicators
+        if (__any(odd)) {
+#pragma unroll 1
+            for (int p = max(t.kv0, (min(all, t.kv1) & ~63) - 64); p < end; p += 32) {
+                // (a block is masked or not as a whole; its blocks begin at kv0)
+                const int b0 = t.kv0 + ((p - t.kv0) & ~63);
+                if (b0 + 64 <= all && b0 + 64 <= t.kv1) continue;
+                const bf16* vb = a.c.template head<bf16>(table[p >> a.c.shift], a.layer, 1, h) + ((p & pmask) >> 5) * (HALF / 2) + lane * 8;
+#pragma unroll 1
+                for (int kind = 0; kind < 3; ++kind) {
+                    const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const V vf = *reinterpret_cast<const V*>(vb + d * 512);
+                        V is;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float y = (float)vf[e];
+                            is[e] = (__bf16)((kind == 2 ? y != y : y == what) ? 1.f : 0.f);
+                        }
+#pragma unroll
+                        for (int u = 0; u < UT; ++u) {
+                            V seen;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                seen[e] = (__bf16)((e & 3) + (e >> 2) * 16 < lim[u] - p - fc * 4 ? 1.f : 0.f);
+                            const mfma_f32x4 x =
+                                __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, seen, mfma_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) o[d][u][r] += x[r] > 0.f ? what : 0.f;
+                        }
+                    }
+                }
+            }
+        }
+        // lane: O^T[dim d * 16 + fc * 4 + r][row r0 + u * 16 + fr]
+#pragma unroll
+        for (int u = 0; u < UT; ++u) {
+            float lt = l[u];
+            lt += __shfl_xor(lt, 16, 64);
+            lt += __shfl_xor(lt, 32, 64);
+            const int j = r0 + u * 16 + fr;
+            if (u >= nu || j >= rows) continue;
+            if (t.part < 0) {
+                const int tk = j / a.G, gg = j - tk * a.G;
+                const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    attn_store<bf16, false>(a, t.tok0 + tk, h * a.G + gg, D, d * 16 + fc * 4, o[d][u][0] * inv, o[d][u][1] * inv,
+                                            o[d][u][2] * inv, o[d][u][3] * inv);
+            } else {
+                float* ps = a.parts + ((long long)(t.part + wave * UT + u) * a.c.Hkv + h) * (16 * (D + 2));
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    st4(ps + fr * D + d * 16 + fc * 4, o[d][u][0], o[d][u][1], o[d][u][2], o[d][u][3]);
+                if (fc == 0) {
+                    ps[16 * D + fr] = m[u];
+                    ps[16 * D + 16 + fr] = lt;
+                }
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(WMI_VMCNT_LDS(0));
+        __syncthreads();  // the next item's LDS
     }
 }
 
@@ -508,7 +790,7 @@ static __global__ __launch_bounds__(128) void paged_rows_kernel(const int* __res
                                                                 const int* __restrict__ pos, int n,
                                                                 int* __restrict__ plan) {
     const int r = threadIdx.x;
-    if (r == 0) *reinterpret_cast<ListHead*>(plan) = ListHead{n, 0, 0, 0, 0, {}};
+    if (r == 0) *reinterpret_cast<ListHead*>(plan) = ListHead{n, 0, 0, 0, 0, 0, 0, 0};
     if (r < n) {
         const int s = list[r], p = pos[s];
         reinterpret_cast<AttnItem*>(plan + HEAD_INTS)[r] = AttnItem{s, p, 1, r, 0, 0, p + 1, -1};

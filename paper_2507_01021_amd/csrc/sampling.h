@@ -67,7 +67,7 @@ struct RowWork {
     float max[MAX_CHUNKS];
     int id[MAX_CHUNKS];                   // lowest id with that maximum
     u64 need;                             // the first cut: what its bin has to give,
-    int bin;                              // the bin, or -1 if it keeps all
+    int bin;                              // the bin, or -1 if the filter keeps all
     int n_blocks;                         // blocks of the list (more than BLOCKS: it is not whole)
     unsigned block[BLOCKS];               // wave << 24 | number in the wave << 8 | ids
     u32x2 list[BLOCKS * BLOCK];           // id, logit; a wave's blocks in the order of its ids
@@ -254,10 +254,7 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_max_kernel(SampleA
     RowWork& ws = reinterpret_cast<RowWork*>(a.ws)[r];
     constexpr int EL = LogitRow<T>::EL;
     for (int i = blockIdx.x * 64 * CUT_WAVES + tid; i < BINS; i += a.chunks * 64 * CUT_WAVES) ws.bins[i] = 0;
-    if (blockIdx.x == 0 && tid == 0) {
-        ws.bin = -1;
-        ws.n_blocks = 0;
-    }
+    if (blockIdx.x == 0 && tid == 0) ws.n_blocks = 0;
     float m = -INFINITY;
     int id = 0x7fffffff;
     row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
@@ -380,7 +377,10 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(Sample
     }
     u64 e = wave_scan64(run, lane);
     if (lane == 63) red[wave] = e;
-    if (tid == 0) sh_bin = -1;
+    if (tid == 0) {
+        sh_bin = -1;
+        sh_need = 0;
+    }
     __syncthreads();
     e -= run;
     u64 total = 0;
@@ -401,12 +401,11 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(Sample
         }
     }
     __syncthreads();
-    const int bin = sh_bin;
-    if (bin < 0) return;  // (ws.bin is -1)
     if (blockIdx.x == 0 && tid == 0) {
-        ws.bin = bin;
+        ws.bin = sh_bin;
         ws.need = sh_need;
     }
+    const int bin = sh_bin < 0 ? 2046 : sh_bin;  // a filter that keeps all: every id of some weight
     const Scale sc(o, lmax, nullptr);
     int own = 0, last = 0;  // the wave's ids so far, the block it is filling
     row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
@@ -518,7 +517,7 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
     int stage = BIN, digit = 0, shift = 52, nb = 0, bin = -1;
     u64 prefix = 0, sum = 0;
     const int n_blocks = ws.n_blocks;
-    const bool listed = !summed && ws.bin >= 0 && n_blocks <= BLOCKS;
+    const bool listed = !summed && n_blocks <= BLOCKS;
     if (!summed) {
         if (ws.bin >= 0) stage = RANK;
         else ++cut;  // it keeps all
@@ -531,11 +530,12 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
         // the list's blocks in the order of their waves and numbers
         for (int i = tid; i < n_blocks; i += THREADS) block[i] = ws.block[i];
         __syncthreads();
-        for (int i = wave; i < n_blocks; i += WAVES) {
+        for (int i = tid; i < n_blocks; i += THREADS) {
+            const unsigned k = block[i];
             int before = 0;
-            for (int j = lane; j < n_blocks; j += 64) before += block[j] < block[i];
-            before = (int)wave_sum64((u64)before);
-            if (lane == 0) in_order[before] = i << 8 | (int)(block[i] & 0xff);
+#pragma unroll 8
+            for (int j = 0; j < n_blocks; ++j) before += block[j] < k;
+            in_order[before] = i << 8 | (int)(k & 0xff);
         }
     }
     // this wave's blocks
