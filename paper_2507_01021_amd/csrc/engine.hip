@@ -628,6 +628,12 @@ class EngineT final : public Engine {
                        float* out_logp) override {
         WMI_HIP(hipSetDevice(dev_));
         join_chains();
+        if (!draw_) {  // a context that never draws has no room for it
+            draw_logp_ = dalloc<float>(S_);
+            draw_ws_ = dalloc<unsigned char>(sample_ws_bytes(S_));
+            draw_ = dalloc<float>(5 * (size_t)S_);
+            WMI_HIP(hipDeviceSynchronize());
+        }
         if (!same_rows(slots, n)) put_rows(slots, n);
         std::vector<float> up((size_t)n * 5);
         for (int i = 0; i < n; ++i) {
@@ -1766,9 +1772,6 @@ class EngineT final : public Engine {
         stop_at_ = dalloc<int>(S);
         never_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 2);  // a word to spare: 64 bits are read at once
         first_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 2);
-        draw_ = dalloc<float>(5 * S);
-        draw_logp_ = dalloc<float>(S);
-        draw_ws_ = dalloc<unsigned char>(sample_ws_bytes(S_));
         xlist_ = list_;
         if (paged_) {
             pages_ = dalloc<T>((size_t)book_.free_pages() * 2 * Ld * H * (64 << PAGE_SHIFT));

@@ -15,9 +15,10 @@
 // the exponentials and, over 2047 bins of distance from the largest logit, the
 // ids (top-k) or the weights (top-p) of every bin, or without both filters the
 // weights' sums by position; sample_list_kernel the bin in which the first
-// filter cuts, and lists the ids up to it (some dozens to thousands).
-// sample_pick_kernel, a workgroup per row, settles the rest in that list, or if
-// they were too many, by further passes over the row.
+// filter cuts. For top-k it lists the ids up to that bin, for top-p alone those
+// in it, and adds up the weights of the ids before it by position.
+// sample_pick_kernel, a workgroup per row, settles the rest with the list, or
+// if that was too long, by further passes over the row.
 #pragma once
 
 #include "common.h"
@@ -62,7 +63,7 @@ constexpr int BLOCKS = 512, BLOCK = 64;        // a row's list: blocks of ids, e
 // What the first three kernels leave of a row for the last.
 struct RowWork {
     u64 bins[BINS];                       // by distance: ids, or weights
-    u64 sums[MAX_CHUNKS * CUT_WAVES];     // without top-k and top-p: a wave's kept weights
+    u64 sums[MAX_CHUNKS * CUT_WAVES];     // a wave's weights: without filters, or top-p's before the cut's bin
     double exps[MAX_CHUNKS * CUT_WAVES];  // sums of exp(l - l_max)
     float max[MAX_CHUNKS];
     int id[MAX_CHUNKS];                   // lowest id with that maximum
@@ -128,11 +129,13 @@ struct LogitRow {
             if (a.pos[slot] != a.n_prompt[slot] - 1) first = nullptr;
         }
     }
+    __device__ __forceinline__ int pieces() const { return (V + shift + EL - 1) / EL; }
+    __device__ __forceinline__ int per_wave(int waves) const { return ((pieces() + waves - 1) / waves + 63) / 64 * 64; }
     __device__ __forceinline__ void take(int wave, int waves) {
-        const int n = (V + shift + EL - 1) / EL, per = ((n + waves - 1) / waves + 63) / 64 * 64;
-        lo = min(n, wave * per);
-        hi = min(n, lo + per);
+        lo = min(pieces(), wave * per_wave(waves));
+        hi = min(pieces(), lo + per_wave(waves));
     }
+    __device__ __forceinline__ int wave_of(int id, int waves) const { return (id + shift) / EL / per_wave(waves); }
     // Piece v as loaded: its 16 bytes and the bits of ids that are left out.
     // Loads of pieces that are not wholly the row's go to a whole one instead,
     // so that a run of loads has no branches; unpack() then reads their ids one by one.
@@ -351,14 +354,15 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_sum_kernel(SampleA
 }
 
 // Bin of the first cut among the summed bins (every workgroup finds it by
-// itself), and the ids up to it: each wave lists its own in their order, in
-// blocks that it takes from the row's pool.
+// itself), and the ids up to it (top-k) or in it (top-p alone): each wave lists
+// its own in their order, in blocks that it takes from the row's pool.
 template <class T>
 __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(SampleArgs a) {
     using namespace smp;
     constexpr int PER = BINS / (64 * CUT_WAVES);
     __shared__ u64 red[CUT_WAVES];
     __shared__ u64 sh_need;
+    __shared__ double tab[256];
     __shared__ int sh_bin;
     const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int gw = blockIdx.x * CUT_WAVES + wave;
@@ -377,6 +381,7 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(Sample
     }
     u64 e = wave_scan64(run, lane);
     if (lane == 63) red[wave] = e;
+    fill_table(tab);
     if (tid == 0) {
         sh_bin = -1;
         sh_need = 0;
@@ -405,14 +410,24 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(Sample
         ws.bin = sh_bin;
         ws.need = sh_need;
     }
-    const int bin = sh_bin < 0 ? 2046 : sh_bin;  // a filter that keeps all: every id of some weight
-    const Scale sc(o, lmax, nullptr);
+    const int bin = sh_bin < 0 ? 2047 : sh_bin;  // 2047: a filter that keeps all ids of some weight
+    const bool by_weight = o.top_k <= 0;
+    const Scale sc(o, lmax, tab);
+    u64 sum = 0;
     int own = 0, last = 0;  // the wave's ids so far, the block it is filling
     row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
         unsigned in = 0;
 #pragma unroll
-        for (int x = 0; x < EL; ++x)
-            if (l[x] > -INFINITY && sc.bin(l[x]) <= bin) in |= 1u << x;
+        for (int x = 0; x < EL; ++x) {
+            const int b = sc.bin(l[x]);
+            if (b > bin || b == 2047) continue;
+            if (!by_weight || b == bin) {
+                in |= 1u << x;
+            } else {
+                const u64 w = sc.weigh(l[x]);
+                sum += w >= sc.least ? w : 0;
+            }
+        }
         if (!__any(in)) return;
         const int c = __popc(in);
         int before = c;
@@ -443,6 +458,10 @@ __global__ __launch_bounds__(64 * smp::CUT_WAVES) void sample_list_kernel(Sample
             ws.block[at] = (unsigned)gw << 24 | (unsigned)(q & 0xffff) << 8 | (unsigned)min(BLOCK, own - q * BLOCK);
         if (more) last = base + more - 1;
     });
+    if (by_weight) {
+        sum = wave_sum64(sum);
+        if (lane == 0) ws.sums[gw] = sum;
+    }
 }
 
 template <class T>
@@ -452,6 +471,7 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
     __shared__ u64 hw[BINS];
     __shared__ u64 lk[BIN_IDS], lw[BIN_IDS];
     __shared__ unsigned block[BLOCKS];
+    __shared__ u64 sums[MAX_CHUNKS * CUT_WAVES];
     __shared__ int in_order[BLOCKS];  // the list's blocks in the order of ids: number << 8 | ids
     __shared__ u64 red[WAVES];
     __shared__ double tab[256];
@@ -513,12 +533,14 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
     // top-p's (an id measures its weight); the first of them has its bin already.
     enum { BIN, RANK, DIGIT, SUM };
     int cut = o.top_k > 0 ? 0 : o.top_p < 1.f ? 1 : 2;
-    const bool summed = cut == 2;  // no filters: the sums are there
+    const bool none = cut == 2, by_weight = cut == 1;  // no filter, top-p alone
     int stage = BIN, digit = 0, shift = 52, nb = 0, bin = -1;
     u64 prefix = 0, sum = 0;
     const int n_blocks = ws.n_blocks;
-    const bool listed = !summed && n_blocks <= BLOCKS;
-    if (!summed) {
+    const bool listed = !none && n_blocks <= BLOCKS;
+    // the sums by position are there: all of them, or (top-p) but for the cut's bin
+    const bool summed = none || (by_weight && listed);
+    if (!none) {
         if (ws.bin >= 0) stage = RANK;
         else ++cut;  // it keeps all
         if (tid == 0) {
@@ -588,7 +610,7 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
         if (stage == BIN && cut == 0 && o.top_k <= 0) cut = 1;
         if (stage == BIN && cut == 1 && !(o.top_p < 1.f)) cut = 2;
         if (cut == 2) stage = SUM;
-        if (summed) break;
+        if (cut == 2 && summed) break;
         nb = digit < 2 ? 11 : 10;
         if (stage == DIGIT) shift -= nb;
         if (stage == BIN || stage == DIGIT)
@@ -676,16 +698,26 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
     // The place of u times the sum of the kept weights. The waves' sums, in the
     // order of their ids, say which wave's ids it is among.
     const int waves = summed ? cut_waves : WAVES;
-    if (!summed) {
+    if (summed) {
+        for (int i = tid; i < cut_waves; i += THREADS) sums[i] = ws.sums[i];
+        __syncthreads();
+        if (by_weight)  // and the kept ids of the cut's bin
+            each_listed([&](int i, float l) __attribute__((always_inline)) {
+                if (!(l > -INFINITY) || !kept(i, l)) return false;
+                const u64 w = sc.weigh(l);
+                if (w >= sc.least) atomicAdd(&sums[row.wave_of(i, cut_waves)], w);
+                return false;
+            });
+    } else {
         sum = wave_sum64(sum);
-        if (lane == 0) red[wave] = sum;
+        if (lane == 0) sums[wave] = sum;
     }
     __syncthreads();
     u64 part[PER], mine = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int w = PER * lane + k;
-        part[k] = w < waves ? summed ? ws.sums[w] : red[w] : 0;
+        part[k] = w < waves ? sums[w] : 0;
         mine += part[k];
     }
     u64 run = wave_scan64(mine, lane);
@@ -701,7 +733,7 @@ __global__ __launch_bounds__(smp::THREADS) void sample_pick_kernel(SampleArgs a)
         }
     owner = __shfl(owner, at_lane, 64);
     u64 before = __shfl(run, at_lane, 64);
-    if (listed) {
+    if (listed && !summed) {
         if (wave != owner) return;
         each_listed([&](int i, float l) __attribute__((always_inline)) {
             u64 w = l > -INFINITY && kept(i, l) ? sc.weigh(l) : 0;
