@@ -68,6 +68,7 @@ class PagedCacheT final : public PagedCache {
     void set_stream(void* s) override {
         if (dev_ == WHISPER_NO_DEVICE || s == st_) return;
         DeviceScope scope(dev_);
+        no_capture();
         WMI_HIP(hipStreamSynchronize(st_));
         st_ = static_cast<hipStream_t>(s);
     }
@@ -112,7 +113,8 @@ class PagedCacheT final : public PagedCache {
     void append(int layer, const void* k, const void* v, int64_t k_ld, int64_t v_ld) override {
         need_chunk();
         DeviceScope scope(dev_);
-        const int n = capturing(st_) ? max_tiles_ : n_tiles_;
+        // a recorded launch goes through whatever list is current at its replay in strides
+        const int n = capturing(st_) ? std::min(max_tiles_, ATTN_WGS) : n_tiles_;
         if (n == 0) return;
         move<true>(layer, plan_.dev, n, k, v, k_ld, v_ld, tokens_);
     }
@@ -183,6 +185,9 @@ class PagedCacheT final : public PagedCache {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the cache has no device");
         DeviceScope scope(dev_);
         no_capture();
+        long long rows = 0;
+        for (int i = 0; i < n; ++i) rows += book_.length(seqs[i]);
+        if (rows > INT32_MAX) throw ArgError(WHISPER_E_INVAL, "more than 2^31 - 1 positions to read at once");
         std::vector<int> t(HEAD_INTS);
         int row = 0;
         for (int i = 0; i < n; ++i) row = add_tiles(t, seqs[i], 0, book_.length(seqs[i]), row);

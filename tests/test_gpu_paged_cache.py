@@ -342,3 +342,40 @@ def test_state_errors():
     p.c.append(0, x, x)
     p.c.attend(0, x, x)
     p.check_rows([0])
+
+
+def test_offsets_beyond_32_bits():
+    """Pages behind the first 4 GiB of a cache's memory, in its last layer."""
+    H, D, P, layers = 8, 128, 256, 32
+    c = binding.Cache(binding.DTYPE_F32, layers, H, H, D, P, 100, 2, 90 * P, 90 * P)  # 67 MB a page
+    c.extend([0], [80 * P])  # pages 0 .. 79, 5.4 GB
+    n = 300
+    k, v, q = (torch.randn(n, H, D, device="cuda") for _ in range(3))
+    c.extend([1], [n])
+    out = torch.empty_like(q)
+    for layer in (0, layers - 1):
+        c.append(layer, k.data_ptr(), v.data_ptr())
+        c.attend(layer, q.data_ptr(), out.data_ptr())
+        torch.cuda.synchronize()
+        s = torch.matmul(q.double().transpose(0, 1), k.double().permute(1, 2, 0).contiguous()) * D ** -0.5
+        s += torch.full((n, n), -math.inf, device="cuda").double().triu(1)
+        ref = torch.matmul(torch.softmax(s, -1), v.double().transpose(0, 1).contiguous()).transpose(0, 1)
+        # rounding as in Pair.check, with |q . k| D ** -0.5 below 64 and |v| below 6
+        assert (out.double() - ref).abs().max() <= 6 * (4 * (D + 4) * 2.0 ** -24 * 64 + 2.0 ** -20 + 2 * n * 2.0 ** -24)
+    kb, vb = torch.empty_like(k), torch.empty_like(v)
+    c.read(layers - 1, [1], kb.data_ptr(), vb.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(kb, k) and torch.equal(vb, v)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_outputs_in_place_of_queries(dtype):
+    p = Pair(dtype, 8, 2, 64, 32, 3, 3000, seed=4)
+    p.add([0, 1, 2], [2600, 70, 0])
+    for counts in ([1, 5, 3], [40, 200, 1]):
+        p.add([0, 1, 2], counts)
+        q = p.rows(sum(counts), 8)[0]
+        x = q.clone()
+        p.c.attend(0, x.data_ptr(), x.data_ptr())
+        torch.cuda.synchronize()
+        p.check(x, q, [0, 1, 2], counts)

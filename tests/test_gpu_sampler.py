@@ -230,3 +230,44 @@ def test_recorded_choice():
         torch.cuda.synchronize()
         want, wl = run(x, un, opt, check=True)
         assert (tok.cpu().numpy() == want).all() and (lp.cpu().numpy() == wl).all()
+
+
+def test_more_rows_than_the_workspace_holds():
+    V, rows = 257, 1300
+    r = np.random.RandomState(12)
+    run(logits_like_a_model(rows, V, 12), r.rand(rows), dict(temperature=r.choice([0.0, 0.7, 1.0], rows), top_k=r.choice([0, 9], rows),
+                                                             top_p=r.choice([1.0, 0.8], rows)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_wide_nuclei_and_long_lists(dtype):
+    """Filters that keep tens of thousands of ids: more than the list of a row
+    holds, bins of thousands of equal logits, ids sorted by their logits."""
+    V = 120001
+    x = logits_like_a_model(8, V, 13, dtype, peak=1.0)
+    x[1] = x[1].sort(descending=True).values
+    x[2] = x[2].sort().values
+    x[3] = (x[3].float() * 2).round().to(dtype) / 2
+    x[4] = 0
+    x[5, : V // 2] = 3
+    u = np.random.RandomState(14).rand(8)
+    for opt in (dict(top_p=0.999), dict(top_p=0.5), dict(top_k=50000), dict(top_k=100000, top_p=0.9), dict(top_k=40000, top_p=0.99, min_p=1e-4),
+                dict(temperature=20.0, top_p=0.7), dict(temperature=0.3, top_k=60000), dict(top_p=0.9, min_p=0.5)):
+        run(x, u, opt)
+
+
+def test_other_stream():
+    x = logits_like_a_model(4, 5000, 15)
+    u = torch.rand(4, device="cuda")
+    s = binding.Sampler(5000, 4)
+    s.options(top_p=0.9)
+    toks = []
+    st = torch.cuda.Stream()
+    for handle in (None, st.cuda_stream, None):
+        s.set_stream(handle)
+        torch.cuda.synchronize()
+        t = torch.empty(4, dtype=torch.int32, device="cuda")
+        s.run(x.data_ptr(), 0, 4, u.data_ptr(), t.data_ptr())
+        torch.cuda.synchronize()
+        toks.append(t.tolist())
+    assert toks[0] == toks[1] == toks[2]
