@@ -105,8 +105,7 @@ class PagedCacheT final : public PagedCache {
         const size_t u0 = blob_.size(), c0 = u0 + upd.size();
         blob_.insert(blob_.end(), upd.begin(), upd.end());
         for (auto& c : copies) blob_.insert(blob_.end(), {c.src, c.dst});
-        put(plan_, blob_);
-        update_table(plan_.dev + u0, (int)upd.size() / 2);
+        put(plan_, blob_, u0, (int)upd.size() / 2);
         copy_pages(plan_.dev + c0, (int)copies.size());
     }
 
@@ -194,7 +193,7 @@ class PagedCacheT final : public PagedCache {
         if (row == 0) return;
         const ListHead head{0, 0, (int)(t.size() - HEAD_INTS) / 4, 0, HEAD_INTS, 0, 0, 0};
         memcpy(t.data(), &head, sizeof(head));
-        put(list_, t);
+        put(list_, t, 0, 0);
         move<false>(layer, list_.dev, head.tiles, k, v, k_ld, v_ld, row);
     }
 
@@ -250,9 +249,10 @@ class PagedCacheT final : public PagedCache {
         return PagedView{pages_, table_, book_.max_list(), shift_, P_.n_layer, P_.n_kv_head, head_elems_};
     }
 
-    // Copies a list to the device: as a kernel argument if it is short, else
-    // through pinned memory (a ring, so that the host rarely waits).
-    void put(DevList& d, const std::vector<int>& v) {
+    // Copies a list to the device, as a kernel argument if it is short, else
+    // through pinned memory (a ring, so that the host rarely waits), and makes
+    // the n changes of page lists that begin at upd.
+    void put(DevList& d, const std::vector<int>& v, size_t upd, int n) {
         if (&d == &plan_ && v.size() > d.cap) throw DeviceError("paged cache: a longer plan than planned for");
         if (v.size() > d.cap) {
             WMI_HIP(hipStreamSynchronize(st_));
@@ -265,13 +265,15 @@ class PagedCacheT final : public PagedCache {
             d.cap = cap;
         }
         if (v.size() <= 2 * PUT_INTS) {
+            const bool once = v.size() <= PUT_INTS;
             for (size_t i = 0; i < v.size(); i += PUT_INTS) {
                 PutInts a;
                 a.n = (int)std::min<size_t>(PUT_INTS, v.size() - i);
                 memcpy(a.v, v.data() + i, a.n * sizeof(int));
-                hipLaunchKernelGGL(put_ints_kernel, dim3(1), dim3(256), 0, st_, a, d.dev + i);
+                hipLaunchKernelGGL(put_ints_kernel, dim3(1), dim3(256), 0, st_, a, d.dev + i, (int)upd, once ? n : 0, table_);
             }
             WMI_HIP(hipGetLastError());
+            if (!once) update_table(d.dev + upd, n);
             return;
         }
         Stage& s = ring_[next_++ % 8];
@@ -288,6 +290,7 @@ class PagedCacheT final : public PagedCache {
         memcpy(s.host, v.data(), v.size() * sizeof(int));
         WMI_HIP(hipMemcpyAsync(d.dev, s.host, v.size() * sizeof(int), hipMemcpyHostToDevice, st_));
         WMI_HIP(hipEventRecord(s.ev, st_));
+        update_table(d.dev + upd, n);
     }
 
     void add_update(std::vector<int>& upd, int seq, int k, int page) const {
@@ -311,8 +314,7 @@ class PagedCacheT final : public PagedCache {
         for (auto& c : copies) v.insert(v.end(), {c.src, c.dst});
         if (v.empty()) return;
         DeviceScope scope(dev_);
-        put(list_, v);
-        update_table(list_.dev, (int)upd.size() / 2);
+        put(list_, v, 0, (int)upd.size() / 2);
         copy_pages(list_.dev + upd.size(), (int)copies.size());
     }
 

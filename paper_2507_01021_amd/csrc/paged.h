@@ -75,8 +75,12 @@ struct PutInts {
     int n;
     int v[PUT_INTS];
 };
-static __global__ __launch_bounds__(256) void put_ints_kernel(PutInts a, int* __restrict__ dst) {
+// The list's numbers upd .. upd + 2 n - 1 are changes of page lists as well
+// (table[first] = second), made at once.
+static __global__ __launch_bounds__(256) void put_ints_kernel(PutInts a, int* __restrict__ dst, int upd, int n,
+                                                              int* __restrict__ table) {
     for (int i = threadIdx.x; i < a.n; i += 256) dst[i] = a.v[i];
+    for (int i = threadIdx.x; i < n; i += 256) table[a.v[upd + 2 * i]] = a.v[upd + 2 * i + 1];
 }
 // table[at[2 i]] = at[2 i + 1]
 static __global__ __launch_bounds__(256) void table_update_kernel(const int* __restrict__ at, int n, int* __restrict__ table) {
