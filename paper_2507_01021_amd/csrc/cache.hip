@@ -37,7 +37,8 @@ class PagedCacheT final : public PagedCache {
         page_bytes_ = 2LL * p.n_layer * p.n_kv_head * head_elems_ * sizeof(T);
         while ((1 << shift_) < p.page_size) ++shift_;
         pages_ = dalloc<unsigned char>((size_t)p.n_pages * page_bytes_);
-        table_ = dalloc<int>((size_t)p.max_seqs * book_.max_list());
+        table_ = dalloc<int>((size_t)p.max_seqs * book_.max_list() + 1);
+        odd_ = table_ + (size_t)p.max_seqs * book_.max_list();  // (the pages are cleared: all finite)
         // room for the longest plan, so that recorded launches keep their addresses
         const long long T0 = p.max_tokens, S0 = p.max_seqs;
         max_tiles_ = (int)std::min(T0, T0 / 32 + 2 * S0);
@@ -214,7 +215,7 @@ class PagedCacheT final : public PagedCache {
     PageBook book_;
     hipStream_t st_ = nullptr;  // the device's default stream unless one was chosen
     unsigned char* pages_ = nullptr;
-    int* table_ = nullptr;
+    int *table_ = nullptr, *odd_ = nullptr;
     float* parts_ = nullptr;
     DevList plan_, list_;
     Stage ring_[8];
@@ -246,7 +247,7 @@ class PagedCacheT final : public PagedCache {
         if (!plan_ok_) throw ArgError(WHISPER_E_STATE, "no chunk: call whisper_cache_extend first");
     }
     PagedView view() const {
-        return PagedView{pages_, table_, book_.max_list(), shift_, P_.n_layer, P_.n_kv_head, head_elems_};
+        return PagedView{pages_, table_, book_.max_list(), shift_, P_.n_layer, P_.n_kv_head, head_elems_, odd_};
     }
 
     // Copies a list to the device, as a kernel argument if it is short, else

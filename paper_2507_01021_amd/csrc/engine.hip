@@ -589,7 +589,7 @@ class EngineT final : public Engine {
     }
     PagedView view() const {
         return PagedView{reinterpret_cast<unsigned char*>(pages_), table_, book_.max_list(), PAGE_SHIFT, Ld_, H_,
-                         (long long)(64 << PAGE_SHIFT)};
+                         (long long)(64 << PAGE_SHIFT), nullptr};
     }
 
     void fork_slot(int src, int pos, const int* dst, int n) override {

@@ -30,6 +30,11 @@ __host__ __device__ inline int val_off(int p, int c, int D) {
         return ((p >> 4) * (D >> 4) + (c >> 4)) * 256 + (((p >> 2) & 3) * 16 + (c & 15)) * 4 + (p & 3);
 }
 
+// An entry of a list that no running kernel writes, at an address that is the
+// same in all lanes: a scalar load, which does not queue behind vector loads.
+typedef const int __attribute__((address_space(4))) * ScalarList;
+__device__ __forceinline__ int list_at(const int* list, int i) { return ((ScalarList)(uintptr_t)list)[i]; }
+
 // The pages of a cache as a kernel sees them. table[seq * ld + i] is the
 // i-th page of a sequence.
 struct PagedView {
@@ -39,6 +44,10 @@ struct PagedView {
     int shift;             // log2 of the positions per page
     int n_layer, Hkv;
     long long head_elems;  // P * D
+    // 1 once a value that is not finite was appended: attention then takes care
+    // of 0 * inf at hidden positions. Null: it always does.
+    int* odd;
+    __device__ __forceinline__ bool may_be_odd() const { return !odd || list_at(odd, 0) != 0; }
     template <class T>
     __device__ T* head(int page, int layer, int kv, int h) const {
         return reinterpret_cast<T*>(pages) + (((long long)page * n_layer + layer) * 2 + kv) * Hkv * head_elems +
@@ -46,10 +55,17 @@ struct PagedView {
     }
 };
 
-// An entry of a list that no running kernel writes, at an address that is the
-// same in all lanes: a scalar load, which does not queue behind vector loads.
-typedef const int __attribute__((address_space(4))) * ScalarList;
-__device__ __forceinline__ int list_at(const int* list, int i) { return ((ScalarList)(uintptr_t)list)[i]; }
+// Whether a 16-byte piece has a number that is not finite (all exponent bits set).
+template <class T>
+__device__ __forceinline__ bool not_finite(u32x4 x) {
+    bool odd = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        odd = odd || (x[k] & 0x7f800000u) == 0x7f800000u;
+        if (sizeof(T) == 2) odd = odd || (x[k] & 0x7f80u) == 0x7f80u;
+    }
+    return odd;
+}
 
 // A run of up to 32 positions of one sequence inside one block of 32, and the
 // row of its first position in the caller's rows.
@@ -115,6 +131,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, const in
         T* vd = c.head<T>(page, layer, 1, h);
         const T* ks = k + blockIdx.z * k_layer + (long long)t.row * k_ld + h * D;
         const T* vs = v + blockIdx.z * v_layer + (long long)t.row * v_ld + h * D;
+        bool odd = false;
         for (int i = tid; i < t.n * CH; i += 256) {
             const int r = i / CH, ch = i - r * CH;
             if constexpr (VEC) {
@@ -122,13 +139,16 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, const in
                 const u32x4 b = *reinterpret_cast<const u32x4*>(vs + r * v_ld + ch * EL);
                 *reinterpret_cast<u32x4*>(kd + dec_off<T>(p0 + r, ch * EL, D)) = a;
                 *reinterpret_cast<u32x4*>(sv + ((p0 + r) & 31) * LD + ch * EL) = b;
+                odd = odd || not_finite<T>(b);
             } else {
                 for (int e = 0; e < EL; ++e) {
+                    odd = odd || !(fabsf(ldf(vs + r * v_ld + ch * EL + e)) < INFINITY);
                     kd[dec_off<T>(p0 + r, ch * EL + e, D)] = ks[r * k_ld + ch * EL + e];
                     sv[((p0 + r) & 31) * LD + ch * EL + e] = vs[r * v_ld + ch * EL + e];
                 }
             }
         }
+        if (c.odd && odd) *c.odd = 1;
         __syncthreads();
         // value pieces of the tile's block of 32 positions: EL positions of one dim each
         const int lo = p0 & 31, hi = lo + t.n;
@@ -295,9 +315,10 @@ template <> struct Piece<float> {
 //   weights as the B operand.
 // Scores, maxima, sums and outputs are fp32; the bf16 weights enter the product
 // rounded to bf16 (2^-9 of each weight at most), their sum does not.
-// Positions at or beyond kv1 may hold anything: their values are replaced by
-// zeros. A block some of whose positions only some rows see is multiplied row
-// by row if its values are not all finite, since 0 * inf is not 0.
+// Positions at or beyond kv1 may hold what was there before, and a block may
+// have positions that only some rows see: weights 0, and since 0 * inf is not
+// 0, values behind kv1 are replaced by zeros and such a block is multiplied row
+// by row if its values are not all finite (if any ever was not).
 template <class T, int D, bool FRAG>
 __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
     typedef typename Piece<T>::V V;
@@ -309,6 +330,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
     const AttnItem* items = reinterpret_cast<const AttnItem*>(a.plan + HEAD_INTS);
     const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool check = a.c.may_be_odd();
     for (int w0 = blockIdx.x; w0 < head.items * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const AttnItem t = items[it];
@@ -390,7 +412,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
             // position of element e of a value fragment
             auto vpos = [&](int b, int e) { return p + fc * 4 + (sizeof(T) == 2 ? (e & 3) + (e >> 2) * 16 : b * 16 + e); };
             bool by_row = false;
-            if (p + 32 > all) {
+            if (check && p + 32 > all) {
                 bool odd = false;
 #pragma unroll
                 for (int b = 0; b < NV; ++b)
@@ -568,6 +590,7 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
     const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pmask = (1 << a.c.shift) - 1;
+    const bool check = a.c.may_be_odd();
     for (int w0 = blockIdx.x; w0 < head.bigs * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const AttnItem t = items[it];
@@ -615,12 +638,12 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
             for (int i = 0; i < N; ++i) load_to_lds(src + i * 512, dst + i * 1024);
         };
         // One block of 64 positions from LDS. MASKED: not every row sees all of
-        // them. Values behind the range may be anything and count as 0, and so
-        // do values that are not finite: 0 * inf would reach rows that do not
-        // see them (what they are to the others is added at the end).
+        // them. ODD: values may be anything; behind the range they count as 0,
+        // and so do those that are not finite: 0 * inf would reach rows that do
+        // not see them (what they are to the others is added at the end).
         bool odd = false;
-        auto block = [&](auto is_masked, int p, const unsigned char* tk) __attribute__((always_inline)) {
-            constexpr bool MASKED = decltype(is_masked)::value;
+        auto block = [&](auto is_masked, auto is_odd, int p, const unsigned char* tk) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(is_masked)::value, ODD = decltype(is_odd)::value;
             const unsigned char* tv = tk + 2 * HALF;
             mfma_f32x4 sc[UT][4];
 #pragma unroll
@@ -685,7 +708,7 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     V vf = *reinterpret_cast<const V*>(tv + (s * ND + d) * 1024);
-                    if constexpr (MASKED) {
+                    if constexpr (ODD) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const bool in = s * 32 + (e & 3) + (e >> 2) * 16 < t.kv1 - p - fc * 4;
@@ -718,8 +741,9 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
             }
             const unsigned char* tk = lds + buf * TILE + lane * 16;
             buf = buf + 1 == NB ? 0 : buf + 1;
-            if (p + 64 <= all && p + 64 <= t.kv1) block(std::false_type{}, p, tk);
-            else if (p < end) block(std::true_type{}, p, tk);
+            if (p + 64 <= all && p + 64 <= t.kv1) block(std::false_type{}, std::false_type{}, p, tk);
+            else if (p < end && !check) block(std::true_type{}, std::false_type{}, p, tk);
+            else if (p < end) block(std::true_type{}, std::true_type{}, p, tk);
         }
         // values of masked blocks that are not finite: what they add to the rows
         // that see them, inf, -inf or NaN, by products of indicators
