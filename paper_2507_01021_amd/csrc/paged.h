@@ -498,40 +498,43 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
     }
 }
 
-// Joins the parts of cut ranges: one workgroup per 16 rows and kv head. Wave w
-// adds up parts w, w + 4, ..., its lane dims D/4 (lane % 4) .. of row lane / 4,
-// weighted by the largest maximum of all parts; the waves' sums are added in order.
+// Joins the parts of cut ranges: one workgroup per 16 rows and kv head. Four
+// lanes take a row of a part; where there are fewer than 16 rows the other
+// lanes take further parts, up to 64 at a time. Parts are weighted by the largest
+// maximum of all of them; the lanes' sums are added in order.
 template <class T, int D, bool FRAG>
 __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
     constexpr int N = D / 16;  // 16-byte pieces of a lane
-    __shared__ float so[3][16][D + 4];
-    __shared__ float sl[4][16], sm[4][16];
+    __shared__ float so[64][D + 4];
+    __shared__ float sl[64], sm[64];
     const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
     const MergeItem* merges = reinterpret_cast<const MergeItem*>(a.plan + head.merges_at);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane >> 2, q4 = lane & 3;
+    const int quad = threadIdx.x >> 2, q4 = threadIdx.x & 3;
     for (int w0 = blockIdx.x; w0 < head.merges * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const MergeItem t = merges[it];
-        const int j = t.j0 + row;
-        const bool live = j < t.count * a.G;
+        const int rows = min(16, t.count * a.G - t.j0);
+        const int lg = rows > 8 ? 4 : rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0;  // rows, rounded up to a power of two
+        const int row = quad & ((1 << lg) - 1), first = quad >> lg, stride = 64 >> lg;
+        const bool live = row < rows;
         const long long step = (long long)t.step * a.c.Hkv * (16 * (D + 2));
         const float* ps = a.parts + ((long long)t.part * a.c.Hkv + h) * (16 * (D + 2));
-        // the largest maximum: every lane takes every 16th part of its row
+        // the largest maximum: a quad's lanes take its parts in turn
         float m = -INFINITY;
-        for (int i = wave * 4 + q4; i < t.n; i += 16) m = fmaxf(m, live ? ps[i * step + 16 * D + row] : -INFINITY);
+        for (int i = first + q4 * stride; i < t.n; i += 4 * stride) m = fmaxf(m, live ? ps[i * step + 16 * D + row] : -INFINITY);
         m = fmaxf(m, __shfl_xor(m, 1, 64));
         m = fmaxf(m, __shfl_xor(m, 2, 64));
-        if (q4 == 0) sm[wave][row] = m;
+        if (q4 == 0) sm[quad] = m;
         __syncthreads();
-        m = fmaxf(fmaxf(sm[0][row], sm[1][row]), fmaxf(sm[2][row], sm[3][row]));
+        for (int i = row; i < 64; i += 1 << lg) m = fmaxf(m, sm[i]);
         const float mu = m == -INFINITY ? 0.f : m;
         float l = 0.f;
         mfma_f32x4 x[N];
 #pragma unroll
         for (int c = 0; c < N; ++c) x[c] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
         if (live) {
-#pragma unroll 4
-            for (int i = wave; i < t.n; i += 4) {
+#pragma unroll 2
+            for (int i = first; i < t.n; i += stride) {
                 const float* p = ps + i * step;
                 const float w = exp2_softmax(p[16 * D + row] - mu);
                 l += w * p[16 * D + 16 + row];
@@ -539,23 +542,21 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
                 for (int c = 0; c < N; ++c) x[c] += w * *reinterpret_cast<const mfma_f32x4*>(p + row * D + (c * 4 + q4) * 4);
             }
         }
-        if (q4 == 0) sl[wave][row] = l;
-        if (wave > 0) {
+        if (q4 == 0) sl[quad] = l;
 #pragma unroll
-            for (int c = 0; c < N; ++c) *reinterpret_cast<mfma_f32x4*>(&so[wave - 1][row][(c * 4 + q4) * 4]) = x[c];
-        }
+        for (int c = 0; c < N; ++c) *reinterpret_cast<mfma_f32x4*>(&so[quad][(c * 4 + q4) * 4]) = x[c];
         __syncthreads();
-        if (wave == 0 && live) {
-            l = sl[0][row] + sl[1][row] + sl[2][row] + sl[3][row];
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
-            const int tk = j / a.G, gg = j - tk * a.G;
-#pragma unroll
-            for (int c = 0; c < N; ++c) {
-                const int d = (c * 4 + q4) * 4;
-#pragma unroll
-                for (int w = 0; w < 3; ++w) x[c] += *reinterpret_cast<const mfma_f32x4*>(&so[w][row][d]);
-                attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d, x[c][0] * inv, x[c][1] * inv, x[c][2] * inv, x[c][3] * inv);
+        for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = (i - r * (D / 4)) * 4;
+            mfma_f32x4 y{0.f, 0.f, 0.f, 0.f};
+            float lt = 0.f;
+            for (int k = r; k < 64; k += 1 << lg) {
+                y += *reinterpret_cast<const mfma_f32x4*>(&so[k][d]);
+                lt += sl[k];
             }
+            const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+            const int j = t.j0 + r, tk = j / a.G, gg = j - tk * a.G;
+            attn_store<T, FRAG>(a, t.tok0 + tk, h * a.G + gg, D, d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
         }
         __syncthreads();  // the next item's LDS
     }
