@@ -13,13 +13,15 @@ namespace wmi {
 namespace {
 
 // Workgroups that an attention call is cut into when its rows alone give
-// fewer: four per CU.
+// fewer: four per CU (paged_attn_kernel has both sides' times).
 constexpr int ATTN_WGS = 1024;
 // Fewest positions of a cut range: two blocks of 32 per wave.
 constexpr int ATTN_PART = 512;
 // Rows of a sequence and key/value head from which the kernel of 128 rows per
 // workgroup takes them (bf16), the workgroups it is cut into where the rows
-// give fewer (one per CU), and the fewest positions of a part.
+// give fewer (one per CU), and the fewest positions of a part: with 1024, two
+// sequences of 100 tokens over 3000 positions, 32 / 8 heads of 128, took 45
+// instead of 35 us, one of 30 tokens with 8 query heads 28 instead of 19.
 constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
 
 template <class T>

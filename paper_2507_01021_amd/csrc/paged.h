@@ -110,7 +110,9 @@ static __global__ __launch_bounds__(256) void table_update_kernel(const int* __r
 // elements). One workgroup per (tile, kv head, layer) moves a tile's keys and
 // values through LDS, so that memory is accessed in 16-byte pieces on both
 // sides; a tile that does not cover a whole value piece writes single
-// elements. VEC: rows are 16-byte aligned.
+// elements. VEC: rows are 16-byte aligned. Bound by HBM: 2514 tokens, 12 heads of
+// 64, 12 layers in bf16 are written in 36 us (5.0 TB/s read and written); five
+// sequences of 229, 20 heads, 32 layers read out in 58 us (6.4 TB/s).
 template <class T, int D, bool VEC>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, const int* __restrict__ list, int layer0,
                                                            const T* __restrict__ k, const T* __restrict__ v,
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedView c, const int*
 }
 
 // Copies whole pages (all layers): pairs (source, destination), `bytes` each,
-// a multiple of 4096. Workgroups of a pair take 16 KiB each.
+// a multiple of 4096; five pages of 10.5 MB in 12.6 us (from L2 and the cache behind it). Workgroups of a pair take 16 KiB each.
 constexpr int PAGE_RUN = 16384;
 static __global__ __launch_bounds__(256) void paged_copy_kernel(unsigned char* __restrict__ pages,
                                                          const int* __restrict__ pairs, long long bytes) {
@@ -313,6 +315,12 @@ template <> struct Piece<float> {
 //   S^T[position][row] = K Q^T, running maximum and sum per row (a lane holds
 //   8 positions of one row), O^T[dim][row] += V^T P^T with the lane's own
 //   weights as the B operand.
+// Bound by the bytes of the cache where it is long (4 tokens over 60001
+// positions, 32 / 8 heads of 128 in bf16: 127 us, 5.0 TB/s), else by the chain of
+// loads plan - page - keys (32 tokens over 447 positions at most, 20 heads of
+// 64: 8.6 us for 40 MB). Parts are 512 positions at least: with 256 those 32
+// tokens took 14.5 us, the merge included; 2048 workgroups instead of 1024 took
+// 196 instead of 162 us for the long ones.
 // Scores, maxima, sums and outputs are fp32; the bf16 weights enter the product
 // rounded to bf16 (2^-9 of each weight at most), their sum does not.
 // Positions at or beyond kv1 may hold what was there before, and a block may
@@ -501,7 +509,9 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
 // Joins the parts of cut ranges: one workgroup per 16 rows and kv head. Four
 // lanes take a row of a part; where there are fewer than 16 rows the other
 // lanes take further parts, up to 64 at a time. Parts are weighted by the largest
-// maximum of all of them; the lanes' sums are added in order.
+// maximum of all of them; the lanes' sums are added in order. Bound by the
+// latency of reading what other workgroups wrote: 47 parts of 4 rows 7 us (29
+// with four parts at a time).
 template <class T, int D, bool FRAG>
 __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
     constexpr int N = D / 16;  // 16-byte pieces of a lane
@@ -569,6 +579,12 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
 // LDS access is a linear 16 bytes per lane. Two waves share a SIMD: the matrix
 // products of one run beside the other's softmax. A row's reference moves only
 // when a score is more than 2^8 above it, so the sums are rescaled rarely.
+// Bound by the matrix cores and the issue of the softmax beside them: 4096
+// tokens over 4097 positions, 32 / 8 heads of 128, 437 us (944 TFLOP/s; the 16-row
+// kernel 967). 256 rows per workgroup take 448 instead of 466 us there, but 51
+// instead of 34 for nine prompts of up to 513 tokens, which then give fewer
+// workgroups than CUs; 64 rows per wave at head size 128 leave one wave a SIMD
+// and took 1040.
 // An item's rows may be fewer than 128 (its waves and tiles without rows do
 // nothing but help loading) and its positions a part of a cut range; slot
 // part + i then holds the i-th 16 rows.

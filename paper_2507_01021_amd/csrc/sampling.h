@@ -19,6 +19,14 @@
 // in it, and adds up the weights of the ids before it by position.
 // sample_pick_kernel, a workgroup per row, settles the rest with the list, or
 // if that was too long, by further passes over the row.
+//
+// One row of 51865 fp32 logits: 16.5 us without filters, 27 with top-k 50, 32 with
+// top-p 0.9 (launches of 4, 6, 7 and 12 us, each a chain of dependent loads; one
+// workgroup that reads the row once per digit of a 52-bit key took 98 to 133).
+// 384 rows of 151937 bf16 logits (117 MB): 140 us without filters or with top-k,
+// 280 with top-p 0.9, of which the fp64 instructions of the weights (13 of about
+// 35 per id) are most. Weights from fp32 exponentials would be off by 2^-22: sums
+// of 50000 of them would then put one row in a hundred on the other side of a border.
 #pragma once
 
 #include "common.h"
