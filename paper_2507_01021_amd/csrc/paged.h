@@ -389,7 +389,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             const float mn = fmaxf(m, mx);
-            const float mu = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing yet
+            const float mu = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing, or only -inf
             if (__any(mn > m)) {
                 const float alpha = exp2_softmax(m - mu);
                 l *= alpha;
@@ -399,13 +399,16 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(AttnArgs a) {
                     for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
                 m = mn;
             }
+            {
+#pragma clang fp contract(off)  // mu is a rounded product, and so is what it is taken from
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    sc[b][r] = exp2_softmax(sc[b][r] - mu);
-                    l += sc[b][r];
-                }
+                    for (int r = 0; r < 4; ++r) {
+                        sc[b][r] = exp2_softmax(sc[b][r] - mu);
+                        l += sc[b][r];
+                    }
+            }
             V pf[NV];
             if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -574,13 +577,13 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
 
 // ------------------------------------------------------------------ attention of many rows (bf16)
 //
-// 128 rows per workgroup, 32 per wave in two tiles of 16, and blocks of 64 positions that all waves read from LDS: two or three buffers,
-// filled by direct global->LDS loads of whole 1 KiB fragments, so that every
+// 128 rows per workgroup, 32 per wave in two tiles of 16, and blocks of 64
+// positions that all waves read from LDS: two or three buffers, filled by direct global->LDS loads of whole 1 KiB fragments, so that every
 // LDS access is a linear 16 bytes per lane. Two waves share a SIMD: the matrix
 // products of one run beside the other's softmax. A row's reference moves only
 // when a score is more than 2^8 above it, so the sums are rescaled rarely.
 // Bound by the matrix cores and the issue of the softmax beside them: 4096
-// tokens over 4097 positions, 32 / 8 heads of 128, 437 us (944 TFLOP/s; the 16-row
+// tokens over 4097 positions, 32 / 8 heads of 128, 440 us (937 TFLOP/s; the 16-row
 // kernel 967). 256 rows per workgroup take 448 instead of 466 us there, but 51
 // instead of 34 for nine prompts of up to 513 tokens, which then give fewer
 // workgroups than CUs; 64 rows per wave at head size 128 leave one wave a SIMD
@@ -703,13 +706,23 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
 #pragma unroll
                         for (int r = 0; r < 4; ++r) o[d][u][r] *= alpha;
                 }
-                float mu = m[u];
-                if constexpr (MASKED) mu = mu == -INFINITY ? 0.f : mu;  // a row that has seen nothing yet
+                const float mu = m[u] == -INFINITY ? 0.f : m[u];  // a row that has seen nothing, or only -inf
+                // m is a rounded product: the exact one exceeds it by up to 2^-24 |m|,
+                // which is an exponent. Harmless below 2^30 (all of a row's weights
+                // have it alike); above, products are rounded before m is taken off.
+                float scale = a.scale;
+                if (__any(fabsf(mu) >= 0x1p30f)) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) cur[b][r] *= a.scale;
+                    scale = 1.f;
+                }
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        cur[b][r] = exp2_softmax(fmaf(cur[b][r], a.scale, -mu));
+                        cur[b][r] = exp2_softmax(fmaf(cur[b][r], scale, -mu));
                         l[u] += cur[b][r];
                     }
 #pragma unroll

@@ -381,3 +381,75 @@ def test_outputs_in_place_of_queries(dtype):
         p.c.attend(0, x.data_ptr(), x.data_ptr())
         torch.cuda.synchronize()
         p.check(x, q, [0, 1, 2], counts)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_of_minus_infinity_weigh_nothing(dtype, D):
+    """Keys that make a score -inf, or the type's lowest value, over whole blocks
+    in front of, between and behind the others."""
+    low = torch.finfo(DT[dtype][0]).min
+    for past, m in ((300, 1), (300, 5), (300, 200)):
+        p = Pair(dtype, 4, 2, D, 64, 1, 600)
+        k, v = p.rows(past + m), p.rows(past + m)
+        q = p.rows(m, 4)[0]
+        q[..., 0] = 1.0
+        gone = torch.zeros(past + m, dtype=torch.bool, device="cuda")
+        gone[:130] = True
+        gone[190:256] = True
+        gone[past + m // 2: past + m - 1: 2] = True
+        for value in (-math.inf, low):
+            kk = k.clone()
+            kk[0, gone, :, 0] = value
+            c = binding.Cache(DT[dtype][1], 1, 4, 2, D, 64, 20, 1, 600, 600)
+            c.extend([0], [past])
+            kp, vp = kk[:, :past].contiguous(), v[:, :past].contiguous()
+            c.append(0, kp.data_ptr(), vp.data_ptr())
+            torch.cuda.synchronize()
+            c.extend([0], [m])
+            kn, vn = kk[:, past:].contiguous(), v[:, past:].contiguous()
+            c.append(0, kn.data_ptr(), vn.data_ptr())
+            out = torch.empty_like(q)
+            c.attend(0, q.data_ptr(), out.data_ptr())
+            torch.cuda.synchronize()
+            keep = ~gone
+            for i in range(m):
+                at = keep[: past + i + 1].nonzero()[:, 0]
+                s = torch.einsum("hd,thd->ht", q[i].double().cpu(), k[0, at].double().cpu().repeat_interleave(2, 1)) * D ** -0.5
+                w = torch.softmax(s, -1)
+                x = v[0, at].double().cpu().repeat_interleave(2, 1)
+                ref = torch.einsum("ht,thd->hd", w, x)
+                mean = torch.einsum("ht,thd->hd", w, x.abs())
+                one = torch.finfo(p.t).eps / 2
+                # rounding as in Pair.check; |q| |k| D ** -0.5 summed over D stays below 64
+                rel = 4 * (D + 4) * 2.0 ** -24 * 64 + 2.0 ** -20 + 2 * 600 * 2.0 ** -24 + (one if p.t == torch.bfloat16 else 0)
+                err = (out[i].double().cpu() - ref).abs()
+                assert (err <= one * ref.abs() + rel * mean * (1 + one)).all(), (past, m, value, i)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 7, 200])
+def test_all_scores_the_lowest_value(dtype, D, m):
+    """Equal scores weigh alike, also where they are the type's lowest value."""
+    p = Pair(dtype, 4, 2, D, 64, 1, 600)
+    k, v = p.rows(300 + m), p.rows(300 + m)
+    k[..., 0] = torch.finfo(p.t).min
+    q = p.rows(m, 4)[0]
+    q[..., 0] = 1.0
+    for at, n in ((0, 300), (300, m)):
+        p.c.extend([0], [n])
+        kn, vn = k[:, at:at + n].contiguous(), v[:, at:at + n].contiguous()
+        p.c.append(0, kn.data_ptr(), vn.data_ptr())
+        torch.cuda.synchronize()
+    out = torch.empty_like(q)
+    p.c.attend(0, q.data_ptr(), out.data_ptr())
+    torch.cuda.synchronize()
+    x = v[0].double().cpu().repeat_interleave(2, 1)
+    one = torch.finfo(p.t).eps / 2
+    for i in range(m):
+        n = 301 + i
+        ref, mean = x[:n].mean(0), x[:n].abs().mean(0)
+        # weights of 1, summed over n positions in float32; the output is rounded
+        err = (out[i].double().cpu() - ref).abs()
+        assert (err <= one * ref.abs() + 2 * n * 2.0 ** -24 * mean * (1 + one)).all(), i
