@@ -643,7 +643,9 @@ class EngineT final : public Engine {
         }
         upload(1, draw_, up.data(), up.size() * sizeof(float));
         draw_rows_ = n;
+        prof_begin(WHISPER_K_DEC_STEP, st_);
         launch_rows(0, n, false, true, st_, 0);
+        prof_end(WHISPER_K_DEC_STEP, st_);
         draw_rows_ = 0;
         WMI_HIP(hipGetLastError());
         WMI_HIP(hipMemcpyAsync(out_tok, outtok_, n * sizeof(int), hipMemcpyDeviceToHost, st_));

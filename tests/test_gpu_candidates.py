@@ -225,6 +225,19 @@ def test_temperature_zero_is_the_greedy_step():
     assert got == want
 
 
+@pytest.mark.parametrize("paged", [0, 1])
+def test_drawn_steps_are_profiled(paged):
+    shape, W, blob = model("tiny")
+    segs = segments(shape, 8, 36, [3, 3])
+    with binding.Context(blob, max_slots=2, prefill=1, paged=paged) as ctx:
+        ctx.encode(segs, [0, 1])
+        ctx.profile_enable(binding.K_DEC_STEP, True)
+        for _ in range(3):
+            ctx.decode_sample([0, 1], [0.2, 0.9])
+        ms, n = ctx.profile_read(binding.K_DEC_STEP)
+        assert n == 3 and ms > 0
+
+
 def test_allocation_free_steps_of_forks():
     torch = pytest.importorskip("torch")
     shape, W, blob = model("base", n_enc=1, n_dec=2)
