@@ -562,10 +562,12 @@ whisper_status whisper_test_kernel_choice(int32_t choice_of, int32_t dtype, cons
  * Streams: the calls enqueue work on the cache's stream (at first the device's
  * default stream, see whisper_cache_set_stream) and return without waiting;
  * host arrays are read before a call returns, device memory when the work
- * runs (device pointers of a call that has no rows may be NULL). append and attend may be recorded into a graph, after an extend; each
- * replay takes the chunk that is current when it runs (k, v, q and out need a
- * row per token of it; a layer = -1 append as many tokens as at its
- * recording). The other calls refuse a recording stream (WHISPER_E_STATE).
+ * runs (device pointers of a call that has no rows may be NULL). append and
+ * attend may be recorded into a graph, after an extend; each replay takes the
+ * chunk that is current when it runs (k, v, q and out need a row per token of
+ * it; a layer = -1 append as many tokens as at its recording) and does nothing
+ * if there is none. The other calls that change the cache or enqueue work
+ * refuse a recording stream (WHISPER_E_STATE).
  * All calls on one cache, replays too, share its workspace: order them on one
  * stream.
  * Device: calls run on the cache's device and leave the current device as it

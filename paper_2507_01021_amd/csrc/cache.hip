@@ -23,6 +23,9 @@ constexpr int ATTN_PART = 512;
 // sequences of 100 tokens over 3000 positions, 32 / 8 heads of 128, took 45
 // instead of 35 us, one of 30 tokens with 8 query heads 28 instead of 19.
 constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
+// Most workgroups of a launch along its list (a grid holds fewer than 2^32
+// threads): the kernels go through longer lists in strides.
+constexpr int MOST_WGS = 1 << 22;
 
 template <class T>
 class PagedCacheT final : public PagedCache {
@@ -139,10 +142,20 @@ class PagedCacheT final : public PagedCache {
                 throw ArgError(WHISPER_E_INVAL, "sequence " + std::to_string(seqs[i]) + " holds " +
                                                     std::to_string(book_.length(seqs[i])) + " positions, fewer than " +
                                                     std::to_string(lengths[i]));
+        if (dev_ != WHISPER_NO_DEVICE) {
+            DeviceScope scope(dev_);
+            no_capture();
+        }
+        bool taken = false;
         for (int i = 0; i < n; ++i)
-            if (lengths[i] < book_.length(seqs[i]) && std::find(chunk_.begin(), chunk_.end(), seqs[i]) != chunk_.end())
-                plan_ok_ = false;
+            taken = taken || (lengths[i] < book_.length(seqs[i]) && std::find(chunk_.begin(), chunk_.end(), seqs[i]) != chunk_.end());
         book_.truncate(seqs, lengths, n);
+        if (!taken || !plan_ok_) return;
+        plan_ok_ = false;
+        if (dev_ == WHISPER_NO_DEVICE) return;
+        // a replay must find no rows: the pages may soon be another sequence's
+        DeviceScope scope(dev_);
+        put(plan_, std::vector<int>(HEAD_INTS, 0), 0, 0);
     }
 
     void fork(int src, const int* dst, int n) override {
@@ -410,7 +423,7 @@ class PagedCacheT final : public PagedCache {
     template <int D>
     void launch_attn(const AttnArgs& a, bool rec) {
         // a recorded launch may meet a longer list at its replay: the kernels go through it in strides
-        const unsigned ni = rec ? 2 * ATTN_WGS : (unsigned)n_items_ * P_.n_kv_head;
+        const unsigned ni = rec ? 2 * ATTN_WGS : std::min(n_items_ * P_.n_kv_head, MOST_WGS);
         const unsigned nm = rec ? ATTN_WGS : (unsigned)n_merges_ * P_.n_kv_head;
         if constexpr (sizeof(T) == 2) {
             const unsigned nb = rec ? (max_bigs() ? 2 * BIG_WGS : 0) : (unsigned)n_bigs_ * P_.n_kv_head;
@@ -435,7 +448,7 @@ class PagedCacheT final : public PagedCache {
         constexpr int EL = 16 / sizeof(T);
         const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0 && k_ld % EL == 0 &&
                          v_ld % EL == 0;
-        const dim3 grid(n, P_.n_kv_head, nl), block(256);
+        const dim3 grid(std::min(n, MOST_WGS), P_.n_kv_head, nl), block(256);
         if constexpr (IN) {
             const T *kk = static_cast<const T*>(k), *vv = static_cast<const T*>(v);
             if (vec) hipLaunchKernelGGL((paged_append_kernel<T, D, true>), grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);

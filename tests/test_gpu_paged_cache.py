@@ -453,3 +453,48 @@ def test_all_scores_the_lowest_value(dtype, D, m):
         # weights of 1, summed over n positions in float32; the output is rounded
         err = (out[i].double().cpu() - ref).abs()
         assert (err <= one * ref.abs() + 2 * n * 2.0 ** -24 * mean * (1 + one)).all(), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_replay_without_a_chunk(dtype):
+    """A truncate that ends the chunk also ends it for recorded launches: the
+    freed pages, which another sequence holds now, and the outputs stay."""
+    p = Pair(dtype, 4, 2, 64, 32, 2, 200)
+    p.add([0], [70])
+    k, v, q = p.rows(80), p.rows(80), p.rows(80, 4)[0]
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    p.c.set_stream(st.cuda_stream)
+    p.c.extend([0], [40])
+    p.c.append(0, k.data_ptr(), v.data_ptr())
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        p.c.append(0, k.data_ptr(), v.data_ptr())
+        p.c.attend(0, q.data_ptr(), out.data_ptr())
+        with pytest.raises(binding.WhisperError) as e:
+            p.c.truncate([0], [70])
+        assert e.value.status == binding.E_STATE
+    p.c.set_stream(0)
+    for _ in range(2):
+        with torch.cuda.stream(st):
+            g.replay()
+        torch.cuda.synchronize()
+        p.k[0], p.v[0] = torch.cat([p.k[0][:, :70], k[:, :40]], 1), torch.cat([p.v[0][:, :70], v[:, :40]], 1)
+        p.check(out, q, [0], [40])
+        p.cut([0], [0])
+        p.add([1], [70])  # from the freed pages
+        p.cut([1], [69])
+        before = out.clone()
+        k.add_(1)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, before)
+        p.check_rows([1])
+        p.cut([1], [0])
+        p.add([0], [70])
+        p.c.extend([0], [40])
+        torch.cuda.synchronize()
