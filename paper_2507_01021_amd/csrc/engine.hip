@@ -581,10 +581,15 @@ class EngineT final : public Engine {
         if (region_[s] >= 0) --region_used_[region_[s]];
         region_[s] = -1;
     }
+    // The slots' page lists, then their regions. Lists end in a page that no slot
+    // holds: a recorded step that is replayed beyond a slot's tokens writes there.
     void put_table() {
         const int ld = book_.max_list();
-        std::vector<int> t((size_t)S_ * ld, 0);
-        for (int s = 0; s < S_; ++s) std::copy(book_.pages(s).begin(), book_.pages(s).end(), t.begin() + (size_t)s * ld);
+        std::vector<int> t((size_t)S_ * (ld + 1), book_.n_pages());
+        for (int s = 0; s < S_; ++s) {
+            std::copy(book_.pages(s).begin(), book_.pages(s).end(), t.begin() + (size_t)s * ld);
+            t[(size_t)S_ * ld + s] = std::max(0, region_[s]);
+        }
         upload(5, table_, t.data(), t.size() * sizeof(int));
     }
     PagedView view() const {
@@ -868,10 +873,9 @@ class EngineT final : public Engine {
         int* list = reinterpret_cast<int*>(z + L.list);
         hipLaunchKernelGGL(put_list_kernel, dim3(1), dim3(WHISPER_NOALLOC_MAX_ROWS), 0, st_, rl, list);
         int* xlist = reinterpret_cast<int*>(z + L.xlist);
-        if (paged_) {
-            for (int i = 0; i < n; ++i) rl.slot[i] = region_[slots[i]];
-            hipLaunchKernelGGL(put_list_kernel, dim3(1), dim3(WHISPER_NOALLOC_MAX_ROWS), 0, st_, rl, xlist);
-        }
+        if (paged_)  // from device memory: a recorded step's slots may have other regions at its replay
+            hipLaunchKernelGGL(slot_regions_kernel, dim3(1), dim3(WHISPER_NOALLOC_MAX_ROWS), 0, st_, list, n,
+                               table_ + (size_t)S_ * book_.max_list(), xlist);
         const StepBufs b{RowBufs{list, xlist, nullptr, reinterpret_cast<float*>(z + L.dx), reinterpret_cast<T*>(z + L.dz),
                                  reinterpret_cast<T*>(z + L.dq), reinterpret_cast<T*>(z + L.datt),
                                  reinterpret_cast<T*>(z + L.dh), reinterpret_cast<int*>(z + L.rowlen),
@@ -1773,8 +1777,8 @@ class EngineT final : public Engine {
         first_mask_ = dalloc<unsigned>((size_t)V_ / 32 + 2);
         xlist_ = list_;
         if (paged_) {
-            pages_ = dalloc<T>((size_t)book_.free_pages() * 2 * Ld * H * (64 << PAGE_SHIFT));
-            table_ = dalloc<int>(S * book_.max_list());
+            pages_ = dalloc<T>((size_t)(book_.n_pages() + 1) * 2 * Ld * H * (64 << PAGE_SHIFT));
+            table_ = dalloc<int>(S * (book_.max_list() + 1));
             plan_ = dalloc<int>(MAXC * plan_ints(S_));
             xlist_ = dalloc<int>(S);
             forked_ = dalloc<int>(3 * S);

@@ -2495,6 +2495,12 @@ __global__ void seat_kernel(const int* __restrict__ slots, const int* __restrict
     }
 }
 
+// regions[i] = of[list[i]]
+__global__ void slot_regions_kernel(const int* __restrict__ list, int n, const int* __restrict__ of, int* __restrict__ regions) {
+    const int i = threadIdx.x;
+    if (i < n) regions[i] = of[list[i]];
+}
+
 // Makes slot dst[blockIdx.x] continue where slot src stands.
 __global__ void fork_slots_kernel(int src, const int* __restrict__ dst, int* __restrict__ seq, int* __restrict__ gen,
                                   int* __restrict__ pos, int* __restrict__ n_prompt, int* __restrict__ stop_at) {

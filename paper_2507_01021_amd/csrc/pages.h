@@ -31,6 +31,7 @@ class PageBook {
     int page_size() const { return P_; }
     int max_seqs() const { return (int)len_.size(); }
     int length(int s) const { return len_[s]; }
+    int n_pages() const { return (int)ref_.size(); }
     int free_pages() const { return (int)free_.size(); }
     const std::vector<int>& pages(int s) const { return pages_[s]; }
     int max_list() const { return pages_for(max_pos_); }

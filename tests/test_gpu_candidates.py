@@ -258,6 +258,42 @@ def test_allocation_free_steps_of_forks():
         assert np.array_equal(ctx.slot_tokens(0), want)
 
 
+def test_recorded_step_of_a_later_fork():
+    """A recorded allocation-free step, replayed when its slot has become the
+    fork of another and then past the tokens it reserved, reads the caches that
+    the slot has by then and leaves the other slots' pages alone."""
+    torch = pytest.importorskip("torch")
+    shape, W, blob = model("base", n_enc=1, n_dec=2)
+    a, b = segments(shape, 30, 40, [40, 40])
+    b.audio = a.audio[::-1].copy()
+    b.max_new_tokens = 1
+    with binding.Context(blob, max_slots=3, prefill=1, paged=1) as ctx:
+        want, other = (ctx.transcribe([s])[0]["tokens"] for s in (a, b))
+        st = torch.cuda.Stream()
+        ctx.set_stream(st.cuda_stream)
+        out = torch.full((1,), -7, dtype=torch.int32, device="cuda")
+        ctx.encode([a], [0])
+        ctx.encode([b], [1])
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            ctx.decode_step_noalloc([1], out.data_ptr())
+        g.replay()
+        torch.cuda.synchronize()
+        assert out.item() == other[0]
+        # slot 1 has its one token and is idle
+        ctx.fork(0, [1])
+        ctx.encode([b], [2])
+        for step in range(100):  # positions 39 .. 138: the fork holds 70, in two pages of 64
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            if step < 30:
+                assert out.item() == want[step], step
+        got = [ctx.decode_step([0])[0] for _ in range(30)]
+        assert np.array_equal(np.ravel(got), want)
+
+
 def test_best_of_five():
     """As a program uses them: a segment's prompt prefilled once, five
     candidates drawn, the likeliest kept; its log-probability is the oracle's."""
