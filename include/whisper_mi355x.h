@@ -286,7 +286,10 @@ whisper_status whisper_batch_decode_step(whisper_ctx* ctx, const int32_t* slots,
  * Every call on one GPU shares that GPU's array and leaves its contents
  * behind: calls whose work overlaps in time on one GPU (contexts on
  * different streams) race on it. A row without an admissible token is
- * reported by the next call that synchronises. Errors: E_INVAL, E_STATE
+ * reported by the next call that synchronises. A call recorded into a graph
+ * steps its slots whenever the graph is replayed; replays beyond a slot's
+ * max_new_tokens return tokens of no meaning and leave other slots alone.
+ * Errors: E_INVAL, E_STATE
  * (slot idle, or kernel timing on), E_CAPACITY (n above the maximum, or the
  * model's rows need more than the array; the message states the size).
  */

@@ -581,8 +581,10 @@ class EngineT final : public Engine {
         if (region_[s] >= 0) --region_used_[region_[s]];
         region_[s] = -1;
     }
-    // The slots' page lists, then their regions. Lists end in a page that no slot
-    // holds: a recorded step that is replayed beyond a slot's tokens writes there.
+    // The slots' page lists, then their regions. A list has an entry for every
+    // position of the text context, which no step leaves; those behind what a slot
+    // reserved are a page that no slot holds: a recorded step that is replayed
+    // beyond a slot's tokens writes there, or at the end of the slot's own pages.
     void put_table() {
         const int ld = book_.max_list();
         std::vector<int> t((size_t)S_ * (ld + 1), book_.n_pages());

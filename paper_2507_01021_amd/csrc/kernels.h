@@ -2343,7 +2343,8 @@ __host__ __device__ inline int key_token(unsigned long long k, int* bad) {
 
 // eot >= 0: the first time a slot's generated token is eot, stop_at[slot]
 // becomes the number of tokens generated before it. One wave per row over
-// its nk keys.
+// its nk keys. A recorded step may be replayed beyond the text context: a slot
+// stays at its last position, 447, and nothing behind its entries is written.
 __global__ __launch_bounds__(64) void argmax_step_kernel(const unsigned long long* __restrict__ keys, int nk,
                                                          const int* __restrict__ list, int* __restrict__ pos,
                                                          const int* __restrict__ n_prompt, int* __restrict__ seq,
@@ -2382,12 +2383,12 @@ __global__ __launch_bounds__(64) void argmax_step_kernel(const unsigned long lon
         const int g = p - (np - 1);
         if (eot >= 0 && tok == eot && stop_at[s] < 0) stop_at[s] = g;
         gen[s * 448 + g] = tok;
-        seq[s * 448 + p + 1] = forced ? forced[r] : tok;
+        if (p < 447) seq[s * 448 + p + 1] = forced ? forced[r] : tok;
         out_tok[r] = tok;
     } else {
         out_tok[r] = -1;
     }
-    pos[s] = p + 1;
+    pos[s] = min(p + 1, 447);
 }
 
 // Output head with the first stage of the greedy choice: the

@@ -356,3 +356,52 @@ def test_refusals():
         assert ctx.decode_step([0, 2])[1] == -1
     p = binding.params_from_blob(blob)
     assert p.paged == 0
+
+
+def record(torch, ctx, slots, out, steps=1):
+    """A stream for the context, and a graph of allocation-free steps on it."""
+    st = torch.cuda.Stream()
+    ctx.set_stream(st.cuda_stream)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        for _ in range(steps):
+            ctx.decode_step_noalloc(slots, out.data_ptr())
+    return st, g
+
+
+def replay(torch, g, n, out=None):
+    got = []
+    for _ in range(n):
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        if out is not None:
+            got.append(out.cpu().numpy().copy())
+    return got
+
+
+@pytest.mark.parametrize("paged", [0, 1])
+def test_replays_past_the_text_context(paged):
+    """A recorded step that is replayed beyond position 447 leaves the other
+    slots' tokens, prompts and caches alone: an idle neighbour's seated prompt,
+    a half-decoded neighbour's first positions, and what lies behind the last slot."""
+    torch = pytest.importorskip("torch")
+    shape, W, blob = model("base", n_enc=1, n_dec=2)
+    full = segments(shape, 444, 44, [4, 4, 4])
+    near = segments(shape, 30, 45, [6, 6])
+    out = torch.full((3,), -7, dtype=torch.int32, device="cuda")
+    with binding.Context(blob, max_slots=5, paged=paged) as ctx:
+        want = [r["tokens"] for r in ctx.transcribe(full + near)]
+        ctx.encode([full[0], near[0], full[1], near[1], full[2]], [0, 1, 2, 3, 4])
+        for _ in range(7):
+            ctx.decode_step([3])
+        st, g = record(torch, ctx, [0, 2, 4], out)
+        got = np.stack(replay(torch, g, 470, out))
+        assert (got[:3] == -1).all()
+        for k in range(3):
+            assert np.array_equal(got[3: 447, k], want[k])
+        tail = [ctx.decode_step([1])[0] for _ in range(35)][5:]
+        assert np.array_equal(tail, want[3])
+        tail = [ctx.decode_step([3])[0] for _ in range(28)]
+        assert np.array_equal(tail, want[4][2:])
