@@ -289,6 +289,8 @@ whisper_status whisper_batch_decode_step(whisper_ctx* ctx, const int32_t* slots,
  * reported by the next call that synchronises. A call recorded into a graph
  * steps its slots whenever the graph is replayed; replays beyond a slot's
  * max_new_tokens return tokens of no meaning and leave other slots alone.
+ * Which slots are idle and how many tokens whisper_slot_tokens returns goes by
+ * the calls (one, when it is recorded), not by the replays.
  * Errors: E_INVAL, E_STATE
  * (slot idle, or kernel timing on), E_CAPACITY (n above the maximum, or the
  * model's rows need more than the array; the message states the size).
@@ -339,8 +341,11 @@ whisper_status whisper_batch_decode_sample(whisper_ctx* ctx, const int32_t* slot
  * on their own (candidates of one segment, drawn apart by
  * whisper_batch_decode_sample). The cross-attention cache is shared, and so
  * are the self-attention cache's full pages; a partly filled page is copied.
- * n = 0 is a no-op. Errors: E_STATE (src idle, a destination active, the
- * context's params.paged is 0), E_INVAL, E_CAPACITY.
+ * Replays of recorded steps that were enqueued before on the context's stream
+ * count: the copies are made where src stands then, and what the calls had
+ * counted of it is set right. n = 0 is a no-op. Errors: E_STATE (src idle or
+ * with all its tokens, a destination active, the context's params.paged is 0),
+ * E_INVAL, E_CAPACITY.
  */
 whisper_status whisper_slot_fork(whisper_ctx* ctx, int32_t src, const int32_t* dst, int32_t n);
 

@@ -1,6 +1,7 @@
 // C ABI (include/whisper_mi355x.h): argument validation, slot bookkeeping,
 // error codes and messages, and the continuous-batching driver that ties the
 // batcher to the engine. Every check runs before any device work.
+#include <algorithm>
 #include <string.h>
 
 #include <chrono>
@@ -577,9 +578,18 @@ whisper_status whisper_slot_fork(whisper_ctx* ctx, int32_t src, const int32_t* d
             return fail(ctx, WHISPER_E_STATE, "slot " + std::to_string(dst[i]) + " is active");
     }
     return guarded(ctx, [&]() -> whisper_status {
-        ctx->eng->fork_slot(src, ctx->slots[src].steps, dst, n);
+        // replays of recorded steps are not counted here: the copy is cut where the
+        // slot stands on the device, and its counts are set to that
+        SlotState& s = ctx->slots[src];
+        s.steps = std::min(ctx->eng->position(src), s.n_prompt - 1 + s.max_new);
+        s.generated = std::max(0, s.steps - (s.n_prompt - 1));
+        if (s.generated == s.max_new) {
+            s.active = false;
+            return fail(ctx, WHISPER_E_STATE, "slot " + std::to_string(src) + " has all its tokens: it is idle");
+        }
+        ctx->eng->fork_slot(src, s.steps, dst, n);
         ctx->eng->sync();
-        for (int i = 0; i < n; ++i) ctx->slots[dst[i]] = ctx->slots[src];
+        for (int i = 0; i < n; ++i) ctx->slots[dst[i]] = s;
         return WHISPER_OK;
     });
 }

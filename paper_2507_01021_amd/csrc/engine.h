@@ -38,6 +38,9 @@ class Engine {
     // row (host), tokens and log-probabilities out (host, the latter or null).
     virtual void decode_sample(const int* slots, int n, const whisper_sampling* options, const float* uniforms,
                                int* out_tok, float* out_logp) = 0;
+    // The position of a slot's next input on the device, which replays of
+    // recorded steps move on by themselves (waits for the context's work).
+    virtual int position(int slot) = 0;
     // Paged caches: makes the n slots dst copies of slot src, whose next input
     // is at position pos; enqueued on the context's stream.
     virtual void fork_slot(int src, int pos, const int* dst, int n) = 0;

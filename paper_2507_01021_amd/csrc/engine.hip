@@ -599,6 +599,15 @@ class EngineT final : public Engine {
                          (long long)(64 << PAGE_SHIFT), nullptr};
     }
 
+    int position(int slot) override {
+        join_chains();
+        WMI_HIP(hipSetDevice(dev_));
+        int p = 0;
+        WMI_HIP(hipMemcpyAsync(&p, pos_ + slot, sizeof(int), hipMemcpyDeviceToHost, st_));
+        WMI_HIP(hipStreamSynchronize(st_));
+        return p;
+    }
+
     void fork_slot(int src, int pos, const int* dst, int n) override {
         if (!paged_) throw ArgError(WHISPER_E_STATE, "forking needs a context with paged caches");
         join_chains();

@@ -405,3 +405,54 @@ def test_replays_past_the_text_context(paged):
         assert np.array_equal(tail, want[3])
         tail = [ctx.decode_step([3])[0] for _ in range(28)]
         assert np.array_equal(tail, want[4][2:])
+
+
+@pytest.mark.parametrize("name", ["tiny", "base"])
+def test_fork_of_a_slot_that_replays_moved_on(name):
+    """Replays move a slot on the device alone: a fork is made where the slot
+    stands there, and the calls' counts follow."""
+    torch = pytest.importorskip("torch")
+    shape, W, blob = model(name, n_enc=1, n_dec=2)
+    seg = segments(shape, 150, 42, [5])[0]
+    out = torch.full((1,), -7, dtype=torch.int32, device="cuda")
+    with binding.Context(blob, max_slots=4, prefill=1, paged=1) as ctx:
+        want = ctx.transcribe([seg])[0]["tokens"]
+        other = segments(shape, 140, 43, [300])[0]
+        for _ in range(2):  # pages that hold something else's keys
+            ctx.encode([other] * 4, [0, 1, 2, 3])
+            for _ in range(140):
+                ctx.decode_step([0, 1, 2, 3])
+        ctx.encode([seg], [0])
+        st, g = record(torch, ctx, [0], out)
+        got = replay(torch, g, 81, out)
+        assert np.array_equal(np.ravel(got), want[:81])
+        ctx.fork(0, [1, 3])
+        for s in (0, 1, 3):
+            assert np.array_equal(ctx.slot_tokens(s), want[:81])
+        rest = [ctx.decode_step([3, 0, 1]) for _ in range(69)]
+        assert (np.stack(rest) == want[81:, None]).all()
+        for s in (0, 1, 3):  # all 150: idle
+            assert np.array_equal(ctx.slot_tokens(s), want)
+            with pytest.raises(binding.WhisperError) as e:
+                ctx.decode_step([s])
+            assert e.value.status == binding.E_STATE
+        # recorded steps that never ran: the device is where the encode left it
+        ctx.encode([seg], [0])
+        st, g = record(torch, ctx, [0], out, steps=70)
+        ctx.fork(0, [2])
+        assert ctx.slot_tokens(0).size == 0 and ctx.slot_tokens(2).size == 0
+        rest = [ctx.decode_step([2, 0]) for _ in range(150)]
+        assert (np.stack(rest) == want[:, None]).all()
+        # inside the prompt, and past the last token
+        ctx.encode([seg], [1])
+        st, g = record(torch, ctx, [1], out)
+        replay(torch, g, 150)
+        with pytest.raises(binding.WhisperError) as e:
+            ctx.fork(1, [3])
+        assert e.value.status == binding.E_STATE
+    with binding.Context(blob, max_slots=2, paged=1) as ctx:
+        ctx.encode([seg], [0])
+        st, g = record(torch, ctx, [0], out)
+        assert [int(x[0]) for x in replay(torch, g, 3, out)] == [-1, -1, -1]
+        ctx.fork(0, [1])
+        assert [ctx.decode_step([0, 1]).tolist() for _ in range(3)] == [[-1, -1], [want[0]] * 2, [want[1]] * 2]
