@@ -641,7 +641,7 @@ whisper_status whisper_cache_extend(whisper_cache* cache, const int32_t* seqs, c
  * Writes the chunk's keys and values of one layer: device rows k and v
  * [tokens][n_kv_head][head_size], row strides in elements (0: rows without
  * gaps). layer -1: all layers, k and v [n_layer][tokens] rows. Errors:
- * E_INVAL, E_STATE (no chunk).
+ * E_INVAL, E_STATE (no chunk, or a sequence of it was forked).
  */
 whisper_status whisper_cache_append(whisper_cache* cache, int32_t layer, const void* k, const void* v, int64_t k_stride,
                                     int64_t v_stride);
@@ -665,8 +665,12 @@ whisper_status whisper_cache_attend(whisper_cache* cache, int32_t layer, const v
 whisper_status whisper_cache_truncate(whisper_cache* cache, const int32_t* seqs, const int32_t* lengths, int32_t n);
 
 /* Makes the n empty sequences dst copies of sequence src: full pages are
- * shared, a partly filled last page is copied. Errors: E_INVAL, E_STATE (a
- * destination is not empty), E_CAPACITY (no such sequence, too few free pages). */
+ * shared, a partly filled last page is copied. If src has new positions in the
+ * current chunk, the copies hold what was appended to them so far, and the
+ * chunk's rows can be attended to but not appended any more (appends return
+ * E_STATE, recorded ones do nothing when replayed) until the next extend.
+ * Errors: E_INVAL, E_STATE (a destination is not empty), E_CAPACITY (no such
+ * sequence, too few free pages). */
 whisper_status whisper_cache_fork(whisper_cache* cache, int32_t src, const int32_t* dst, int32_t n);
 
 /* Moves the pages in use to the front of the cache's memory. */

@@ -97,7 +97,8 @@ class PagedCacheT final : public PagedCache {
         book_.extend(seqs, counts, n, copies);
         tokens_ = total;
         chunk_.assign(seqs, seqs + n);
-        plan_ok_ = true;
+        counts_.assign(counts, counts + n);
+        plan_ok_ = append_ok_ = true;
         if (dev_ == WHISPER_NO_DEVICE) return;
         DeviceScope scope(dev_);
         // the plan, the changed entries of the page lists and the page copies in one list
@@ -117,6 +118,8 @@ class PagedCacheT final : public PagedCache {
 
     void append(int layer, const void* k, const void* v, int64_t k_ld, int64_t v_ld) override {
         need_chunk();
+        if (!append_ok_)
+            throw ArgError(WHISPER_E_STATE, "a sequence of the chunk was forked: its rows cannot be written any more");
         DeviceScope scope(dev_);
         // a recorded launch goes through whatever list is current at its replay in strides
         const int n = capturing(st_) ? std::min(max_tiles_, ATTN_WGS) : n_tiles_;
@@ -175,6 +178,18 @@ class PagedCacheT final : public PagedCache {
             for (int k = 0; k < (int)pg.size(); ++k) add_update(upd, dst[i], k, pg[k]);
         }
         apply(upd, copies);
+        // pages of the chunk's new positions are shared now, or were copied as they
+        // were: nothing more is written there, by replays either
+        bool open = false;
+        for (size_t i = 0; i < chunk_.size(); ++i) open = open || (chunk_[i] == src && counts_[i] > 0);
+        if (n == 0 || !open || !plan_ok_ || !append_ok_) return;
+        append_ok_ = false;
+        DeviceScope scope(dev_);
+        ListHead head = head_;
+        head.tiles = 0;
+        std::vector<int> h(HEAD_INTS);
+        memcpy(h.data(), &head, sizeof(head));
+        put(plan_, h, 0, 0);
     }
 
     void compact() override {
@@ -236,8 +251,10 @@ class PagedCacheT final : public PagedCache {
     Stage ring_[8];
     int next_ = 0;
     // the chunk: its sequences, new tokens and the lengths of its lists
-    std::vector<int> chunk_, blob_;
-    bool plan_ok_ = false;
+    std::vector<int> chunk_, counts_, blob_;
+    ListHead head_{};
+    bool plan_ok_ = false;    // there is a chunk
+    bool append_ok_ = false;  // none of its sequences was forked since
     int tokens_ = 0, n_items_ = 0, n_bigs_ = 0, n_merges_ = 0, n_tiles_ = 0;
     int max_tiles_ = 0;
 
@@ -416,8 +433,8 @@ class PagedCacheT final : public PagedCache {
         const size_t ma = add(merges.data(), merges.size() * (sizeof(MergeItem) / sizeof(int)));
         const size_t ta = add(tiles.data(), tiles.size());
         const size_t ba = add(bigs.data(), bigs.size() * (sizeof(AttnItem) / sizeof(int)));
-        const ListHead head{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, 0};
-        memcpy(blob_.data(), &head, sizeof(head));
+        head_ = ListHead{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, 0};
+        memcpy(blob_.data(), &head_, sizeof(head_));
     }
 
     template <int D>

@@ -1,9 +1,9 @@
 // C ABI (include/whisper_mi355x.h): argument validation, slot bookkeeping,
 // error codes and messages, and the continuous-batching driver that ties the
 // batcher to the engine. Every check runs before any device work.
-#include <algorithm>
 #include <string.h>
 
+#include <algorithm>
 #include <chrono>
 #include <memory>
 #include <thread>

@@ -498,3 +498,78 @@ def test_replay_without_a_chunk(dtype):
         p.add([0], [70])
         p.c.extend([0], [40])
         torch.cuda.synchronize()
+
+
+def recorded(p, st, *calls):
+    """The calls in a graph on stream st, which the cache gets."""
+    torch.cuda.synchronize()
+    p.c.set_stream(st.cuda_stream)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        for f in calls:
+            f()
+    return g
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("past,m", [(0, 64), (10, 70), (64, 1), (70, 130)])
+def test_fork_inside_a_chunk_ends_its_appends(dtype, past, m):
+    """A fork shares the chunk's pages: whatever is appended afterwards, by a call
+    or by a recorded launch, may not reach them. Attention goes on."""
+    p = Pair(dtype, 4, 2, 64, 64, 4, 300, seed=past + m)
+    p.add([0, 2], [past, 5])
+    p.c.extend([0, 2], [m, 3])
+    k, v, q = p.rows(m + 3), p.rows(m + 3), p.rows(m + 3, 4)[0]
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    p.c.append(-1, k.data_ptr(), v.data_ptr())
+    for s, lo, hi in ((0, 0, m), (2, m, m + 3)):
+        p.k[s], p.v[s] = torch.cat([p.k[s], k[:, lo:hi]], 1), torch.cat([p.v[s], v[:, lo:hi]], 1)
+    st = torch.cuda.Stream()
+    kk, vv = k + 1, v + 1
+    g = recorded(p, st, lambda: p.c.append(-1, kk.data_ptr(), vv.data_ptr()), lambda: p.c.attend(0, q.data_ptr(), out.data_ptr()))
+    p.c.fork(0, [1, 3])
+    for s in (1, 3):
+        p.k[s], p.v[s] = p.k[0], p.v[0]
+    with pytest.raises(binding.WhisperError) as e:
+        p.c.append(-1, kk.data_ptr(), vv.data_ptr())
+    assert e.value.status == binding.E_STATE
+    for _ in range(2):
+        out.fill_(7)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            g.replay()
+        torch.cuda.synchronize()
+        p.check(out, q, [0, 2], [m, 3])
+        p.check_rows([0, 1, 2, 3])
+    p.attend([0, 2], [m, 3], q=q)
+    p.add([3, 0, 1], [1, 2, 1])  # the next chunk may be appended again
+    p.attend([3, 0, 1], [1, 2, 1])
+    p.check_rows([0, 1, 2, 3])
+
+
+def test_fork_before_the_append():
+    """A copied page would miss the rows that are still to come: such a chunk
+    can no longer be appended. A fork of a sequence without new positions leaves it."""
+    p = Pair("bf16", 4, 2, 64, 64, 4, 300)
+    p.add([0, 1], [40, 40])
+    k, v = p.rows(70), p.rows(70)
+    p.c.extend([1, 0], [0, 70])
+    p.c.fork(1, [2])  # (listed, without new positions)
+    p.k[2], p.v[2] = p.k[1], p.v[1]
+    p.c.append(-1, k.data_ptr(), v.data_ptr())
+    p.k[0], p.v[0] = torch.cat([p.k[0], k], 1), torch.cat([p.v[0], v], 1)
+    p.check_rows([0, 1, 2])
+    p.c.extend([0], [30])
+    p.c.fork(0, [])  # no copy
+    p.c.append(-1, k.data_ptr(), v.data_ptr())
+    p.k[0], p.v[0] = torch.cat([p.k[0], k[:, :30]], 1), torch.cat([p.v[0], v[:, :30]], 1)
+    p.check_rows([0])
+    p.c.extend([0], [7])
+    p.c.fork(0, [3])
+    with pytest.raises(binding.WhisperError) as e:
+        p.c.append(-1, k.data_ptr(), v.data_ptr())
+    assert e.value.status == binding.E_STATE
+    p.c.truncate([0, 3], [140, 140])
+    p.k[3], p.v[3] = p.k[0], p.v[0]
+    p.check_rows([0, 3])
