@@ -456,3 +456,26 @@ def test_fork_of_a_slot_that_replays_moved_on(name):
         assert [int(x[0]) for x in replay(torch, g, 3, out)] == [-1, -1, -1]
         ctx.fork(0, [1])
         assert [ctx.decode_step([0, 1]).tolist() for _ in range(3)] == [[-1, -1], [want[0]] * 2, [want[1]] * 2]
+
+
+def drawn_steps(ctx, slots, n, seed):
+    r = np.random.RandomState(seed)
+    return [ctx.decode_sample(slots, r.rand(len(slots)), temperature=1.0, top_p=0.95) for _ in range(n)]
+
+
+@pytest.mark.parametrize("paged", [0, 1])
+def test_drawn_tokens_are_the_slots_tokens(paged):
+    """slot_tokens returns what the drawn steps returned, and the next step's
+    input is the drawn token."""
+    shape, W, blob = model("tiny", n_enc=1, n_dec=2)
+    segs = segments(shape, 10, 41)
+    with binding.Context(blob, max_slots=8, paged=paged, prefill=1) as ctx:
+        ctx.encode(segs, [0, 1, 2, 3])
+        drawn = [t for t, _ in drawn_steps(ctx, [0, 1, 2, 3], 9, 5)]
+        ctx.encode(segs, [4, 5, 6, 7])
+        for t in drawn:
+            ctx.decode_step([4, 5, 6, 7], forced=t)
+        last, logits = ctx.decode_step([0, 1, 2, 3, 4, 5, 6, 7], logits=True)
+        assert np.array_equal(logits[:4], logits[4:])
+        for k in range(4):
+            assert np.array_equal(ctx.slot_tokens(k), [t[k] for t in drawn] + [last[k]])
