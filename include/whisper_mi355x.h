@@ -593,8 +593,11 @@ typedef struct whisper_cache whisper_cache;
 
 /*
  *   dtype          WHISPER_DTYPE_*: type of keys, values, queries and outputs;
- *                  sums, maxima and softmax weights are fp32 (bf16: weights
- *                  enter the product with the values rounded to bf16)
+ *                  sums, maxima and softmax weights are fp32. In bf16 a weight
+ *                  enters the product with the values as two bf16 numbers
+ *                  (2^-16 of it is lost at most), or, if a sequence has 128 or
+ *                  more new tokens times query heads of a kv head, rounded to
+ *                  one (2^-8)
  *   n_layer        1..256
  *   n_head         query heads, 1..256
  *   n_kv_head      key/value heads, a divisor of n_head: query head h reads

@@ -573,3 +573,71 @@ def test_fork_before_the_append():
     p.c.truncate([0, 3], [140, 140])
     p.k[3], p.v[3] = p.k[0], p.v[0]
     p.check_rows([0, 3])
+
+
+@pytest.mark.parametrize("H,Hkv,D", HEADS)
+def test_few_rows_keep_their_weights(H, Hkv, D):
+    """bf16 caches: rows that the kernel of few rows takes lose nothing of their
+    softmax weights but what fp32 sums lose; the output alone is rounded to bf16."""
+    G = H // Hkv
+    p = Pair("bf16", H, Hkv, D, 64, 4, 2500, seed=D + H)
+    p.add([0, 1, 2, 3], [0, 63, 700, 2100])
+    for m in (1, 5):
+        counts = [m] * 4
+        p.add([0, 1, 2, 3], counts)
+        q = p.rows(4 * m, H)[0] * 1.5
+        out = torch.empty_like(q)
+        torch.cuda.synchronize()
+        p.c.attend(0, q.data_ptr(), out.data_ptr())
+        torch.cuda.synchronize()
+        for s in range(4):
+            k, v = (x[s][0].double().repeat_interleave(G, 1).transpose(0, 1) for x in (p.k, p.v))
+            e = k.shape[1]
+            qs = q[s * m: s * m + m].double().transpose(0, 1)
+            hidden = torch.arange(e, device="cuda")[None] > torch.arange(e - m, e, device="cuda")[:, None]
+            sc = (torch.matmul(qs, k.transpose(1, 2).contiguous()) * D ** -0.5).masked_fill(hidden, -math.inf)
+            w = torch.softmax(sc, -1)
+            ref, mean = torch.matmul(w, v), torch.matmul(w, v.abs())
+            # a score: D products and sums in fp32; a weight: the hardware exponential 2^-21, and as two
+            # bf16 numbers 2^-8 of 2^-8; sums over the positions in fp32 (Pair.check), the output rounded once
+            es = (D + 4) * 2.0 ** -24 * D ** -0.5 * torch.matmul(qs.abs(), k.abs().transpose(1, 2).contiguous()).amax()
+            rel = 4 * es + 2.0 ** -20 + 2 * e * 2.0 ** -24 + 2.0 ** -16
+            err = (out[s * m: s * m + m].double().transpose(0, 1) - ref).abs()
+            tol = 2.0 ** -8 * ref.abs() + rel * mean * (1 + 2.0 ** -8) + 1e-30
+            assert (err <= tol).all(), (s, m, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 5, 200])
+def test_infinite_values_in_sight(dtype, D, m):
+    """An infinite value makes its dim infinite in the rows that see it, with its
+    sign, two of different signs make it no number; other dims and rows go on."""
+    p = Pair(dtype, 4, 2, D, 32, 1, 700, seed=m)
+    past = 300
+    k, v = p.rows(past + m), p.rows(past + m)
+    k *= 0.25  # weights of one size: none of them vanishes
+    v[0, 40, 0, 3] = math.inf
+    v[0, 131, 1, 7] = -math.inf
+    v[0, 140, 1, 9], v[0, 250, 1, 9] = math.inf, -math.inf
+    late = past + m // 2
+    v[0, late, 0, 11] = -math.inf
+    q = p.rows(m, 4)[0]
+    for a, b in ((0, past), (past, past + m)):
+        p.add([0], [b - a], k[:, a:b].contiguous(), v[:, a:b].contiguous())
+    out = torch.empty_like(q)
+    p.c.attend(0, q.data_ptr(), out.data_ptr())
+    torch.cuda.synchronize()
+    x = out.float()
+    assert (x[:, :2, 3] == math.inf).all() and (x[:, 2:, 7] == -math.inf).all() and x[:, 2:, 9].isnan().all()
+    assert (x[m // 2:, :2, 11] == -math.inf).all() and x[: m // 2, :2, 11].isfinite().all()
+    keep = torch.ones(4, D, dtype=torch.bool, device="cuda")
+    keep[:2, 3] = keep[2:, 7] = keep[2:, 9] = keep[:2, 11] = False
+    assert x[:, keep].isfinite().all()
+    p.v[0] = torch.where(p.v[0].float().isfinite(), p.v[0], torch.zeros_like(p.v[0]))
+    p.c.truncate([0], [0])
+    p.k[0], p.v[0], kk, vv = p.k[0][:, :0], p.v[0][:, :0], p.k[0].contiguous(), p.v[0].contiguous()
+    for a, b in ((0, past), (past, past + m)):
+        p.add([0], [b - a], kk[:, a:b].contiguous(), vv[:, a:b].contiguous())
+    zero = p.attend([0], [m], q=q)
+    p.check(torch.where(keep, out, zero), q, [0], [m])
