@@ -698,8 +698,8 @@ whisper_status whisper_cache_info(whisper_cache* cache, int32_t seq, int32_t* le
  * are taken as integers of 2^-43 of the largest, so a row's token depends on
  * nothing but its logits, its options and u.
  * Streams, device, threads: as for whisper_cache; whisper_sampler_run may be
- * recorded into a graph and takes the options that are set when it runs
- * (except that suppress lists stay on or off as they were).
+ * recorded into a graph and takes the options and suppressed ids that are set
+ * when it runs.
  */
 typedef struct whisper_sampler whisper_sampler;
 

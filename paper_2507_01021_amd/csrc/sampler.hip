@@ -29,6 +29,8 @@ class SamplerImpl final : public Sampler {
         ws_ = static_cast<unsigned char*>(q) + head;
         host_.assign(R_, SampleRow{1.f, 0, 1.f, 0.f});
         WMI_HIP(hipMemcpy(rows_, host_.data(), R_ * sizeof(SampleRow), hipMemcpyHostToDevice));
+        const std::vector<unsigned> none(words, 0u);
+        WMI_HIP(hipMemcpy(never_, none.data(), words * sizeof(unsigned), hipMemcpyHostToDevice));
     }
     ~SamplerImpl() override {
         if (dev_ == WHISPER_NO_DEVICE) return;
@@ -66,9 +68,9 @@ class SamplerImpl final : public Sampler {
     void run(const void* logits, int dtype, int n_rows, int64_t ld, const float* u, int32_t* tok, float* logp) override {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the sampler has no device");
         DeviceScope scope(dev_);
-        const SampleArgs a{logits, ld, V_, rows_, use_never_ ? never_ : nullptr, u, tok, logp, nullptr, nullptr, nullptr, nullptr, nullptr, ws_, 0};
-        // a recorded run may meet other options at its replay
-        const bool filters = filters_ || capturing(st_);
+        // a recorded run may meet other options and other suppressed ids at its replay
+        const bool rec = capturing(st_), filters = filters_ || rec;
+        const SampleArgs a{logits, ld, V_, rows_, use_never_ || rec ? never_ : nullptr, u, tok, logp, nullptr, nullptr, nullptr, nullptr, nullptr, ws_, 0};
         if (dtype == WHISPER_DTYPE_BF16) sample_rows<bf16>(a, n_rows, filters, st_);
         else sample_rows<float>(a, n_rows, filters, st_);
         WMI_HIP(hipGetLastError());

@@ -271,3 +271,32 @@ def test_other_stream():
         torch.cuda.synchronize()
         toks.append(t.tolist())
     assert toks[0] == toks[1] == toks[2]
+
+
+def test_suppress_lists_set_after_the_recording():
+    """A recorded run takes the ids suppressed when it is replayed, whether or
+    not there were any when it was recorded."""
+    V, rows = 5003, 4
+    s = binding.Sampler(V, rows)
+    st = torch.cuda.Stream()
+    s.set_stream(st.cuda_stream)
+    x = logits_like_a_model(rows, V, 21)
+    un = np.array([0.1, 0.4, 0.7, 0.95])
+    u = torch.from_numpy(un.astype(np.float32)).cuda()
+    tok = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    lp = torch.zeros(rows, device="cuda")
+    torch.cuda.synchronize()
+    best = [int(i) for i in x.argmax(1)]
+    for before in ((), best):
+        s.options(top_p=0.9, suppress=before)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            s.run(x.data_ptr(), 0, rows, u.data_ptr(), tok.data_ptr(), lp.data_ptr())
+        for sup in ((), best, (), range(2500, V), before):
+            s.options(top_p=0.9, suppress=list(sup))
+            with torch.cuda.stream(st):
+                g.replay()
+            torch.cuda.synchronize()
+            want, wl = run(x, un, dict(top_p=0.9), suppress=list(sup))
+            assert not set(tok.tolist()) & set(sup)
+            assert (tok.cpu().numpy() == want).all() and (lp.cpu().numpy() == wl).all(), len(sup)
