@@ -220,13 +220,17 @@ __device__ __forceinline__ float exp_neg(float x) {
 
 // What the options and the largest logit make of a logit.
 struct Scale {
-    float lmax, per_bin;
-    double top, per;  // the largest logit; log2 of a weight per logit
-    u64 least;        // min_p
+    float lmax;
+    float unit, per_bin;  // of a distance from lmax
+    double top, per;      // the largest logit; log2 of a weight per logit
+    u64 least;            // min_p
     const double* tab;
     __device__ __forceinline__ Scale(const SampleRow& o, float m, const double* t) : lmax(m), top(m), tab(t) {
         per = 1.4426950408889634074 / (double)o.temperature;
-        per_bin = 2047.f / 45.f * (float)per;
+        // distances that have a weight may exceed fp32 at the highest temperatures, and
+        // bins per logit at the lowest (where a logit that exceeds it then has no weight)
+        unit = per < 0x1p-100 ? 0.5f : per > 0x1p100 ? 0x1p64f : 1.f;
+        per_bin = 2047.f / 45.f * (float)(per / unit);
         least = (u64)ceil((double)o.min_p * ONE);
     }
     // weight of an admissible logit (0 for -inf); the largest, +inf too: 2^43
@@ -235,7 +239,9 @@ struct Scale {
         return weight(((double)l - top) * per, tab);
     }
     // bin by distance, as wide as 45 T ln 2 / 2047; 2047: weight 0
-    __device__ __forceinline__ int bin(float l) const { return l == lmax ? 0 : (int)fminf((lmax - l) * per_bin, 2047.f); }
+    __device__ __forceinline__ int bin(float l) const {
+        return l == lmax ? 0 : (int)fminf(fabsf(fmaf(-l, unit, lmax * unit)) * per_bin, 2047.f);
+    }
 };
 __device__ __forceinline__ void fill_table(double* tab) {
     if (threadIdx.x < 256) tab[threadIdx.x] = exp2((double)threadIdx.x / 256.0);

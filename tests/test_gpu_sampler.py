@@ -300,3 +300,36 @@ def test_suppress_lists_set_after_the_recording():
             want, wl = run(x, un, dict(top_p=0.9), suppress=list(sup))
             assert not set(tok.tolist()) & set(sup)
             assert (tok.cpu().numpy() == want).all() and (lp.cpu().numpy() == wl).all(), len(sup)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_temperatures_at_the_ends_of_the_range(dtype):
+    """Logits as far apart as the type allows at the highest temperatures (their
+    difference exceeds fp32, their weights do not vanish), and denormal ones at
+    the lowest: the filters count every id that has a weight. (A log-probability
+    below fp32's range, of a logit 6.6e38 below the largest, is rounded to -inf.)"""
+    def check_ends(x, u, opt):
+        tok, lp = run(x, u, opt, check=False)
+        o = {n: float(np.float32(opt.get(n, d))) for n, d in (("temperature", 1.0), ("top_p", 1.0), ("min_p", 0.0))}
+        for i, l in enumerate(x.double().cpu().numpy()):
+            t, want = choose(l, float(np.float32(u[i])), o["temperature"], opt.get("top_k", 0), o["top_p"], o["min_p"])
+            assert tok[i] == t, (i, int(tok[i]), t, opt)
+            with np.errstate(over="ignore"):
+                w = np.float32(want)
+            # as in run(): rounded once, a sum of fp32 exponentials
+            assert lp[i] == w or abs(float(lp[i]) - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -22 + 100 * 2.0 ** -24, (i, lp[i], want)
+
+    V = 200
+    g = torch.Generator(device="cuda")
+    g.manual_seed(17)
+    big = ((torch.rand(6, V, generator=g, device="cuda") * 2 - 1) * 3.3e38).to(dtype)
+    big[0, ::2], big[0, 1::2] = 3.3e38, -3.3e38
+    u = np.linspace(0.02, 0.98, 6)
+    filters = (dict(), dict(top_k=150), dict(top_p=0.9), dict(top_k=180, top_p=0.97), dict(top_p=0.99, min_p=0.2))
+    for t in (3.4e38, 1e38, 2e37):
+        for f in filters:
+            check_ends(big, u, dict(temperature=t, **f))
+    tiny = (torch.randint(-400, 400, (6, V), generator=g, device="cuda").double() * 2.0 ** -133).float().to(dtype)
+    for t in (200 * 2.0 ** -133, 20 * 2.0 ** -133, 2.0 ** -149):
+        for f in filters:
+            check_ends(tiny, u, dict(temperature=t, **f))
