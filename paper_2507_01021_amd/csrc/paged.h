@@ -787,10 +787,12 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
         int page = page_of(t.kv0 + AHEAD);  // of the block that is issued next
         for (int p = t.kv0; p < t.kv1; p += 64) {
             // this block is in LDS (the later ones' loads may be on their way), and
-            // every wave is done with the one before
+            // every wave is done with the one before; no read moves across
+            __builtin_amdgcn_sched_barrier(0);
             if (NB == 3 && p + 64 < t.kv1) __builtin_amdgcn_s_waitcnt(WMI_VMCNT_LDS(N));
             else __builtin_amdgcn_s_waitcnt(WMI_VMCNT_LDS(0));
             __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
             if (p + AHEAD < t.kv1) {
                 issue(p + AHEAD, page, buf == 0 ? NB - 1 : buf - 1);
                 page = page_of(p + 64 + AHEAD);

@@ -102,3 +102,15 @@ def test_analysis_sees_an_unwaited_read():
     assert unwaited(two) == {4} and not unwaited(two, 1)
     del two[2]
     assert unwaited(two, 1) == {12}
+
+
+def test_paged_barriers_are_fenced():
+    """Nothing else keeps the compiler from moving an LDS read from behind a bare
+    barrier to before it, where its buffer is still being filled."""
+    with open(os.path.join(os.path.dirname(binding.__file__), "csrc", "paged.h")) as f:
+        lines = [x.strip() for x in f]
+    at = [i for i, x in enumerate(lines) if "__builtin_amdgcn_s_barrier()" in x]
+    assert at
+    for i in at:
+        assert "__builtin_amdgcn_sched_barrier(0)" in lines[i + 1], i + 1
+        assert any("__builtin_amdgcn_sched_barrier(0)" in x for x in lines[i - 4: i]), i + 1
