@@ -329,7 +329,8 @@ typedef struct {
  *                 at temperature 1 among all ids the filters leave (the sum of
  *                 these ranks candidates), 0 inside the prompt
  * With temperature 0 in every row the tokens are whisper_batch_decode_step's.
- * n = 0 is a no-op. Errors: E_INVAL, E_STATE (slot idle).
+ * n = 0 is a no-op. Errors: E_INVAL, E_STATE (slot idle, or the context's
+ * stream is recording a graph).
  */
 whisper_status whisper_batch_decode_sample(whisper_ctx* ctx, const int32_t* slots, int32_t n,
                                            const whisper_sampling* options, const float* uniforms, int32_t* out_tokens,
@@ -344,8 +345,8 @@ whisper_status whisper_batch_decode_sample(whisper_ctx* ctx, const int32_t* slot
  * Replays of recorded steps that were enqueued before on the context's stream
  * count: the copies are made where src stands then, and what the calls had
  * counted of it is set right. n = 0 is a no-op. Errors: E_STATE (src idle or
- * with all its tokens, a destination active, the context's params.paged is 0),
- * E_INVAL, E_CAPACITY.
+ * with all its tokens, a destination active, the context's params.paged is 0,
+ * the context's stream is recording a graph), E_INVAL, E_CAPACITY.
  */
 whisper_status whisper_slot_fork(whisper_ctx* ctx, int32_t src, const int32_t* dst, int32_t n);
 

@@ -39,6 +39,7 @@
 #include <string>
 #include <vector>
 
+#include "device.h"
 #include "engine.h"
 #include "kernels.h"
 #include "pages.h"
@@ -599,9 +600,16 @@ class EngineT final : public Engine {
                          (long long)(64 << PAGE_SHIFT), nullptr};
     }
 
+    // Calls that wait for the device would end a recording of the context's stream.
+    void no_capture() const {
+        if (capturing(st_))
+            throw ArgError(WHISPER_E_STATE, "the stream is recording a graph: only the allocation-free step may be recorded");
+    }
+
     int position(int slot) override {
-        join_chains();
         WMI_HIP(hipSetDevice(dev_));
+        no_capture();
+        join_chains();
         int p = 0;
         WMI_HIP(hipMemcpyAsync(&p, pos_ + slot, sizeof(int), hipMemcpyDeviceToHost, st_));
         WMI_HIP(hipStreamSynchronize(st_));
@@ -643,6 +651,7 @@ class EngineT final : public Engine {
     void decode_sample(const int* slots, int n, const whisper_sampling* options, const float* uniforms, int* out_tok,
                        float* out_logp) override {
         WMI_HIP(hipSetDevice(dev_));
+        no_capture();
         join_chains();
         if (!draw_) {  // a context that never draws has no room for it
             draw_logp_ = dalloc<float>(S_);

@@ -479,3 +479,29 @@ def test_drawn_tokens_are_the_slots_tokens(paged):
         assert np.array_equal(logits[:4], logits[4:])
         for k in range(4):
             assert np.array_equal(ctx.slot_tokens(k), [t[k] for t in drawn] + [last[k]])
+
+
+def test_draws_and_forks_refuse_a_recording_stream():
+    """They wait for the device, which would end the recording: refused, and the
+    recording, the context and its slots go on."""
+    torch = pytest.importorskip("torch")
+    shape, W, blob = model("tiny", n_enc=1, n_dec=2)
+    seg = segments(shape, 6, 46, [4])[0]
+    out = torch.full((1,), -7, dtype=torch.int32, device="cuda")
+    with binding.Context(blob, max_slots=3, prefill=1, paged=1) as ctx:
+        want = ctx.transcribe([seg])[0]["tokens"]
+        ctx.encode([seg, seg], [0, 1])
+        st = torch.cuda.Stream()
+        ctx.set_stream(st.cuda_stream)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            ctx.decode_step_noalloc([0], out.data_ptr())
+            for f in (lambda: ctx.decode_sample([1], [0.5]), lambda: ctx.fork(1, [2])):
+                with pytest.raises(binding.WhisperError) as e:
+                    f()
+                assert e.value.status == binding.E_STATE
+        got = replay(torch, g, 2, out)
+        assert np.array_equal(np.ravel(got), want[:2])
+        ctx.fork(0, [2])
+        assert ctx.decode_sample([2, 1], [0.5, 0.5], temperature=0.0)[0].tolist() == [want[2], want[0]]
