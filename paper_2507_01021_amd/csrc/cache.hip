@@ -15,13 +15,24 @@ namespace {
 // Workgroups that an attention call is cut into when its rows alone give
 // fewer: four per CU (paged_attn_kernel has both sides' times).
 constexpr int ATTN_WGS = 1024;
-// Fewest positions of a cut range: two blocks of 32 per wave.
+// Longest range that is never cut: four blocks of 32 positions per wave. Longer
+// ones give equal parts of 384 positions or more, and a last one of what is left.
 constexpr int ATTN_PART = 512;
 // Rows of a sequence and key/value head from which the kernel of 128 rows per
 // workgroup takes them (bf16), the workgroups it is cut into where the rows
-// give fewer (one per CU), and the fewest positions of a part: with 1024, two
-// sequences of 100 tokens over 3000 positions, 32 / 8 heads of 128, took 45
+// give fewer (one per CU), and the longest range that it never cuts: with 1024,
+// two sequences of 100 tokens over 3000 positions, 32 / 8 heads of 128, took 45
 // instead of 35 us, one of 30 tokens with 8 query heads 28 instead of 19.
+// us of the 16-row kernel and of this one, 20 heads of 64, per rows of a sequence:
+//                              32         64          96        128        256
+//    1 sequence  over  200   4.5  8.3   5.2  9.8   5.1 10.0   5.4 11.3   6.4 13.7
+//    1           over 4000    14   16    15   18    19   19    19   19    30   26
+//    9 sequences over  200   5.2  8.3   6.6 10.0  10.9 10.3  12.7 11.9  25.5 17.6
+//    9           over 1000    21   21    26   23    35   25    43   27   106   36
+//   32           over 1000    52   38   102   36   152   45   206   47   430   84
+// Rows alone do not say which is faster. From 128 on, the 16-row kernel would save
+// some 7 us where it is faster (few sequences, short contexts) and lose several
+// times the time where it is not; below, it loses with many sequences too.
 constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
 // Most workgroups of a launch along its list (a grid holds fewer than 2^32
 // threads): the kernels go through longer lists in strides.
@@ -368,7 +379,8 @@ class PagedCacheT final : public PagedCache {
 
     // The chunk's lists: header, attention items, merges, append tiles.
     // Ranges of positions are cut where the rows alone give fewer workgroups
-    // than ATTN_WGS, into parts of equal length, ATTN_PART at least.
+    // than ATTN_WGS, if they are longer than ATTN_PART, into parts of equal length
+    // but for the last.
     void build_plan(const int* seqs, const int* counts, int n) {
         std::vector<AttnItem> items, cut;
         std::vector<MergeItem> merges;

@@ -111,8 +111,10 @@ static __global__ __launch_bounds__(256) void table_update_kernel(const int* __r
 // values through LDS, so that memory is accessed in 16-byte pieces on both
 // sides; a tile that does not cover a whole value piece writes single
 // elements. VEC: rows are 16-byte aligned. Bound by HBM: 2514 tokens, 12 heads of
-// 64, 12 layers in bf16 are written in 36 us (5.0 TB/s read and written); five
-// sequences of 229, 20 heads, 32 layers read out in 58 us (6.4 TB/s).
+// 64, 12 layers in bf16 are written in 36 us (5.1 TB/s read and written); five
+// sequences of 229, 20 heads, 32 layers read out in 57 us (6.6 TB/s, three pages
+// of four being shared). A single appended token's values are 2-byte stores 16
+// bytes apart: 32 tokens, 20 heads of 64 take 28 us for 32 layers at once, 5 for one.
 template <class T, int D, bool VEC>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, const int* __restrict__ list, int layer0,
                                                            const T* __restrict__ k, const T* __restrict__ v,
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedView c, const int*
 }
 
 // Copies whole pages (all layers): pairs (source, destination), `bytes` each,
-// a multiple of 4096; five pages of 10.5 MB in 12.6 us (from L2 and the cache behind it). Workgroups of a pair take 16 KiB each.
+// a multiple of 4096; five pages of 10.5 MB in 12.8 us (from L2 and the cache behind it). Workgroups of a pair take 16 KiB each.
 constexpr int PAGE_RUN = 16384;
 static __global__ __launch_bounds__(256) void paged_copy_kernel(unsigned char* __restrict__ pages,
                                                          const int* __restrict__ pairs, long long bytes) {
@@ -316,15 +318,15 @@ template <> struct Piece<float> {
 //   8 positions of one row), O^T[dim][row] += V^T P^T with the lane's own
 //   weights as the B operand.
 // Bound by the bytes of the cache where it is long (4 tokens over 60001
-// positions, 32 / 8 heads of 128 in bf16: 127 us, 5.0 TB/s), else by the chain of
-// loads plan - page - keys (32 tokens over 447 positions at most, 20 heads of
-// 64: 8.6 us for 40 MB). Parts are 512 positions at least: with 256 those 32
-// tokens took 14.5 us, the merge included; 2048 workgroups instead of 1024 took
-// 196 instead of 162 us for the long ones.
+// positions at most, 32 / 8 heads of 128 in bf16, 733 MB: 128 us, 5.7 TB/s), else
+// by the chain of loads plan - page - keys (32 tokens over 447 positions at most,
+// 20 heads of 64: 8.7 us for 40 MB). Ranges of up to 512 positions are not cut:
+// cut from 256 on, those 32 tokens took 14.5 us, the merge included; 2048
+// workgroups instead of 1024 took 196 instead of 162 us for the long ones.
 // Scores, maxima, sums and outputs are fp32; a weight enters the product with
 // bf16 values as the sum of two bf16 numbers, which leaves 2^-16 of it at most
 // (rounded to one it would lose 2^-8): 9.7 instead of 9.6 us for the 32 tokens,
-// 133 for the long ones either way.
+// 133 for the long ones either way, 3 % on average for 4 to 96 rows a sequence.
 // Positions at or beyond kv1 may hold what was there before, and a block may
 // have positions that only some rows see: weights 0, and since 0 * inf is not
 // 0, values behind kv1 are replaced by zeros and such a block is multiplied row
@@ -607,10 +609,12 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
 // Scores, maxima, sums and outputs are fp32; the weights enter the product with
 // the values rounded to bf16 (2^-8 of each at most), their sum does not. As two
 // bf16 numbers, as above, they would take half as many products again: 569 instead
-// of 435 us for the 4096 tokens below, 39 instead of 30 for the nine prompts.
-// Bound by the matrix cores and the issue of the softmax beside them: 4096
-// tokens over 4097 positions, 32 / 8 heads of 128, 440 us (937 TFLOP/s; the 16-row
-// kernel 967). 256 rows per workgroup take 448 instead of 466 us there, but 51
+// of 436 us for the 4096 tokens below, 39 instead of 30 for the nine prompts.
+// Bound by the matrix cores, the issue of the softmax beside them and LDS reads
+// (a fragment serves two products): 4096 tokens over 4097 positions, 32 / 8 heads
+// of 128, 436 us (946 TFLOP/s; the 16-row kernel 967 us) at full clocks, up to 540
+// in the first launches after a pause. Few prompts are bound by a workgroup's
+// chain of blocks: 4.6 us and 1.15 per block, alone on its CU. 256 rows per workgroup take 448 instead of 466 us there, but 51
 // instead of 34 for nine prompts of up to 513 tokens, which then give fewer
 // workgroups than CUs; 64 rows per wave at head size 128 leave one wave a SIMD
 // and took 1040.
