@@ -320,7 +320,8 @@ class PagedCacheT final : public PagedCache {
             if (!once) update_table(d.dev + upd, n);
             return;
         }
-        Stage& s = ring_[next_++ % 8];
+        Stage& s = ring_[next_];
+        next_ = (next_ + 1) % 8;
         if (s.ev) WMI_HIP(hipEventSynchronize(s.ev));
         else WMI_HIP(hipEventCreateWithFlags(&s.ev, hipEventDisableTiming));
         if (v.size() > s.cap) {
