@@ -619,6 +619,30 @@ typedef struct {
  * E_DEVICE; whisper_cache_error(NULL) then holds the message. */
 whisper_status whisper_cache_create(const whisper_cache_params* params, int device, whisper_cache** out);
 
+/*
+ * A cache whose keys and values are kept in `bits` bits each: 8 or 4 (0:
+ * whisper_cache_create). All calls are those of other caches; append quantises,
+ * read returns what the cache stands for, and attention is that of these values.
+ * 64 numbers of a row, from a multiple of 64 on, form a group. With lo and hi
+ * their least and largest, 0 included (hi - lo is taken in fp32),
+ *   step = the smallest number with 4 (8 bits: 1) significant bits that is at
+ *          least (hi - lo) / 15 (8 bits: 255), and at least 2^-100
+ *   zero = round(-lo / step)
+ *   code = round(x / step) + zero, at least 0 and at most 15 (255)
+ * (halves to even); the group stands for (code - zero) * step, at most half a
+ * step from x and exact in bf16 and fp32. It takes 2 bytes for step and zero: 34
+ * bytes for 64 numbers in 4 bits, 66 in 8. A group with a number that is not
+ * below 2^125 in magnitude (infinities and NaN among them) stands for NaN
+ * throughout; a position that is not visible does not enter all the same.
+ * Queries are taken to be below 2^100 in magnitude.
+ * In bf16, a cache whose max_tokens times query heads of a kv head is 128 or more
+ * also holds one layer's keys and values of all its pages in bf16: attention of
+ * sequences with that many rows unpacks their pages there first.
+ * Errors: as whisper_cache_create.
+ */
+whisper_status whisper_cache_create_packed(const whisper_cache_params* params, int32_t bits, int device,
+                                           whisper_cache** out);
+
 /* Waits for the cache's stream and frees what the cache owns. NULL is allowed. */
 void whisper_cache_destroy(whisper_cache* cache);
 
@@ -634,7 +658,7 @@ whisper_status whisper_cache_set_stream(whisper_cache* cache, void* hip_stream);
 /*
  * Adds counts[i] >= 0 positions to sequence seqs[i] (host arrays, n distinct
  * sequences) and makes them the current chunk, until the next extend, or a
- * truncate that takes positions from one of its sequences. A page that is
+ * truncate or reorder that takes positions from one of its sequences. A page that is
  * shared and gets new positions is copied first. Errors: E_INVAL, E_CAPACITY
  * (no such sequence, too few free pages, max_positions or max_tokens; nothing
  * has changed then).
@@ -645,7 +669,8 @@ whisper_status whisper_cache_extend(whisper_cache* cache, const int32_t* seqs, c
  * Writes the chunk's keys and values of one layer: device rows k and v
  * [tokens][n_kv_head][head_size], row strides in elements (0: rows without
  * gaps). layer -1: all layers, k and v [n_layer][tokens] rows. Errors:
- * E_INVAL, E_STATE (no chunk, or a sequence of it was forked).
+ * E_INVAL, E_STATE (no chunk, or a sequence of it was forked or is continued by
+ * others since).
  */
 whisper_status whisper_cache_append(whisper_cache* cache, int32_t layer, const void* k, const void* v, int64_t k_stride,
                                     int64_t v_stride);
@@ -676,6 +701,17 @@ whisper_status whisper_cache_truncate(whisper_cache* cache, const int32_t* seqs,
  * Errors: E_INVAL, E_STATE (a destination is not empty), E_CAPACITY (no such
  * sequence, too few free pages). */
 whisper_status whisper_cache_fork(whisper_cache* cache, int32_t src, const int32_t* dst, int32_t n);
+
+/* Makes sequence seqs[i] (n distinct ones) what sequence from[i] was before the
+ * call, all of them at once: a beam search's step, whose new beams continue old
+ * ones (several of them the same). What seqs[i] held is given up; sequences that
+ * are not listed in `seqs` stay. Pages are shared, and partly filled ones are
+ * copied when they get new positions (a page's last holder writes in place), so
+ * nothing is copied for beams that are given up. A sequence of the current chunk
+ * that becomes another one ends the chunk; if one is continued by others, its
+ * new rows can be attended to but not appended any more, as after a fork.
+ * Errors: E_INVAL, E_CAPACITY (no such sequence). */
+whisper_status whisper_cache_reorder(whisper_cache* cache, const int32_t* seqs, const int32_t* from, int32_t n);
 
 /* Moves the pages in use to the front of the cache's memory. */
 whisper_status whisper_cache_compact(whisper_cache* cache);
@@ -740,6 +776,61 @@ whisper_status whisper_sampler_options(whisper_sampler* sampler, const whisper_s
  */
 whisper_status whisper_sampler_run(whisper_sampler* sampler, const void* logits, int32_t dtype, int32_t n_rows,
                                    int64_t row_stride, const float* uniforms, int32_t* tokens, float* logprobs);
+
+/*
+ * Beam selection: the likeliest continuations of groups of beams. Beam b of a
+ * group (an utterance) has a score c[b], the log-probability of what it holds, and
+ * a row of logits l; its continuation by id i has
+ *   c[b] + l[i] - log(sum exp(l[j])),  the sum over all ids that are not suppressed.
+ * Suppressed ids, NaN and -inf continue nothing; if a row's largest logit is
+ * +inf, only such ids do, all alike. A score that is not finite says that there
+ * is no such beam (its logits are not read): at an utterance's first step, all but
+ * one. Sums and scores are fp64 until they are written.
+ * Streams, device, threads: as for whisper_cache; whisper_beam_run may be
+ * recorded into a graph and takes the suppressed ids that are set when it runs. All
+ * calls on one handle, replays too, share its workspace: order them on one stream.
+ * What to do with continuations by an end-of-text id is the program's: with n_best
+ * of twice the width, enough others remain. whisper_cache_reorder then makes a
+ * cache's sequences those of the chosen parents.
+ */
+typedef struct whisper_beam whisper_beam;
+
+/* Creates a selection over rows of n_vocab (1..2^20) logits, at most max_rows
+ * (1..65536) a call, on HIP device `device` (WHISPER_NO_DEVICE: for the checks of
+ * arguments; run returns WHISPER_E_STATE). Nothing is suppressed at first.
+ * Errors: E_INVAL, E_NOMEM, E_DEVICE; whisper_beam_error(NULL) then holds the message. */
+whisper_status whisper_beam_create(int32_t n_vocab, int32_t max_rows, int device, whisper_beam** out);
+
+/* Waits for the stream and frees what the handle owns. NULL is allowed. */
+void whisper_beam_destroy(whisper_beam* beam);
+
+/* Last error message, as whisper_cache_error. */
+const char* whisper_beam_error(const whisper_beam* beam);
+
+/* Stream of the following calls, as whisper_cache_set_stream. */
+whisper_status whisper_beam_set_stream(whisper_beam* beam, void* hip_stream);
+
+/* Sets the n_suppress ids that continue no beam (host array, replaces the former
+ * list). Waits for the stream. Errors: E_INVAL, E_STATE (the stream is recording a
+ * graph). */
+whisper_status whisper_beam_options(whisper_beam* beam, const int32_t* suppress, int32_t n_suppress);
+
+/*
+ * Enqueues the choice for n_groups groups of `width` (1..32) beams (device
+ * memory throughout; group g's beams are rows g * width ..):
+ *   logits      [n_groups * width][row_stride] of type dtype (WHISPER_DTYPE_*),
+ *               row_stride in elements (0: n_vocab); read only
+ *   scores      fp32 [n_groups * width]
+ *   parents, tokens, out_scores   int32, int32, fp32 [n_groups][n_best] (1..64): the
+ *               group's n_best likeliest continuations, likeliest first, equal ones
+ *               by beam and then by id: the beam's number in the group, the id and
+ *               the continuation's score; -1, -1 and -inf where there are no more.
+ *               out_scores must not overlap scores.
+ * n_groups * width is at most max_rows. Errors: E_INVAL, E_STATE.
+ */
+whisper_status whisper_beam_run(whisper_beam* beam, const void* logits, int32_t dtype, int32_t n_groups, int32_t width,
+                                int32_t n_best, int64_t row_stride, const float* scores, int32_t* parents, int32_t* tokens,
+                                float* out_scores);
 
 #ifdef __cplusplus
 }

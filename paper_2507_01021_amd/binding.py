@@ -33,6 +33,9 @@ EXPORTS = (
     "whisper_cache_fork", "whisper_cache_compact", "whisper_cache_read", "whisper_cache_info",
     "whisper_sampler_create", "whisper_sampler_destroy", "whisper_sampler_error", "whisper_sampler_set_stream",
     "whisper_sampler_options", "whisper_sampler_run",
+    "whisper_cache_create_packed", "whisper_cache_reorder",
+    "whisper_beam_create", "whisper_beam_destroy", "whisper_beam_error", "whisper_beam_set_stream",
+    "whisper_beam_options", "whisper_beam_run",
 )
 
 
@@ -135,6 +138,14 @@ def load(path: str = LIB_PATH) -> C.CDLL:
         "whisper_sampler_set_stream": (i32, [vp, vp]),
         "whisper_sampler_options": (i32, [vp, C.POINTER(whisper_sampling), i32, pi32, i32]),
         "whisper_sampler_run": (i32, [vp, vp, i32, i32, i64, vp, vp, vp]),
+        "whisper_cache_create_packed": (i32, [C.POINTER(whisper_cache_params), i32, C.c_int, C.POINTER(vp)]),
+        "whisper_cache_reorder": (i32, [vp, pi32, pi32, i32]),
+        "whisper_beam_create": (i32, [i32, i32, C.c_int, C.POINTER(vp)]),
+        "whisper_beam_destroy": (None, [vp]),
+        "whisper_beam_error": (C.c_char_p, [vp]),
+        "whisper_beam_set_stream": (i32, [vp, vp]),
+        "whisper_beam_options": (i32, [vp, pi32, i32]),
+        "whisper_beam_run": (i32, [vp, vp, i32, i32, i32, i32, i64, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -348,16 +359,16 @@ class Context:
 
 
 class Cache:
-    """A paged key/value cache (whisper_cache_*). k, v, q and out are device
-    addresses; the calls enqueue work on the cache's stream and return
-    without waiting for it."""
+    """A paged key/value cache (whisper_cache_*), packed in 8 or 4 bits or (bits
+    0) in its dtype. k, v, q and out are device addresses; the calls enqueue
+    work on the cache's stream and return without waiting for it."""
 
     def __init__(self, dtype: int, n_layer: int, n_head: int, n_kv_head: int, head_size: int, page_size: int,
-                 n_pages: int, max_seqs: int, max_positions: int, max_tokens: int, device: int = 0):
+                 n_pages: int, max_seqs: int, max_positions: int, max_tokens: int, device: int = 0, bits: int = 0):
         self.params = whisper_cache_params(dtype, n_layer, n_head, n_kv_head, head_size, page_size, n_pages, max_seqs,
                                            max_positions, max_tokens)
         h = C.c_void_p()
-        st = load().whisper_cache_create(C.byref(self.params), device, C.byref(h))
+        st = load().whisper_cache_create_packed(C.byref(self.params), bits, device, C.byref(h))
         self.h = None
         self._check(st)
         self.h = h
@@ -407,6 +418,12 @@ class Cache:
     def fork(self, src: int, dst):
         d = _ints(dst)
         self._check(load().whisper_cache_fork(self.h, src, _ptr(d, C.c_int32), d.size))
+
+    def reorder(self, seqs, from_seqs):
+        """Sequence seqs[i] becomes what from_seqs[i] was, all at once."""
+        s, f = _ints(seqs), _ints(from_seqs)
+        _same_length(s, f)
+        self._check(load().whisper_cache_reorder(self.h, _ptr(s, C.c_int32), _ptr(f, C.c_int32), s.size))
 
     def compact(self):
         self._check(load().whisper_cache_compact(self.h))
@@ -486,6 +503,51 @@ class Sampler:
             row_stride: int = 0):
         self._check(load().whisper_sampler_run(self.h, logits, dtype, n_rows, row_stride, uniforms, tokens,
                                                logprobs or None))
+
+
+class Beam:
+    """Choice of continuations for groups of beams from logits in device memory
+    (whisper_beam_*). Addresses are device addresses; run enqueues and returns."""
+
+    def __init__(self, n_vocab: int, max_rows: int, device: int = 0):
+        h = C.c_void_p()
+        st = load().whisper_beam_create(n_vocab, max_rows, device, C.byref(h))
+        self.h = None
+        self._check(st)
+        self.h, self.n_vocab, self.max_rows = h, n_vocab, max_rows
+
+    def close(self):
+        if getattr(self, "h", None):
+            load().whisper_beam_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def _check(self, st):
+        if st != OK:
+            raise WhisperError(st, load().whisper_beam_error(self.h).decode())
+
+    def set_stream(self, stream_handle: int | None):
+        self._check(load().whisper_beam_set_stream(self.h, C.c_void_p(stream_handle or None)))
+
+    def options(self, suppress=()):
+        s = _ints(suppress)
+        self._check(load().whisper_beam_options(self.h, _ptr(s, C.c_int32), s.size))
+
+    def run(self, logits: int, dtype: int, n_groups: int, width: int, n_best: int, scores: int, parents: int, tokens: int,
+            out_scores: int, row_stride: int = 0):
+        self._check(load().whisper_beam_run(self.h, logits, dtype, n_groups, width, n_best, row_stride, scores, parents,
+                                            tokens, out_scores))
 
 
 def test_batcher(arrival_us, user_id, segment_id, max_new_tokens, slots, encode_batch, refill_min,

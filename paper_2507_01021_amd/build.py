@@ -20,7 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB_NAME = "libwhisper_mi355x.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
-SOURCES = ["engine.hip", "cache.hip", "sampler.hip", "capi.cpp", "capi_ops.cpp", "batcher.cpp"]
+SOURCES = ["engine.hip", "cache.hip", "sampler.hip", "beam.hip", "capi.cpp", "capi_ops.cpp", "batcher.cpp"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

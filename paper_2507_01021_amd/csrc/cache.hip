@@ -6,6 +6,7 @@
 
 #include "cache.h"
 #include "device.h"
+#include "packed.h"
 #include "paged.h"
 
 namespace wmi {
@@ -41,16 +42,16 @@ constexpr int MOST_WGS = 1 << 22;
 template <class T>
 class PagedCacheT final : public PagedCache {
    public:
-    PagedCacheT(const whisper_cache_params& p, int device)
-        : P_(p), dev_(device), book_(p.page_size, p.n_pages, p.max_seqs, p.max_positions) {
+    PagedCacheT(const whisper_cache_params& p, int bits, int device)
+        : P_(p), bits_(bits), dev_(device), book_(p.page_size, p.n_pages, p.max_seqs, p.max_positions) {
         G_ = p.n_head / p.n_kv_head;
         // parts of cut ranges: ATTN_WGS / n_kv_head whole ones and a partial one for each of as many ranges
         max_parts_ = 2 * (ATTN_WGS / p.n_kv_head + 1);
         if (big_rows(p.max_tokens)) max_parts_ += BIG_ROWS / 16 * 2 * (BIG_WGS / p.n_kv_head + 1);
         if (dev_ == WHISPER_NO_DEVICE) return;
         DeviceScope scope(dev_);
-        head_elems_ = (long long)p.page_size * p.head_size;
-        page_bytes_ = 2LL * p.n_layer * p.n_kv_head * head_elems_ * sizeof(T);
+        head_elems_ = bits_ ? packed_head(p.page_size, p.head_size, bits_) : (long long)p.page_size * p.head_size;
+        page_bytes_ = 2LL * p.n_layer * p.n_kv_head * head_elems_ * (bits_ ? 1 : sizeof(T));
         while ((1 << shift_) < p.page_size) ++shift_;
         pages_ = dalloc<unsigned char>((size_t)p.n_pages * page_bytes_);
         table_ = dalloc<int>((size_t)p.max_seqs * book_.max_list() + 1);
@@ -60,6 +61,10 @@ class PagedCacheT final : public PagedCache {
         max_tiles_ = (int)std::min(T0, T0 / 32 + 2 * S0);
         plan_.cap = HEAD_INTS + 8 * (T0 * G_ / 16 + S0 + max_parts_) + 6LL * max_parts_ + 4LL * max_tiles_ +
                     2 * (std::min(T0, T0 / p.page_size + S0) + 2 * S0);
+        if (unpacks()) {
+            plan_.cap += std::min<long long>(p.n_pages, S0 * book_.max_list());
+            wide_ = dalloc<bf16>((size_t)p.n_pages * 2 * p.n_kv_head * p.page_size * p.head_size);
+        }
         plan_.dev = dalloc<int>(plan_.cap);
         parts_ = dalloc<float>((size_t)max_parts_ * p.n_kv_head * 16 * (p.head_size + 2));
         WMI_HIP(hipDeviceSynchronize());
@@ -74,7 +79,7 @@ class PagedCacheT final : public PagedCache {
             if (s.ev) (void)hipEventDestroy(s.ev);
             if (s.host) (void)hipHostFree(s.host);
         }
-        for (void* q : {(void*)pages_, (void*)table_, (void*)parts_, (void*)plan_.dev, (void*)list_.dev})
+        for (void* q : {(void*)pages_, (void*)table_, (void*)parts_, (void*)plan_.dev, (void*)list_.dev, (void*)wide_})
             if (q) (void)hipFree(q);
         if (old >= 0) (void)hipSetDevice(old);
     }
@@ -167,9 +172,8 @@ class PagedCacheT final : public PagedCache {
         if (!taken || !plan_ok_) return;
         plan_ok_ = false;
         if (dev_ == WHISPER_NO_DEVICE) return;
-        // a replay must find no rows: the pages may soon be another sequence's
         DeviceScope scope(dev_);
-        put(plan_, std::vector<int>(HEAD_INTS, 0), 0, 0);
+        end_chunk(false);
     }
 
     void fork(int src, const int* dst, int n) override {
@@ -196,11 +200,47 @@ class PagedCacheT final : public PagedCache {
         if (n == 0 || !open || !plan_ok_ || !append_ok_) return;
         append_ok_ = false;
         DeviceScope scope(dev_);
-        ListHead head = head_;
-        head.tiles = 0;
-        std::vector<int> h(HEAD_INTS);
-        memcpy(h.data(), &head, sizeof(head));
-        put(plan_, h, 0, 0);
+        end_chunk(true);
+    }
+
+    void reorder(const int* seqs, const int* from, int n) override {
+        if (dev_ != WHISPER_NO_DEVICE) {
+            DeviceScope scope(dev_);
+            no_capture();
+        }
+        // sequences that stay what they are take no part
+        std::vector<int> to, src;
+        for (int i = 0; i < n; ++i)
+            if (seqs[i] != from[i]) {
+                to.push_back(seqs[i]);
+                src.push_back(from[i]);
+            }
+        if (to.empty()) return;
+        auto in_chunk = [&](const std::vector<int>& l) {
+            for (size_t i = 0; i < chunk_.size(); ++i)
+                if (counts_[i] > 0 && std::find(l.begin(), l.end(), chunk_[i]) != l.end()) return true;
+            return false;
+        };
+        std::vector<std::vector<int>> before;
+        for (int s : to) before.push_back(book_.pages(s));
+        book_.reorder(to.data(), src.data(), (int)to.size());
+        // the chunk's rows: those of a sequence that is another now are gone, and
+        // pages that a sequence of the chunk shares now are not written any more
+        const bool gone = plan_ok_ && in_chunk(to), shared = plan_ok_ && append_ok_ && in_chunk(src);
+        if (gone) plan_ok_ = false;
+        if (shared) append_ok_ = false;
+        if (dev_ == WHISPER_NO_DEVICE) return;
+        std::vector<int> upd;
+        for (size_t i = 0; i < to.size(); ++i) {
+            const auto& pg = book_.pages(to[i]);
+            for (size_t k = 0; k < pg.size(); ++k)
+                if (k >= before[i].size() || pg[k] != before[i][k]) add_update(upd, to[i], (int)k, pg[k]);
+        }
+        if (gone || shared) {
+            DeviceScope scope(dev_);
+            end_chunk(!gone);
+        }
+        apply(upd, {});
     }
 
     void compact() override {
@@ -233,7 +273,7 @@ class PagedCacheT final : public PagedCache {
         int row = 0;
         for (int i = 0; i < n; ++i) row = add_tiles(t, seqs[i], 0, book_.length(seqs[i]), row);
         if (row == 0) return;
-        const ListHead head{0, 0, (int)(t.size() - HEAD_INTS) / 4, 0, HEAD_INTS, 0, 0, 0};
+        const ListHead head{0, 0, (int)(t.size() - HEAD_INTS) / 4, 0, HEAD_INTS, 0, 0, 0, 0};
         memcpy(t.data(), &head, sizeof(head));
         put(list_, t, 0, 0);
         move<false>(layer, list_.dev, head.tiles, k, v, k_ld, v_ld, row);
@@ -250,8 +290,9 @@ class PagedCacheT final : public PagedCache {
         hipEvent_t ev = nullptr;
     };
     whisper_cache_params P_;
-    int dev_, G_, shift_ = 0;
-    long long head_elems_ = 0, page_bytes_ = 0;
+    int bits_, dev_, G_, shift_ = 0;
+    long long head_elems_ = 0, page_bytes_ = 0;  // (packed: bytes of a head)
+    bf16* wide_ = nullptr;                       // packed: a layer's unpacked pages, for attention of many rows
     int max_parts_ = 0;
     PageBook book_;
     hipStream_t st_ = nullptr;  // the device's default stream unless one was chosen
@@ -266,7 +307,7 @@ class PagedCacheT final : public PagedCache {
     ListHead head_{};
     bool plan_ok_ = false;    // there is a chunk
     bool append_ok_ = false;  // none of its sequences was forked since
-    int tokens_ = 0, n_items_ = 0, n_bigs_ = 0, n_merges_ = 0, n_tiles_ = 0;
+    int tokens_ = 0, n_items_ = 0, n_bigs_ = 0, n_merges_ = 0, n_tiles_ = 0, n_wide_ = 0;
     int max_tiles_ = 0;
 
     template <class U>
@@ -274,7 +315,7 @@ class PagedCacheT final : public PagedCache {
         void* q = nullptr;
         if (hipMalloc(&q, std::max<size_t>(count, 1) * sizeof(U)) != hipSuccess) {
             (void)hipGetLastError();
-            for (void* x : {(void*)pages_, (void*)table_, (void*)plan_.dev})
+            for (void* x : {(void*)pages_, (void*)table_, (void*)plan_.dev, (void*)wide_})
                 if (x) (void)hipFree(x);
             throw ArgError(WHISPER_E_NOMEM, "device allocation of " + std::to_string(count * sizeof(U)) + " bytes failed");
         }
@@ -288,6 +329,14 @@ class PagedCacheT final : public PagedCache {
     void need_chunk() const {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the cache has no device");
         if (!plan_ok_) throw ArgError(WHISPER_E_STATE, "no chunk: call whisper_cache_extend first");
+    }
+    // What a replay finds from now on: no rows, or rows to attend to but none to append.
+    void end_chunk(bool attend) {
+        ListHead head = attend ? head_ : ListHead{};
+        head.tiles = 0;
+        std::vector<int> h(HEAD_INTS);
+        memcpy(h.data(), &head, sizeof(head));
+        put(plan_, h, 0, 0);
     }
     PagedView view() const {
         return PagedView{pages_, table_, book_.max_list(), shift_, P_.n_layer, P_.n_kv_head, head_elems_, odd_};
@@ -366,6 +415,7 @@ class PagedCacheT final : public PagedCache {
     // Whether a chunk's `count` tokens of one sequence go to the kernel of many rows.
     bool big_rows(int count) const { return sizeof(T) == 2 && (long long)count * G_ >= BIG_FROM; }
     bool max_bigs() const { return big_rows(P_.max_tokens); }
+    bool unpacks() const { return bits_ && max_bigs(); }
 
     // Positions [first, first + n) of a sequence as tiles; returns the row after its last.
     static int add_tiles(std::vector<int>& t, int seq, int first, int n, int row) {
@@ -446,7 +496,22 @@ class PagedCacheT final : public PagedCache {
         const size_t ma = add(merges.data(), merges.size() * (sizeof(MergeItem) / sizeof(int)));
         const size_t ta = add(tiles.data(), tiles.size());
         const size_t ba = add(bigs.data(), bigs.size() * (sizeof(AttnItem) / sizeof(int)));
-        head_ = ListHead{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, 0};
+        // pages of the bigs' sequences, each once
+        std::vector<int> wide;
+        if (bits_ && n_bigs_) {
+            std::vector<bool> seen(P_.n_pages, false);
+            for (int i = 0; i < n; ++i) {
+                if (!big_rows(counts[i])) continue;
+                const auto& pg = book_.pages(seqs[i]);
+                for (size_t k = 0; k < pg.size(); ++k) {
+                    if (!seen[pg[k]]) wide.push_back(seqs[i] * book_.max_list() + (int)k);
+                    seen[pg[k]] = true;
+                }
+            }
+        }
+        n_wide_ = (int)wide.size();
+        const size_t wa = add(wide.data(), wide.size());
+        head_ = ListHead{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, n_wide_, (int)wa};
         memcpy(blob_.data(), &head_, sizeof(head_));
     }
 
@@ -457,9 +522,23 @@ class PagedCacheT final : public PagedCache {
         const unsigned nm = rec ? ATTN_WGS : (unsigned)n_merges_ * P_.n_kv_head;
         if constexpr (sizeof(T) == 2) {
             const unsigned nb = rec ? (max_bigs() ? 2 * BIG_WGS : 0) : (unsigned)n_bigs_ * P_.n_kv_head;
-            if (nb) hipLaunchKernelGGL(paged_attn_big_kernel<D>, dim3(nb), dim3(BIG_THREADS), 0, st_, a);
+            AttnArgs w = a;
+            if (bits_ && nb) {
+                const int nw = rec ? 8 * BIG_WGS : std::min(n_wide_ * P_.n_kv_head * (P_.page_size / 64 + 1), MOST_WGS);
+                if (bits_ == 4) hipLaunchKernelGGL((packed_unpack_kernel<D, 4>), dim3(nw), dim3(256), 0, st_, a.c, a.layer, a.plan, wide_);
+                else hipLaunchKernelGGL((packed_unpack_kernel<D, 8>), dim3(nw), dim3(256), 0, st_, a.c, a.layer, a.plan, wide_);
+                w.c.pages = reinterpret_cast<unsigned char*>(wide_);
+                w.c.n_layer = 1;
+                w.c.head_elems = (long long)P_.page_size * D;
+                w.layer = 0;
+            }
+            if (nb) hipLaunchKernelGGL(paged_attn_big_kernel<D>, dim3(nb), dim3(BIG_THREADS), 0, st_, w);
         }
-        if (ni) hipLaunchKernelGGL((paged_attn_kernel<T, D, false>), dim3(ni), dim3(256), 0, st_, a);
+        if (ni) {
+            if (bits_ == 4) hipLaunchKernelGGL((packed_attn_kernel<T, D, 4>), dim3(ni), dim3(256), 0, st_, a);
+            else if (bits_ == 8) hipLaunchKernelGGL((packed_attn_kernel<T, D, 8>), dim3(ni), dim3(256), 0, st_, a);
+            else hipLaunchKernelGGL((paged_attn_kernel<T, D, false>), dim3(ni), dim3(256), 0, st_, a);
+        }
         if (nm) hipLaunchKernelGGL((paged_merge_kernel<T, D, false>), dim3(nm), dim3(256), 0, st_, a);
     }
 
@@ -479,23 +558,28 @@ class PagedCacheT final : public PagedCache {
         const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0 && k_ld % EL == 0 &&
                          v_ld % EL == 0;
         const dim3 grid(std::min(n, MOST_WGS), P_.n_kv_head, nl), block(256);
+        auto go = [&](auto kernel, auto* kk, auto* vv) {
+            hipLaunchKernelGGL(kernel, grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);
+        };
         if constexpr (IN) {
             const T *kk = static_cast<const T*>(k), *vv = static_cast<const T*>(v);
-            if (vec) hipLaunchKernelGGL((paged_append_kernel<T, D, true>), grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);
-            else hipLaunchKernelGGL((paged_append_kernel<T, D, false>), grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);
+            if (bits_ == 4) vec ? go(packed_append_kernel<T, D, 4, true>, kk, vv) : go(packed_append_kernel<T, D, 4, false>, kk, vv);
+            else if (bits_ == 8) vec ? go(packed_append_kernel<T, D, 8, true>, kk, vv) : go(packed_append_kernel<T, D, 8, false>, kk, vv);
+            else vec ? go(paged_append_kernel<T, D, true>, kk, vv) : go(paged_append_kernel<T, D, false>, kk, vv);
         } else {
             T *kk = static_cast<T*>(const_cast<void*>(k)), *vv = static_cast<T*>(const_cast<void*>(v));
-            if (vec) hipLaunchKernelGGL((paged_read_kernel<T, D, true>), grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);
-            else hipLaunchKernelGGL((paged_read_kernel<T, D, false>), grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);
+            if (bits_ == 4) vec ? go(packed_read_kernel<T, D, 4, true>, kk, vv) : go(packed_read_kernel<T, D, 4, false>, kk, vv);
+            else if (bits_ == 8) vec ? go(packed_read_kernel<T, D, 8, true>, kk, vv) : go(packed_read_kernel<T, D, 8, false>, kk, vv);
+            else vec ? go(paged_read_kernel<T, D, true>, kk, vv) : go(paged_read_kernel<T, D, false>, kk, vv);
         }
     }
 };
 
 }  // namespace
 
-std::unique_ptr<PagedCache> make_paged_cache(const whisper_cache_params& p, int device) {
-    if (p.dtype == WHISPER_DTYPE_BF16) return std::unique_ptr<PagedCache>(new PagedCacheT<bf16>(p, device));
-    return std::unique_ptr<PagedCache>(new PagedCacheT<float>(p, device));
+std::unique_ptr<PagedCache> make_paged_cache(const whisper_cache_params& p, int bits, int device) {
+    if (p.dtype == WHISPER_DTYPE_BF16) return std::unique_ptr<PagedCache>(new PagedCacheT<bf16>(p, bits, device));
+    return std::unique_ptr<PagedCache>(new PagedCacheT<float>(p, bits, device));
 }
 
 }  // namespace wmi

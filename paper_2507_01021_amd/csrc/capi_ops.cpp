@@ -1,6 +1,7 @@
 // C ABI of the operators that work on a program's own device memory
-// (include/whisper_mi355x.h): the paged key/value cache and the sampler. Argument checks,
-// error codes and messages; every check runs before any device work.
+// (include/whisper_mi355x.h): the paged key/value cache, the sampler and the
+// choice of beams. Argument checks, error codes and messages; every check runs
+// before any device work.
 #include <hip/hip_runtime.h>
 
 #include <memory>
@@ -9,6 +10,7 @@
 #include <string>
 #include <vector>
 
+#include "beam.h"
 #include "cache.h"
 #include "sampler.h"
 
@@ -28,6 +30,13 @@ struct whisper_cache {
 struct whisper_sampler {
     int n_vocab, max_rows;
     std::unique_ptr<wmi::Sampler> impl;
+    std::string err;
+    bool broken = false;
+};
+
+struct whisper_beam {
+    int n_vocab, max_rows;
+    std::unique_ptr<wmi::Beam> impl;
     std::string err;
     bool broken = false;
 };
@@ -124,6 +133,19 @@ whisper_status check_rows(whisper_cache* c, const void* p, int64_t given, int he
     return WHISPER_OK;
 }
 
+// Ids that are never chosen: in the vocabulary, and not all of it.
+template <class H>
+whisper_status check_suppressed(H* h, int n_vocab, const int32_t* suppress, int32_t n) {
+    if (n < 0 || (n > 0 && !suppress)) return fail(h, WHISPER_E_INVAL, "suppress must not be NULL");
+    std::set<int> ids;
+    for (int i = 0; i < n; ++i) {
+        if (suppress[i] < 0 || suppress[i] >= n_vocab) return fail(h, WHISPER_E_INVAL, "suppressed id out of range");
+        ids.insert(suppress[i]);
+    }
+    if ((int)ids.size() >= n_vocab) return fail(h, WHISPER_E_INVAL, "every id would be suppressed");
+    return WHISPER_OK;
+}
+
 whisper_status check_layer(whisper_cache* c, int32_t layer, bool all) {
     if (layer < (all ? -1 : 0) || layer >= c->p.n_layer)
         return fail(c, WHISPER_E_INVAL, "layer outside 0..n_layer-1" + std::string(all ? " and not -1" : ""));
@@ -141,16 +163,21 @@ whisper_status check_layer(whisper_cache* c, int32_t layer, bool all) {
 extern "C" {
 
 whisper_status whisper_cache_create(const whisper_cache_params* params, int device, whisper_cache** out) {
+    return whisper_cache_create_packed(params, 0, device, out);
+}
+
+whisper_status whisper_cache_create_packed(const whisper_cache_params* params, int32_t bits, int device, whisper_cache** out) {
     whisper_cache* none = nullptr;
     if (!params || !out) return fail(none, WHISPER_E_INVAL, "params and out must not be NULL");
     const std::string bad = check_cache(*params);
     if (!bad.empty()) return fail(none, WHISPER_E_INVAL, bad);
+    if (bits != 0 && bits != 4 && bits != 8) return fail(none, WHISPER_E_INVAL, "bits must be 0, 4 or 8");
     WMI_TRY(check_device(device));
     std::unique_ptr<whisper_cache> c(new (std::nothrow) whisper_cache());
     if (!c) return fail(none, WHISPER_E_NOMEM, "host allocation failed");
     c->p = *params;
     WMI_TRY(guarded(none, [&]() -> whisper_status {
-        c->impl = wmi::make_paged_cache(*params, device);
+        c->impl = wmi::make_paged_cache(*params, bits, device);
         return WHISPER_OK;
     }));
     *out = c.release();
@@ -232,6 +259,19 @@ whisper_status whisper_cache_fork(whisper_cache* cache, int32_t src, const int32
     });
 }
 
+whisper_status whisper_cache_reorder(whisper_cache* cache, const int32_t* seqs, const int32_t* from, int32_t n) {
+    WMI_TRY(usable(cache));
+    WMI_TRY(check_seqs(cache, seqs, seqs, n, "from"));
+    if (n > 0 && !from) return fail(cache, WHISPER_E_INVAL, "seqs and from must not be NULL");
+    for (int i = 0; i < n; ++i)
+        if (from[i] < 0 || from[i] >= cache->p.max_seqs)
+            return fail(cache, WHISPER_E_CAPACITY, "sequence " + std::to_string(from[i]) + " outside 0..max_seqs-1");
+    return guarded(cache, [&]() -> whisper_status {
+        cache->impl->reorder(seqs, from, n);
+        return WHISPER_OK;
+    });
+}
+
 whisper_status whisper_cache_compact(whisper_cache* cache) {
     WMI_TRY(usable(cache));
     return guarded(cache, [&]() -> whisper_status {
@@ -302,19 +342,12 @@ whisper_status whisper_sampler_options(whisper_sampler* sampler, const whisper_s
                                        const int32_t* suppress, int32_t n_suppress) {
     WMI_TRY(usable(sampler));
     if (n < 0 || n > sampler->max_rows) return fail(sampler, WHISPER_E_INVAL, "n must be in 0..max_rows");
-    if ((n > 0 && !rows) || n_suppress < 0 || (n_suppress > 0 && !suppress))
-        return fail(sampler, WHISPER_E_INVAL, "rows and suppress must not be NULL");
+    if (n > 0 && !rows) return fail(sampler, WHISPER_E_INVAL, "rows and suppress must not be NULL");
     for (int i = 0; i < n; ++i) {
         const char* bad = wmi::sampling_fault(rows[i]);
         if (bad) return fail(sampler, WHISPER_E_INVAL, "row " + std::to_string(i) + ": " + bad);
     }
-    std::set<int> ids;
-    for (int i = 0; i < n_suppress; ++i) {
-        if (suppress[i] < 0 || suppress[i] >= sampler->n_vocab)
-            return fail(sampler, WHISPER_E_INVAL, "suppressed id out of range");
-        ids.insert(suppress[i]);
-    }
-    if ((int)ids.size() >= sampler->n_vocab) return fail(sampler, WHISPER_E_INVAL, "every id would be suppressed");
+    WMI_TRY(check_suppressed(sampler, sampler->n_vocab, suppress, n_suppress));
     return guarded(sampler, [&]() -> whisper_status {
         sampler->impl->options(rows, n, suppress, n_suppress);
         return WHISPER_OK;
@@ -337,6 +370,72 @@ whisper_status whisper_sampler_run(whisper_sampler* sampler, const void* logits,
         return fail(sampler, WHISPER_E_INVAL, "a device pointer is not aligned to its type");
     return guarded(sampler, [&]() -> whisper_status {
         sampler->impl->run(logits, dtype, n_rows, row_stride ? row_stride : sampler->n_vocab, uniforms, tokens, logprobs);
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_beam_create(int32_t n_vocab, int32_t max_rows, int device, whisper_beam** out) {
+    whisper_beam* none = nullptr;
+    if (!out) return fail(none, WHISPER_E_INVAL, "out must not be NULL");
+    if (n_vocab < 1 || n_vocab > (1 << 20)) return fail(none, WHISPER_E_INVAL, "n_vocab must be in 1..1048576");
+    if (max_rows < 1 || max_rows > (1 << 16)) return fail(none, WHISPER_E_INVAL, "max_rows must be in 1..65536");
+    WMI_TRY(check_device(device));
+    std::unique_ptr<whisper_beam> b(new (std::nothrow) whisper_beam());
+    if (!b) return fail(none, WHISPER_E_NOMEM, "host allocation failed");
+    b->n_vocab = n_vocab;
+    b->max_rows = max_rows;
+    WMI_TRY(guarded(none, [&]() -> whisper_status {
+        b->impl = wmi::make_beam(n_vocab, device);
+        return WHISPER_OK;
+    }));
+    *out = b.release();
+    return WHISPER_OK;
+}
+
+void whisper_beam_destroy(whisper_beam* beam) { delete beam; }
+
+const char* whisper_beam_error(const whisper_beam* beam) { return beam ? beam->err.c_str() : g_error.c_str(); }
+
+whisper_status whisper_beam_set_stream(whisper_beam* beam, void* hip_stream) {
+    WMI_TRY(usable(beam));
+    return guarded(beam, [&]() -> whisper_status {
+        beam->impl->set_stream(hip_stream);
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_beam_options(whisper_beam* beam, const int32_t* suppress, int32_t n_suppress) {
+    WMI_TRY(usable(beam));
+    WMI_TRY(check_suppressed(beam, beam->n_vocab, suppress, n_suppress));
+    return guarded(beam, [&]() -> whisper_status {
+        beam->impl->options(suppress, n_suppress);
+        return WHISPER_OK;
+    });
+}
+
+whisper_status whisper_beam_run(whisper_beam* beam, const void* logits, int32_t dtype, int32_t n_groups, int32_t width,
+                                int32_t n_best, int64_t row_stride, const float* scores, int32_t* parents, int32_t* tokens,
+                                float* out_scores) {
+    WMI_TRY(usable(beam));
+    if (dtype != WHISPER_DTYPE_F32 && dtype != WHISPER_DTYPE_BF16)
+        return fail(beam, WHISPER_E_INVAL, "dtype must be 0 (fp32) or 1 (bf16)");
+    if (width < 1 || width > wmi::BEAM_WIDTH) return fail(beam, WHISPER_E_INVAL, "width must be in 1..32");
+    if (n_best < 1 || n_best > wmi::BEAM_BEST) return fail(beam, WHISPER_E_INVAL, "n_best must be in 1..64");
+    if (n_groups < 0 || n_groups > beam->max_rows / width)
+        return fail(beam, WHISPER_E_INVAL, "n_groups x width must be in 0..max_rows");
+    if (row_stride != 0 && (row_stride < beam->n_vocab || row_stride > ((int64_t)1 << 40)))
+        return fail(beam, WHISPER_E_INVAL, "row_stride must be 0 or at least n_vocab");
+    if (n_groups == 0) return WHISPER_OK;
+    if (!logits || !scores || !parents || !tokens || !out_scores)
+        return fail(beam, WHISPER_E_INVAL, "device pointers must not be NULL");
+    const size_t es = dtype == WHISPER_DTYPE_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % es ||
+        (reinterpret_cast<uintptr_t>(scores) | reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(tokens) |
+         reinterpret_cast<uintptr_t>(out_scores)) % 4)
+        return fail(beam, WHISPER_E_INVAL, "a device pointer is not aligned to its type");
+    return guarded(beam, [&]() -> whisper_status {
+        beam->impl->run(logits, dtype, n_groups, width, n_best, row_stride ? row_stride : beam->n_vocab, scores, parents,
+                        tokens, out_scores);
         return WHISPER_OK;
     });
 }

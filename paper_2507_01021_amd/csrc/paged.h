@@ -78,7 +78,8 @@ struct PageTile {
 // Kernels read it when they run and go through their part in strides of the
 // grid, so a recorded launch serves whatever list is current at its replay.
 struct ListHead {
-    int items, merges, tiles, merges_at, tiles_at, bigs, bigs_at, pad;
+    int items, merges, tiles, merges_at, tiles_at, bigs, bigs_at;
+    int pages, pages_at;  // of a packed cache: pages to unpack for the bigs
 };
 constexpr int HEAD_INTS = sizeof(ListHead) / sizeof(int);
 
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedView c, const int*
 }
 
 // Copies whole pages (all layers): pairs (source, destination), `bytes` each,
-// a multiple of 4096; five pages of 10.5 MB in 12.8 us (from L2 and the cache behind it). Workgroups of a pair take 16 KiB each.
+// a multiple of 16; five pages of 10.5 MB in 12.8 us (from L2 and the cache behind it). Workgroups of a pair take 16 KiB each.
 constexpr int PAGE_RUN = 16384;
 static __global__ __launch_bounds__(256) void paged_copy_kernel(unsigned char* __restrict__ pages,
                                                          const int* __restrict__ pairs, long long bytes) {

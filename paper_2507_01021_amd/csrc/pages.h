@@ -109,6 +109,25 @@ class PageBook {
         }
     }
 
+    // Makes sequence seqs[i] what sequence from[i] was before the call, all at
+    // once: pages are shared, partly filled ones too (the next extend copies
+    // those that still have several holders).
+    void reorder(const int* seqs, const int* from, int n) {
+        std::vector<std::vector<int>> lists(n);
+        std::vector<int> lens(n);
+        for (int i = 0; i < n; ++i) {
+            lists[i] = pages_[from[i]];
+            lens[i] = len_[from[i]];
+        }
+        for (auto& l : lists)
+            for (int p : l) ++ref_[p];
+        for (int i = 0; i < n; ++i) {
+            for (int p : pages_[seqs[i]]) give_back(p);
+            pages_[seqs[i]].swap(lists[i]);
+            len_[seqs[i]] = lens[i];
+        }
+    }
+
     // Moves the pages in use to the lowest numbers: afterwards page numbers
     // from used() on are free. Sources and destinations are disjoint.
     void compact(std::vector<PageCopy>& copies) {
