@@ -58,7 +58,8 @@ class BeamImpl final : public Beam {
         DeviceScope scope(dev_);
         // a recorded run may meet other suppressed ids at its replay
         const BeamArgs a{logits, ld, V_, width, n_best, use_never_ || capturing(st_) ? never_ : nullptr, scores,
-                         parents, tokens, out, ws_, 0};
+                         parents, tokens, out, reinterpret_cast<BeamPiece*>(ws_),
+                         reinterpret_cast<u64*>(ws_ + sizeof(BeamPiece) * BEAM_PIECES), 0, 0};
         if (dtype == WHISPER_DTYPE_BF16) beam_rows<bf16>(a, n_groups, st_);
         else beam_rows<float>(a, n_groups, st_);
         WMI_HIP(hipGetLastError());

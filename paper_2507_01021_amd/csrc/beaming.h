@@ -6,16 +6,21 @@
 // the sum over the ids that are not suppressed. A group's n best are wanted, in
 // descending order, equal ones by (b, i).
 //
-// Two kernels. beam_rows_kernel cuts every row over workgroups: in one pass it
-// adds up exponentials and keeps the n largest logits of its piece. Within a row
-// the order of the logits is that of the continuations, so a row's n largest
-// are enough. beam_pick_kernel, a workgroup per group, joins the pieces' sums and
-// picks from their lists.
+// Two kernels. beam_rows_kernel cuts every row into pieces, a workgroup's each,
+// and finds their largest logit, the sum of their exponentials and their n largest
+// logits. Within a row the order of the logits is that of the continuations, so a
+// row's n largest are enough. beam_pick_kernel, a workgroup per group, joins the
+// pieces' sums and picks from their lists.
+// The n largest of many numbers: the n-th largest of the lanes' maxima is a
+// bound that at least n numbers reach, and few more than n; those are listed, and
+// put in order by counting for each the larger ones.
 // Scores of different beams may lie close together, so sums, logarithms and
 // scores are fp64: exponentials of fp32 would be off by 2^-23 of a weight, and
-// one choice in some thousands would be another. An fp64 exponential is 16 of some
-// 24 instructions per id.
+// one choice in some thousands would be another. An fp64 exponential is 15 of some
+// 20 instructions per id.
 #pragma once
+
+#include <cfloat>
 
 #include "beam.h"
 #include "common.h"
@@ -33,27 +38,30 @@ struct BeamArgs {
     int* parents;
     int* tokens;
     float* out;
-    // per (row, piece): the sum and what its exponents were taken from; the largest logits' keys
-    unsigned char* ws;
-    int chunks;
+    // per (row, piece): its sum, and its largest logits' keys
+    struct BeamPiece* pieces;
+    u64* keys;
+    int chunks, batches;  // pieces of a row, batches of a piece
 };
-constexpr int BEAM_ROWS = 512, BEAM_WGS = 1024;  // rows a launch, workgroups that rows are cut into
+// What a piece of a row left beside `best` keys in descending order (0: no more): the
+// sum of exp(l - ref), ref one of its largest logits (-inf: no admissible id; +inf:
+// how many such logits there are).
+struct BeamPiece {
+    double sum;
+    float ref;
+};
+// Rows a launch takes at most, pieces that they are cut into, pieces of a group.
+constexpr int BEAM_ROWS = 512, BEAM_PIECES = 1024, BEAM_LISTS = 1024;
+constexpr int BEAM_BATCHES = 16;  // batches of a piece
 
 namespace bm {
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-struct Piece {
-    double sum;  // of exp(l - ref); ref = +inf: how many logits are
-    float ref;   // -inf: no admissible id
-    int n;       // keys
-    u64 key[BEAM_BEST];
-};
-
-// e^x for x <= 700 with a relative error of 2 10^-12 (x log2(e) as an integer
-// and a rest; 2^rest by Chebyshev interpolation of degree 8 on [-1/2, 1/2]).
-// Anything below -700, and NaN, counts as -700: 10^-304.
+// e^x for -700 <= x <= 700 with a relative error of 2 10^-12: x log2(e) as an
+// integer, by a sum with 1.5 2^52, and a rest; 2^rest by Chebyshev interpolation of
+// degree 8 on [-1/2, 1/2]; the integer is added to the exponent.
 __device__ __forceinline__ double exp_sum(double x) {
-    const double y = fmax(x, -700.0) * 1.4426950408889634074;
-    const double k = rint(y), f = y - k;
+    const double y = fma(x, 1.4426950408889634074, 6755399441055744.0);
+    const double f = fma(x, 1.4426950408889634074, -(y - 6755399441055744.0));
     double p = fma(f, 1.3255179556479267e-06, 1.5310080611926545e-05);
     p = fma(p, f, 0.00015403456082633648);
     p = fma(p, f, 0.0013333450563173552);
@@ -62,328 +70,478 @@ __device__ __forceinline__ double exp_sum(double x) {
     p = fma(p, f, 0.24022650695814518);
     p = fma(p, f, 0.6931471805459332);
     p = fma(p, f, 1.0);
-    return __builtin_amdgcn_ldexp(p, (int)k);
+    const u64 bits = __builtin_bit_cast(u64, p);
+    const int k = (int)__builtin_bit_cast(u64, y);
+    return __builtin_bit_cast(double, bits + ((u64)(unsigned)k << 52));
 }
 
-// A row of logits as a wave reads it: pieces of 16 bytes' worth of ids, counted
-// from the row's first id wherever that lies (16-byte loads need no alignment
-// here), so that a row's sums are the same at every address: beams that are
-// alike stay equal to the last bit.
-template <class T>
-struct Row {
-    static constexpr int EL = 16 / sizeof(T);
-    typedef unsigned Raw128 __attribute__((ext_vector_type(4), aligned(2)));
-    const T* row;
-    int V, whole, lo, hi;  // pieces all of whose ids there are; the wave's pieces lo .. hi - 1
-    const unsigned* never;
-    __device__ __forceinline__ Row(const BeamArgs& a, int r, int wave, int waves) {
-        row = static_cast<const T*>(a.logits) + (long long)r * a.ld;
-        V = a.V;
-        never = a.never;
-        whole = V / EL;
-        const int pieces = (V + EL - 1) / EL, per = ((pieces + waves - 1) / waves + 63) / 64 * 64;
-        lo = min(pieces, wave * per);
-        hi = min(pieces, lo + per);
-    }
-    struct Raw {
-        u32x4 x;
-        unsigned m;
-    };
-    // Piece v, or the last whole one instead, and the bits of its suppressed ids.
-    __device__ __forceinline__ Raw fetch(int v) const {
-        const int id0 = min(v, whole - 1) * EL;
-        Raw r;
-        r.x = *reinterpret_cast<const Raw128*>(row + id0);
-        r.m = never ? never[id0 >> 5] >> (id0 & 31) : 0;
-        return r;
-    }
-    // Its logits; -inf for suppressed ids, NaN, and ids that there are not.
-    __device__ __forceinline__ void unpack(int v, const Raw& r, float (&l)[EL]) const {
+// Bounds that at least k[i] (1 <= k[i] <= 64) of the lanes' numbers (no NaN) reach, and
+// few more: the k[i]-th largest, bit by bit (without branches: two searches beside
+// each other), its last 16 bits only if many share the first.
+__device__ __forceinline__ void bounds_of(float x, const int (&k)[2], float (&bound)[2]) {
+    const unsigned mine = f2ord(x);
+    unsigned t[2] = {0, 0};
+    int n[2] = {64, 64};
+    auto bits = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < EL; ++e) {
-            if constexpr (sizeof(T) == 4) l[e] = __uint_as_float(r.x[e]);
-            else l[e] = __uint_as_float(e & 1 ? r.x[e >> 1] & 0xffff0000u : r.x[e >> 1] << 16);
-            l[e] = ((r.m >> e) & 1u) || !(l[e] > -INFINITY) ? -INFINITY : l[e];
-        }
-        if (v >= whole || v >= hi) {
+        for (int b = from; b > from - 16; --b)
 #pragma unroll
-            for (int e = 0; e < EL; ++e) {
-                const int i = v * EL + e;
-                l[e] = -INFINITY;
-                if (v >= hi || i >= V) continue;
-                const float y = ldf(row + i);
-                l[e] = (never && (never[i >> 5] >> (i & 31) & 1u)) || !(y > -INFINITY) ? -INFINITY : y;
+            for (int i = 0; i < 2; ++i) {
+                const unsigned c = t[i] | 1u << b;
+                const int m = __popcll(__ballot(mine >= c));
+                t[i] = m >= k[i] ? c : t[i];
+                n[i] = m >= k[i] ? m : n[i];
             }
-        }
-    }
-    // f(id of the first, logits) for the wave's pieces, 64 at a time; the next D
-    // are on their way while one is worked on.
-    template <int D, class F>
-    __device__ __forceinline__ void each(int lane, F&& f) const {
-        Raw x[D];
+    };
+    bits(31);
+    if (n[0] > k[0] + 4 || n[1] > k[1] + 4) bits(15);
 #pragma unroll
-        for (int u = 0; u < D; ++u) x[u] = whole > 0 ? fetch(lo + lane + u * 64) : Raw{};
-#pragma unroll 1
-        for (int v0 = lo; v0 < hi; v0 += 64) {
-            const Raw now = x[0];
-#pragma unroll
-            for (int u = 0; u + 1 < D; ++u) x[u] = x[u + 1];
-            const int v = v0 + lane;
-            x[D - 1] = whole > 0 ? fetch(v + D * 64) : Raw{};
-            float l[EL];
-            unpack(v, now, l);
-            f(v * EL, l);
-        }
-    }
-};
-
-// Keys of a wave's or workgroup's largest logits, unordered: key[i] of n.
-// Moves the `best` largest to the front, in descending order (all of the
-// waves that share it call this; `lanes` threads of which this is number t).
-// Keys are distinct, so an entry's place is the number of larger ones.
-template <int CAP, int LANES, class Sync>
-__device__ __forceinline__ int keep_best(u64* key, int n, int best, int t, Sync&& sync) {
-    constexpr int PER = (CAP + LANES - 1) / LANES;
-    u64 mine[PER];
-    int place[PER];
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int i = t + u * LANES;
-        mine[u] = i < n ? key[i] : 0;
-        place[u] = 0;
-    }
-    const int turns = (n + LANES - 1) / LANES;
-    for (int j = 0; j < n; ++j) {
-        const u64 k = key[j];
-#pragma unroll
-        for (int u = 0; u < PER; ++u)
-            if (u < turns) place[u] += k > mine[u];
-    }
-    sync();
-#pragma unroll
-    for (int u = 0; u < PER; ++u)
-        if (t + u * LANES < n && place[u] < best) key[place[u]] = mine[u];
-    sync();
-    return n < best ? n : best;
+    for (int i = 0; i < 2; ++i) bound[i] = t[i] <= f2ord(-INFINITY) ? -INFINITY : ord2f(t[i]);
 }
 
-// The k-th largest (k >= 1) of the lanes' numbers.
-__device__ __forceinline__ float kth_largest(float x, int k, int lane) {
-    int before = 0;  // lanes with a larger number, or an equal one and a lower lane
+// Sum over the 64 lanes, the same in all.
+__device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-        const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i));
-        before += y > x || (y == x && i < lane);
-    }
-    const unsigned long long at = __ballot(before == k - 1);
-    return __shfl(x, __builtin_ctzll(at), 64);
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// A sum of exponentials taken from `from`, as one that is taken from `to` >= `from`.
+__device__ __forceinline__ double sum_from(double v, float from, float to) {
+    if (from == to) return v;
+    return from == -INFINITY || to == INFINITY ? 0.0 : v * exp_sum(fmax((double)from - (double)to, -700.0));
+}
+
+// A wave's LDS accesses are in order; this keeps the compiler's in order too.
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 }  // namespace bm
 
 // Whether a beam of that score is there.
 __device__ __forceinline__ bool beam_lives(float score) { return fabsf(score) < INFINITY; }
 
-template <class T>
-__global__ __launch_bounds__(bm::THREADS) void beam_rows_kernel(BeamArgs a) {
-    using namespace bm;
-    constexpr int EL = Row<T>::EL;
-    constexpr int FULL = 128, CAP = FULL + 64 * EL;  // a wave's keys: put in order when there are more than FULL
-    __shared__ u64 key[WAVES][CAP];
-    __shared__ double wsum[WAVES];
-    __shared__ float wref[WAVES];
-    __shared__ int wn[WAVES];
-    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (!beam_lives(a.scores[r])) return;
-    const Row<T> row(a, r, blockIdx.x * WAVES + wave, a.chunks * WAVES);
-    u64* mine = key[wave];
-    auto sync = [] {  // a wave's LDS accesses are in order; the compiler keeps them so
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    };
-    float ref = -INFINITY, thr = -INFINITY;
-    double sum = 0.0;
-    int n = 0;
-    row.template each<4>(lane, [&](int i0, const float (&l)[EL]) __attribute__((always_inline)) {
-        float mx = l[0];
-#pragma unroll
-        for (int e = 1; e < EL; ++e) mx = fmaxf(mx, l[e]);
-        if (mx > ref + 100.f) {  // exponents are small enough for fp64 till then
-            sum = ref == -INFINITY ? 0.0 : sum * exp_sum((double)ref - (double)mx);
-            if (mx == INFINITY) sum = 0.0;
-            ref = mx;
-        }
-        if (ref == INFINITY) {
-#pragma unroll
-            for (int e = 0; e < EL; ++e) sum += l[e] == INFINITY ? 1.0 : 0.0;
-        } else if (ref > -INFINITY) {
-#pragma unroll
-            for (int e = 0; e < EL; ++e) sum += exp_sum((double)l[e] - (double)ref);
-        }
-        // logits above the wave's n-th largest so far
-        unsigned long long some = __ballot(mx > thr);
-        if (!some) return;
-        if (__popcll(some) > FULL / 4) {  // too many to list: at least n are no smaller than the n-th largest lane's
-            const float x = kth_largest(mx, a.best, lane);
-            if (x > thr) thr = x == 0.f ? -1e-45f : ord2f(f2ord(x) - 1);  // (equal ones count)
-        }
-#pragma unroll
-        for (int e = 0; e < EL; ++e) {
-            const unsigned long long in = __ballot(l[e] > thr);
-            if (l[e] > thr)
-                mine[n + __popcll(in & ((1ull << lane) - 1))] = amax_key(l[e] + 0.f, i0 + e);  // (-0 and 0 are equal)
-            n += __popcll(in);
-        }
-        if (n > FULL) {
-            sync();
-            n = keep_best<CAP, 64>(mine, n, a.best, lane, sync);
-            if (n == a.best) thr = fmaxf(thr, ord2f((uint32_t)(mine[n - 1] >> 32)));
-        }
-    });
-    // the lanes' sums to one exponent: the largest of theirs
-    const float top = wave_max(ref);
-    if (top == INFINITY) sum = ref == INFINITY ? sum : 0.0;
-    else sum = ref == -INFINITY ? 0.0 : sum * exp_sum((double)ref - (double)top);
-#pragma unroll
-    for (int st = 32; st > 0; st >>= 1) sum += __shfl_xor(sum, st, 64);
-    sync();
-    n = keep_best<CAP, 64>(mine, n, a.best, lane, sync);
-    if (lane == 0) {
-        wsum[wave] = sum;
-        wref[wave] = top;
-        wn[wave] = n;
-    }
-    __syncthreads();
-    // the waves' lists as one
-    const float t = fmaxf(fmaxf(wref[0], wref[1]), fmaxf(wref[2], wref[3]));
-    Piece& out = reinterpret_cast<Piece*>(a.ws)[(long long)r * a.chunks + blockIdx.x];
-    int total = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) total += wn[w];
-    // thread: one key of a wave (best <= 64)
-    if (lane < wn[wave]) {
-        const u64 k = mine[lane];
-        int place = lane;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            if (w == wave) continue;
-            for (int j = 0; j < wn[w]; ++j) place += key[w][j] > k;
-        }
-        if (place < a.best) out.key[place] = k;
-    }
-    if (tid == 0) {
-        double y = 0.0;
-        for (int w = 0; w < WAVES; ++w) {
-            if (wref[w] == -INFINITY) continue;
-            if (t == INFINITY) y += wref[w] == INFINITY ? wsum[w] : 0.0;
-            else y += wsum[w] * exp_sum((double)wref[w] - (double)t);
-        }
-        out.sum = y;
-        out.ref = t;
-        out.n = min(total, a.best);
+// Places of n numbers in descending order, by counting the larger ones: calls
+// f(i, place) for those whose place is below `best` (all 256 threads call this;
+// larger(j, i): whether number j comes before number i). Where there are fewer than
+// 256, several lanes share a number's count.
+template <class L, class F>
+__device__ __forceinline__ void in_order(int n, int best, L&& larger, F&& f) {
+    const int lg = n > 128 ? 0 : n > 64 ? 1 : n > 32 ? 2 : 3, team = 1 << lg;
+    const int sub = threadIdx.x & (team - 1);
+    for (int i = threadIdx.x >> lg; i - (int)(threadIdx.x >> lg) < n; i += bm::THREADS >> lg) {
+        int place = 0;
+        if (i < n)
+#pragma unroll 8
+            for (int j = sub; j < n; j += team) place += larger(j, i);
+        for (int st = 1; st < team; st <<= 1) place += __shfl_xor(place, st, 64);
+        if (i < n && sub == 0 && place < best) f(i, place);
     }
 }
 
-// A group's n best from its pieces' lists (each in descending order). Lists as
-// long as j + 1 hold at least (lists) (j + 1) continuations no worse than their
-// j-th, so one of those entries is a bound below which nothing can be among
-// the n best; what is left is put in order by counting.
-static __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
+// A workgroup goes through its piece once, every wave through its part in batches of
+// U 16-byte loads a lane, the next one's under way: it adds up exponentials, from
+// its first batch's largest logit on, and keeps a lane's largest logit of every
+// batch in LDS. What passes the bound that these give is then read again: as a rule
+// some 30 lanes' batches, a thread each; where many logits are equal, everything,
+// a wave's list being cut to its n largest when it is full. NEVER: some ids are
+// suppressed. Ids are counted from the row's first wherever that lies (16-byte
+// loads need no alignment here), so that a row's sums are the same at every
+// address: beams that are alike stay equal to the last bit.
+template <class T, int U, bool NEVER>
+__global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
     using namespace bm;
-    constexpr int CAP = BEAM_WGS;  // lists at most
-    __shared__ double off[BEAM_WIDTH];   // score - log(sum)
-    __shared__ float refs[BEAM_WIDTH];
+    constexpr int EL = 16 / sizeof(T), CAP = 192;  // keys of a wave
+    static_assert(CAP >= BEAM_BEST + 64, "a list has room for one number of every lane");
+    typedef unsigned Raw128 __attribute__((ext_vector_type(4), aligned(2)));
+    __shared__ u64 key[WAVES * CAP], joined[WAVES * CAP];
+    __shared__ float most[BEAM_BATCHES][THREADS];
+    __shared__ int pair[THREADS];
+    __shared__ double wsum[WAVES];
+    __shared__ float wref[WAVES], wbound[2][WAVES];
+    __shared__ int wn[WAVES], pairs, count;
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (!beam_lives(a.scores[r])) return;
+    const T* row = static_cast<const T*>(a.logits) + (long long)r * a.ld;
+    const int whole = a.V / EL;
+    // the ids behind the last whole 16 bytes: one a lane of the last piece's first wave (NaN counts as -inf)
+    float lx = -INFINITY;
+    const int ix = whole * EL + tid;
+    if (blockIdx.x == gridDim.x - 1 && ix < a.V) {
+        lx = fmaxf(ldf(row + ix), -INFINITY);
+        if (NEVER && (a.never[ix >> 5] >> (ix & 31) & 1u)) lx = -INFINITY;
+    }
+    // (a row of less than 16 bytes is all behind: what is loaded is not looked at)
+    const T* from = whole > 0 ? row : reinterpret_cast<const T*>(a.keys);
+    // the first 16 bytes of a thread's batch, a batch's loads, and its logits
+    auto start = [&](int t, int bt) __attribute__((always_inline)) {
+        return ((blockIdx.x * WAVES + (t >> 6)) * a.batches + bt) * U * 64 + (t & 63);
+    };
+    auto fetch = [&](int v0, u32x4 (&x)[U], unsigned (&m)[U]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id0 = max(0, min(v0 + u * 64, whole - 1)) * EL;
+            x[u] = *reinterpret_cast<const Raw128*>(from + id0);
+            if constexpr (NEVER) m[u] = a.never[id0 >> 5] >> (id0 & 31);
+            else m[u] = 0;
+        }
+    };
+    auto unpack = [&](int v0, const u32x4 (&x)[U], const unsigned (&m)[U], float (&l)[U][EL]) __attribute__((always_inline)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // suppressed ids, and those behind the row's, are few
+            const unsigned out = v0 + u * 64 < whole ? m[u] & ((1u << EL) - 1) : ~0u;
+#pragma unroll
+            for (int e = 0; e < EL; ++e) {
+                float y;
+                if constexpr (sizeof(T) == 4) y = __uint_as_float(x[u][e]);
+                else y = __uint_as_float(e & 1 ? x[u][e >> 1] & 0xffff0000u : x[u][e >> 1] << 16);
+                l[u][e] = fmaxf(y, -INFINITY);
+            }
+            if (out)
+#pragma unroll
+                for (int e = 0; e < EL; ++e) l[u][e] = (out >> e) & 1u ? -INFINITY : l[u][e];
+#pragma unroll
+            for (int e = 0; e < EL; ++e) mx = fmaxf(mx, l[u][e]);
+        }
+        return mx;
+    };
+    u32x4 x[U];
+    unsigned m[U];
+    float l[U][EL];
+    fetch(start(tid, 0), x, m);
+    float ref = -INFINITY, all_most = lx;
+    double sum = 0.0;
+#pragma unroll 1
+    for (int bt = 0; bt < a.batches; ++bt) {
+        const int v0 = start(tid, bt);
+        const float last = bt == a.batches - 1 ? lx : -INFINITY;
+        float mx = unpack(v0, x, m, l);
+        most[bt][tid] = mx;
+        mx = fmaxf(mx, last);
+        all_most = fmaxf(all_most, mx);
+        if (bt + 1 < a.batches) fetch(v0 + U * 64, x, m);
+        // (fp64 has room for exponents up to there)
+        if (__any(mx > ref + 500.f)) {
+            const float t = wave_max(mx);
+            sum = ref == -INFINITY || t == INFINITY ? 0.0 : sum * exp_sum(fmax((double)ref - (double)t, -700.0));
+            ref = t;
+        }
+        if (ref < INFINITY && ref > -INFINITY) {
+            const double base = ref;
+            if (last > -INFINITY) sum += exp_sum(fmax((double)last - base, -700.0));
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < EL; e += 4) {
+#pragma unroll
+                    for (int i = e; i < e + 4; ++i) sum += exp_sum(fmax((double)l[u][i] - base, -700.0));
+                    __builtin_amdgcn_sched_barrier(0);  // four at a time: more would take more registers than there are
+                }
+        } else if (ref == INFINITY) {
+            sum += last == INFINITY ? 1.0 : 0.0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < EL; ++e) sum += l[u][e] == INFINITY ? 1.0 : 0.0;
+        }
+    }
+    {
+        const int k[2] = {a.best, (a.best + WAVES - 1) / WAVES};
+        float y[2];
+        bounds_of(all_most, k, y);
+        sum = wave_sum_f64(sum);
+        if (lane == 0) {
+            wbound[0][wave] = y[0];
+            wbound[1][wave] = y[1];
+            wsum[wave] = sum;
+            wref[wave] = ref;
+        }
+        if (tid == 0) pairs = count = 0;
+    }
+    __syncthreads();
+    // `best` logits of one wave, or a quarter of them of every wave's
+    float bound = INFINITY;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) bound = fminf(bound, wbound[1][w]);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) bound = fmaxf(bound, wbound[0][w]);
+    bound = fmaxf(bound, -FLT_MAX);
+    for (int bt = 0; bt < a.batches; ++bt)
+        if (most[bt][tid] >= bound) {
+            const int p = atomicAdd(&pairs, 1);
+            if (p < THREADS) pair[p] = bt << 8 | tid;
+        }
+    __syncthreads();
+    int n = THREADS * CAP;  // keys that were listed: too many till then
+    if (pairs <= THREADS) {
+        auto put = [&](float y, int id) __attribute__((always_inline)) {
+            if (!(y >= bound)) return;
+            const int p = atomicAdd(&count, 1);
+            if (p < WAVES * CAP) joined[p] = amax_key(y + 0.f, id);  // (-0 and 0 are equal)
+        };
+        if (tid < pairs) {
+            const int v0 = start(pair[tid] & 255, pair[tid] >> 8);
+            fetch(v0, x, m);
+            unpack(v0, x, m, l);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < EL; ++e) put(l[u][e], (v0 + u * 64) * EL + e);
+        }
+        put(lx, ix);
+        __syncthreads();
+        n = count;
+    }
+    if (n > WAVES * CAP) {
+        u64* mine = key + wave * CAP;
+        int bound_id = 0x7fffffff;  // of those equal to the bound, lower ids pass
+        n = 0;
+        // lists the lanes' logits that pass; where the list is full, its `best` largest
+        // are kept, and the last of them is the bound from then on
+        auto list = [&](float y, int id) __attribute__((always_inline)) {
+            auto passes = [&]() __attribute__((always_inline)) { return (y > bound) | ((y == bound) & (id < bound_id)); };
+            unsigned long long in = __ballot(passes());
+            if (!in) return;
+            if (n + __popcll(in) > CAP) {
+                u64 own[CAP / 64];
+                int place[CAP / 64];
+#pragma unroll
+                for (int i = 0; i < CAP / 64; ++i) {
+                    own[i] = lane + i * 64 < n ? mine[lane + i * 64] : 0;
+                    place[i] = own[i] ? 0 : a.best;
+                }
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
+                    const u64 k = mine[j];
+#pragma unroll
+                    for (int i = 0; i < CAP / 64; ++i) place[i] += k > own[i];
+                }
+                wave_lds_fence();
+#pragma unroll
+                for (int i = 0; i < CAP / 64; ++i)
+                    if (place[i] < a.best) mine[place[i]] = own[i];
+                wave_lds_fence();
+                n = a.best;
+                const u64 k = mine[n - 1];
+                bound = ord2f((uint32_t)(k >> 32));
+                bound_id = (int)(0xffffffffu - (unsigned)k);
+                in = __ballot(passes());
+            }
+            if (passes()) mine[n + __popcll(in & ((1ull << lane) - 1))] = amax_key(y + 0.f, id);
+            n += __popcll(in);
+        };
+#pragma unroll 1
+        for (int bt = 0; bt < a.batches; ++bt) {
+            if (!__any(most[bt][tid] >= bound)) continue;
+            const int v0 = start(tid, bt);
+            fetch(v0, x, m);
+            unpack(v0, x, m, l);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < EL; ++e) list(l[u][e], (v0 + u * 64) * EL + e);
+        }
+        list(lx, ix);
+        if (lane == 0) wn[wave] = n;
+        __syncthreads();
+        // the waves' lists as one
+        int to = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            for (int i = tid; i < wn[w]; i += THREADS) joined[to + i] = key[w * CAP + i];
+            to += wn[w];
+        }
+        n = to;
+        __syncthreads();
+    }
+    const long long at = (long long)r * a.chunks + blockIdx.x;
+    u64* out = a.keys + at * a.best;
+    in_order(n, a.best, [&](int j, int i) { return joined[j] > joined[i]; }, [&](int i, int place) { out[place] = joined[i]; });
+    for (int i = n + tid; i < a.best; i += THREADS) out[i] = 0;
+    if (tid == 0) {
+        const float t = fmaxf(fmaxf(wref[0], wref[1]), fmaxf(wref[2], wref[3]));
+        double y = 0.0;
+        for (int w = 0; w < WAVES; ++w) y += sum_from(wsum[w], wref[w], t);
+        a.pieces[at] = BeamPiece{y, t};
+    }
+}
+
+// A group's n best from its pieces' lists (each in descending order). A list whose
+// j-th entry is some score has j + 1 continuations no worse, so the k-th largest of
+// the lists' j-th entries, k (j + 1) >= n, is a bound that n continuations reach
+// (rounded down to fp32, it still is). What reaches it is put in order by counting.
+// Bound by the latency of two rounds of loads and of the counting.
+static __global__ __launch_bounds__(bm::THREADS) void beam_pick_kernel(BeamArgs a) {
+    using namespace bm;
+    constexpr int CAP = 1024, PER = BEAM_LISTS / 256, FEW = BEAM_BEST;
+    __shared__ double off[BEAM_WIDTH];  // log of the row's sum
+    __shared__ float refs[BEAM_WIDTH], score[BEAM_WIDTH];
     __shared__ double val[CAP];
-    __shared__ int idx[CAP];
-    __shared__ double bound[4];
-    __shared__ int count;
+    __shared__ int idx[CAP], act[BEAM_LISTS];
+    __shared__ float head[256];
+    __shared__ double red[4];
+    __shared__ int redi[4];
     __shared__ double sh_val;
-    __shared__ int sh_idx;
+    __shared__ int count, n_act, sh_idx;
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Piece* pieces = reinterpret_cast<const Piece*>(a.ws) + (long long)g * a.width * a.chunks;
     const int lists = a.width * a.chunks;
-    // a wave per row
-    for (int b = wave; b < a.width; b += 4) {
-        const float c = a.scores[g * a.width + b];
+    const BeamPiece* pieces = a.pieces + (long long)g * lists;
+    const u64* keys = a.keys + (long long)g * lists * a.best;
+    u64 first[PER];  // of lists tid, tid + 256, ...
+#pragma unroll
+    for (int s = 0; s < PER; ++s) first[s] = tid + s * 256 < lists ? keys[(long long)(tid + s * 256) * a.best] : 0;
+    {
+        // eight lanes per row, four pieces each at a time
+        const int b = tid >> 3, sub = tid & 7;
+        const float c = b < a.width ? a.scores[g * a.width + b] : -INFINITY;
         float t = -INFINITY;
         double y = 0.0;
-        if (beam_lives(c)) {
-            for (int k = lane; k < a.chunks; k += 64) t = fmaxf(t, pieces[b * a.chunks + k].ref);
-            t = wave_max(t);
-            for (int k = lane; k < a.chunks; k += 64) {
-                const Piece& p = pieces[b * a.chunks + k];
-                if (p.ref == -INFINITY) continue;
-                if (t == INFINITY) y += p.ref == INFINITY ? p.sum : 0.0;
-                else y += p.sum * exp_sum((double)p.ref - (double)t);
-            }
+        if (b < a.width) {
+            for (int k0 = sub; k0 < a.chunks; k0 += 32) {
+                BeamPiece p[4];
 #pragma unroll
-            for (int st = 32; st > 0; st >>= 1) y += __shfl_xor(y, st, 64);
+                for (int s = 0; s < 4; ++s) p[s] = pieces[b * a.chunks + min(k0 + 8 * s, a.chunks - 1)];
+                float to = t;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) to = fmaxf(to, p[s].ref);
+                y = sum_from(y, t, to);
+                t = to;
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    if (k0 + 8 * s < a.chunks) y += sum_from(p[s].sum, p[s].ref, t);
+            }
         }
-        if (lane == 0) {
+        {
+            float to = t;
+#pragma unroll
+            for (int st = 1; st < 8; st <<= 1) to = fmaxf(to, __shfl_xor(to, st, 64));
+            y = sum_from(y, t, to);
+            t = beam_lives(c) ? to : -INFINITY;  // (what pieces of a beam that is not there hold is left over)
+#pragma unroll
+            for (int st = 1; st < 8; st <<= 1) y += __shfl_xor(y, st, 64);
+        }
+        if (sub == 0 && b < a.width) {
             refs[b] = t;  // -inf: no continuation
+            score[b] = c;
             off[b] = t == -INFINITY ? 0.0 : log(y);
         }
     }
-    if (tid == 0) count = 0;
+    if (tid == 0) count = n_act = 0;
     __syncthreads();
-    // entry e of list i (i = row * chunks + piece): its score, or -inf
-    auto score = [&](int i, int e, int& at) __attribute__((always_inline)) {
-        const int b = i / a.chunks;
-        at = 0x7fffffff;
-        if (refs[b] == -INFINITY || e >= pieces[i].n) return -(double)INFINITY;
-        const u64 k = pieces[i].key[e];
+    // the continuation of a key of row b: its score, or -inf for none (keys of beams
+    // that are not there are not read as such)
+    auto total = [&](int b, u64 k) __attribute__((always_inline)) {
         const float l = ord2f((uint32_t)(k >> 32));
-        if (refs[b] == INFINITY && l != INFINITY) return -(double)INFINITY;
-        const int id = (int)(0xffffffffu - (unsigned)k);
-        at = b * a.V + id;
-        return (double)a.scores[g * a.width + b] + ((refs[b] == INFINITY ? 0.0 : (double)l - (double)refs[b]) - off[b]);
+        if (refs[b] == -INFINITY || k == 0 || (refs[b] == INFINITY && l != INFINITY)) return -(double)INFINITY;
+        return (double)score[b] + ((refs[b] == INFINITY ? 0.0 : (double)l - (double)refs[b]) - off[b]);
     };
-    // the bound: the k-th largest of the lists' j-th entries, k (j + 1) >= best
-    const int j = (a.best + lists - 1) / lists - 1, k = (a.best + j) / (j + 1);
-    for (int i = tid; i < lists; i += 256) {
-        int at;
-        val[i] = score(i, j, at);
+    auto place_of = [&](int b, u64 k) __attribute__((always_inline)) { return b * a.V + (int)(0xffffffffu - (unsigned)k); };
+    auto below = [](double x) __attribute__((always_inline)) {  // rounded down
+        const float f = (float)x;
+        return (double)f > x ? ord2f(f2ord(f) - 1) : f;
+    };
+    // a bound that at least k of the threads' numbers reach: the k-th largest to 16
+    // bits (every wave finds it by itself)
+    auto kth = [&](float x, int k) __attribute__((always_inline)) {
+        head[tid] = x;
+        __syncthreads();
+        unsigned v[4], t = 0;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) v[s] = f2ord(head[lane + s * 64]);
+#pragma unroll
+        for (int b = 31; b > 15; --b) {
+            const unsigned c = t | 1u << b;
+            int m = 0;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) m += __popcll(__ballot(v[s] >= c));
+            t = m >= k ? c : t;
+        }
+        __syncthreads();
+        return t <= f2ord(-INFINITY) ? -INFINITY : ord2f(t);
+    };
+    float heads[PER], most = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < PER; ++s) {
+        heads[s] = -INFINITY;
+        if (first[s]) heads[s] = below(total((tid + s * 256) / a.chunks, first[s]));
+        most = fmaxf(most, heads[s]);
     }
-    __syncthreads();
-    for (int i = tid; i < lists; i += 256) {
-        const double x = val[i];
-        int before = 0;
-        for (int q = 0; q < lists; ++q) before += val[q] > x || (val[q] == x && q < i);
-        if (before == k - 1) bound[0] = x;
-    }
-    __syncthreads();
-    const double low = bound[0];
-    __syncthreads();
-    for (int i = tid; i < lists; i += 256) {
-        for (int e = 0; e < a.best; ++e) {
-            int at;
-            const double x = score(i, e, at);
-            if (!(x >= low) || x == -(double)INFINITY) break;  // lists descend
-            const int p = atomicAdd(&count, 1);
-            if (p < CAP) {
-                val[p] = x;
-                idx[p] = at;
+    const int live = __syncthreads_count(most > -INFINITY);
+    if (live > 0) {
+        int k = a.best;
+        if (live < a.best) {  // further down the lists
+            const int j = (a.best + live - 1) / live - 1;
+            k = (a.best + j) / (j + 1);
+            most = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < PER; ++s) {
+                const int i = tid + s * 256;
+                if (heads[s] > -INFINITY) most = fmaxf(most, below(total(i / a.chunks, keys[(long long)i * a.best + j])));
             }
         }
+        const float low = kth(most, k);
+        // lists that reach the bound, and their entries that do
+#pragma unroll
+        for (int s = 0; s < PER; ++s)
+            if (heads[s] >= low && heads[s] > -INFINITY) act[atomicAdd(&n_act, 1)] = tid + s * 256;
+        __syncthreads();
+        const int all = n_act * a.best;
+        for (int q = tid; q < all; q += 256) {
+            const int i = act[q / a.best], b = i / a.chunks;
+            const u64 key = keys[(long long)i * a.best + q % a.best];
+            const double x = total(b, key);
+            if (x >= (double)low && x > -(double)INFINITY) {
+                const int p = atomicAdd(&count, 1);
+                if (p < CAP) {
+                    val[p] = x;
+                    idx[p] = place_of(b, key);
+                }
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    const int n = count;
-    int* parents = a.parents + g * a.best;
-    int* tokens = a.tokens + g * a.best;
-    float* out = a.out + g * a.best;
+    int n = count;
+    if (n > FEW && n <= CAP) {
+        // a bound from among them: each thread's largest
+        double own[CAP / 256];
+        int at[CAP / 256];
+        float x = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < CAP / 256; ++s) {
+            const int i = tid + s * 256;
+            own[s] = i < n ? val[i] : -(double)INFINITY;
+            at[s] = i < n ? idx[i] : 0;
+            x = fmaxf(x, below(own[s]));
+        }
+        const float low = kth(x, a.best);
+        if (tid == 0) count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < CAP / 256; ++s)
+            if (tid + s * 256 < n && own[s] >= (double)low) {
+                const int p = atomicAdd(&count, 1);
+                val[p] = own[s];
+                idx[p] = at[s];
+            }
+        __syncthreads();
+        n = count;
+    }
+    int* parents = a.parents + (long long)g * a.best;
+    int* tokens = a.tokens + (long long)g * a.best;
+    float* out = a.out + (long long)g * a.best;
     auto put = [&](int place, double x, int at) __attribute__((always_inline)) {
         parents[place] = at / a.V;
         tokens[place] = at - at / a.V * a.V;
         out[place] = (float)x;
     };
     if (n <= CAP) {
-        for (int i = tid; i < n; i += 256) {
-            const double x = val[i];
-            const int at = idx[i];
-            int place = 0;
-            for (int q = 0; q < n; ++q) place += val[q] > x || (val[q] == x && idx[q] < at);
-            if (place < a.best) put(place, x, at);
-        }
+        in_order(n, a.best, [&](int j, int i) { return (int)(val[j] > val[i]) | ((int)(val[j] == val[i]) & (int)(idx[j] < idx[i])); },
+                 [&](int i, int place) { put(place, val[i], idx[i]); });
         for (int i = n + tid; i < a.best; i += 256) {
             parents[i] = tokens[i] = -1;
             out[i] = -INFINITY;
@@ -397,12 +555,14 @@ static __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
         double bx = -(double)INFINITY;
         int bi = 0x7fffffff;
         for (int i = tid; i < lists; i += 256) {
+            const int b = i / a.chunks;
             for (int e = 0; e < a.best; ++e) {
-                int at;
-                const double x = score(i, e, at);
-                if (x == -(double)INFINITY) break;
+                const u64 key = keys[(long long)i * a.best + e];
+                const double x = total(b, key);
+                if (x == -(double)INFINITY || x < bx) break;
+                const int at = place_of(b, key);
                 if (x > last || (x == last && at <= last_at)) continue;  // chosen already
-                if (x > bx || (x == bx && at < bi)) {
+                if (x > bx || at < bi) {
                     bx = x;
                     bi = at;
                 }
@@ -418,24 +578,19 @@ static __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
             }
         }
         if (lane == 0) {
-            bound[wave] = bx;
-            idx[wave] = bi;
+            red[wave] = bx;
+            redi[wave] = bi;
         }
         __syncthreads();
         if (tid == 0) {
             for (int w = 1; w < 4; ++w)
-                if (bound[w] > bound[0] || (bound[w] == bound[0] && idx[w] < idx[0])) {
-                    bound[0] = bound[w];
-                    idx[0] = idx[w];
+                if (red[w] > red[0] || (red[w] == red[0] && redi[w] < redi[0])) {
+                    red[0] = red[w];
+                    redi[0] = redi[w];
                 }
-            sh_val = bound[0];
-            sh_idx = idx[0];
-            if (bound[0] > -(double)INFINITY) {
-                put(m, bound[0], idx[0]);
-            } else {
-                parents[m] = tokens[m] = -1;
-                out[m] = -INFINITY;
-            }
+            sh_val = red[0];
+            sh_idx = redi[0];
+            put(m, red[0], redi[0]);  // (there are more than CAP >= best)
         }
         __syncthreads();
         last = sh_val;
@@ -443,20 +598,27 @@ static __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
     }
 }
 
-// Workgroups that a row of V logits is cut over when n rows are looked at: as
-// many as fill 256 CUs four times, if every wave has 128 pieces of 16 bytes.
-template <class T>
-inline int beam_chunks(int n, int V) {
-    const int pieces = V / (16 / (int)sizeof(T)) + 1;
-    const int most = (pieces + 128 * bm::WAVES - 1) / (128 * bm::WAVES), want = BEAM_WGS / n;
-    return most < want ? most : want;
+// A launch's pieces: what 1024 workgroups (four per CU) take in batches of 16 ids a
+// thread, or, where that gives fewer than one per CU, in batches of 8 ids.
+template <class T, int U>
+inline void beam_launch(BeamArgs a, int n, int groups, int loads, hipStream_t st) {
+    const int most = (loads + U * bm::THREADS - 1) / (U * bm::THREADS);
+    int c = BEAM_PIECES / n < BEAM_LISTS / a.width ? BEAM_PIECES / n : BEAM_LISTS / a.width;
+    if (c > most) c = most;
+    a.batches = (most + c - 1) / c;
+    a.chunks = (most + a.batches - 1) / a.batches;
+    if (a.never) hipLaunchKernelGGL((beam_rows_kernel<T, U, true>), dim3(a.chunks, n), dim3(bm::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((beam_rows_kernel<T, U, false>), dim3(a.chunks, n), dim3(bm::THREADS), 0, st, a);
+    hipLaunchKernelGGL(beam_pick_kernel, dim3(groups), dim3(256), 0, st, a);
 }
-// Workspace of a launch, of up to BEAM_ROWS rows cut into up to BEAM_WGS pieces.
-inline size_t beam_ws_bytes() { return sizeof(bm::Piece) * (size_t)BEAM_WGS; }
-static_assert(BEAM_ROWS <= BEAM_WGS, "a piece per row at least");
+inline size_t beam_ws_bytes() { return (sizeof(BeamPiece) + sizeof(u64) * BEAM_BEST) * (size_t)BEAM_PIECES; }
 template <class T>
 inline void beam_rows(BeamArgs a, int groups, hipStream_t st) {
-    const int most = BEAM_ROWS / a.width;  // groups of a launch
+    constexpr int U = sizeof(T);
+    const int loads = (int)((a.V * (long long)sizeof(T) + 15) / 16);
+    // pieces of BEAM_BATCHES batches have to do for a launch's rows
+    const int least = (loads + BEAM_BATCHES * U * bm::THREADS - 1) / (BEAM_BATCHES * U * bm::THREADS);
+    const int rows = BEAM_PIECES / least < BEAM_ROWS ? BEAM_PIECES / least : BEAM_ROWS, most = rows / a.width;
     for (int g = 0; g < groups; g += most) {
         const int m = groups - g < most ? groups - g : most, n = m * a.width;
         BeamArgs b = a;
@@ -465,10 +627,11 @@ inline void beam_rows(BeamArgs a, int groups, hipStream_t st) {
         b.parents += (long long)g * a.best;
         b.tokens += (long long)g * a.best;
         b.out += (long long)g * a.best;
-        b.chunks = beam_chunks<T>(n, a.V);
-        hipLaunchKernelGGL(beam_rows_kernel<T>, dim3(b.chunks, n), dim3(bm::THREADS), 0, st, b);
-        hipLaunchKernelGGL(beam_pick_kernel, dim3(m), dim3(256), 0, st, b);
+        if ((long long)n * loads >= 256LL * U * bm::THREADS) beam_launch<T, U>(b, n, m, loads, st);
+        else beam_launch<T, U / 2>(b, n, m, loads, st);
     }
 }
+// the widest group over the widest vocabulary (2^20 ids of 4 bytes) fits a launch, and so its pieces' lists
+static_assert(BEAM_PIECES / ((1 << 18) / (BEAM_BATCHES * 4 * bm::THREADS)) >= BEAM_WIDTH && BEAM_PIECES <= BEAM_LISTS, "");
 
 }  // namespace wmi
