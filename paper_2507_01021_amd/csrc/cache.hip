@@ -35,6 +35,9 @@ constexpr int ATTN_PART = 512;
 // some 7 us where it is faster (few sequences, short contexts) and lose several
 // times the time where it is not; below, it loses with many sequences too.
 constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
+// Rows of a tile, on average, up to which the packed cache's append takes the
+// kernel of few rows.
+constexpr int FEW_ROWS = 4;
 // Most workgroups of a launch along its list (a grid holds fewer than 2^32
 // threads): the kernels go through longer lists in strides.
 constexpr int MOST_WGS = 1 << 22;
@@ -550,6 +553,16 @@ class PagedCacheT final : public PagedCache {
         else move_d<IN, 128>(layer, list, n, k, v, k_ld, v_ld, n_rows);
         WMI_HIP(hipGetLastError());
     }
+    template <int D, int BITS, class G, class F>
+    void append_packed(G& go, F& go_flat, bool vec, bool few, dim3& grid, const T* k, const T* v) {
+        if (few) {
+            const long long rows = 2LL * grid.x * P_.n_kv_head;  // (of keys or values; 256 / (D / 8) a workgroup)
+            grid = dim3((unsigned)std::min<long long>((rows * (D / 8) + 255) / 256, MOST_WGS), 1, grid.z);
+            vec ? go(packed_append_few_kernel<T, D, BITS, true>, k, v) : go(packed_append_few_kernel<T, D, BITS, false>, k, v);
+        } else {
+            vec ? go_flat(packed_append_kernel<T, D, BITS, true>, k, v) : go_flat(packed_append_kernel<T, D, BITS, false>, k, v);
+        }
+    }
     template <bool IN, int D>
     void move_d(int layer, const int* list, int n, const void* k, const void* v, int64_t k_ld, int64_t v_ld, int n_rows) {
         const int l0 = layer < 0 ? 0 : layer, nl = layer < 0 ? P_.n_layer : 1;
@@ -557,19 +570,27 @@ class PagedCacheT final : public PagedCache {
         constexpr int EL = 16 / sizeof(T);
         const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0 && k_ld % EL == 0 &&
                          v_ld % EL == 0;
-        const dim3 grid(std::min(n, MOST_WGS), P_.n_kv_head, nl), block(256);
+        dim3 grid(std::min(n, MOST_WGS), P_.n_kv_head, nl), block(256);
+        // tiles of few rows, on average, go to the kernel of few rows
+        const bool few = IN && bits_ && n_rows <= FEW_ROWS * (long long)n_tiles_;
         auto go = [&](auto kernel, auto* kk, auto* vv) {
             hipLaunchKernelGGL(kernel, grid, block, 0, st_, view(), list, l0, kk, vv, k_ld, v_ld, kl, vl);
         };
+        // packed: a wave per (tile, keys or values, head) and layer
+        auto go_flat = [&](auto kernel, auto* kk, auto* vv) {
+            const long long wgs = (2LL * n * P_.n_kv_head * nl + 3) / 4;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<long long>(wgs, MOST_WGS)), block, 0, st_, view(), list, l0, kk, vv,
+                               k_ld, v_ld, kl, vl, nl);
+        };
         if constexpr (IN) {
             const T *kk = static_cast<const T*>(k), *vv = static_cast<const T*>(v);
-            if (bits_ == 4) vec ? go(packed_append_kernel<T, D, 4, true>, kk, vv) : go(packed_append_kernel<T, D, 4, false>, kk, vv);
-            else if (bits_ == 8) vec ? go(packed_append_kernel<T, D, 8, true>, kk, vv) : go(packed_append_kernel<T, D, 8, false>, kk, vv);
+            if (bits_ == 4) append_packed<D, 4>(go, go_flat, vec, few, grid, kk, vv);
+            else if (bits_ == 8) append_packed<D, 8>(go, go_flat, vec, few, grid, kk, vv);
             else vec ? go(paged_append_kernel<T, D, true>, kk, vv) : go(paged_append_kernel<T, D, false>, kk, vv);
         } else {
             T *kk = static_cast<T*>(const_cast<void*>(k)), *vv = static_cast<T*>(const_cast<void*>(v));
-            if (bits_ == 4) vec ? go(packed_read_kernel<T, D, 4, true>, kk, vv) : go(packed_read_kernel<T, D, 4, false>, kk, vv);
-            else if (bits_ == 8) vec ? go(packed_read_kernel<T, D, 8, true>, kk, vv) : go(packed_read_kernel<T, D, 8, false>, kk, vv);
+            if (bits_ == 4) vec ? go_flat(packed_read_kernel<T, D, 4, true>, kk, vv) : go_flat(packed_read_kernel<T, D, 4, false>, kk, vv);
+            else if (bits_ == 8) vec ? go_flat(packed_read_kernel<T, D, 8, true>, kk, vv) : go_flat(packed_read_kernel<T, D, 8, false>, kk, vv);
             else vec ? go(paged_read_kernel<T, D, true>, kk, vv) : go(paged_read_kernel<T, D, false>, kk, vv);
         }
     }

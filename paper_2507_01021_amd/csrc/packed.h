@@ -66,42 +66,136 @@ __device__ __forceinline__ float group_zero(unsigned w) {
     return (float)(w & (BITS == 4 ? 15u : 255u));
 }
 
-// The codes of 8 numbers of a group whose other numbers are those of the
-// lanes beside this one (8 lanes at a multiple of 8); returns the group's word.
-// Quotients are rounded to fp32 before they are rounded to integers: the step
-// has so few bits that no quotient of a 24-bit number comes to lie on a half, or
-// on a step, by that.
-template <int BITS>
-__device__ __forceinline__ unsigned quantise(const float (&x)[8], unsigned (&code)[8], bool& odd) {
-    constexpr unsigned TOP = BITS == 4 ? 15 : 255, LOW = BITS == 4 ? 0xfffffu : 0x7fffffu;
+// The range of a group, 0 included, and the bits of its largest magnitude (NaN's
+// among them).
+struct Range {
     float lo = 0.f, hi = 0.f;
-    int bad = 0;
+    unsigned big = 0;
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        bad |= !(fabsf(x[e]) < 0x1p125f);
+        for (int e = 0; e < N; ++e) {
+            lo = fminf(lo, x[e]);
+            hi = fmaxf(hi, x[e]);
+            big = max(big, __float_as_uint(x[e]) & 0x7fffffffu);
+        }
     }
-#pragma unroll
-    for (int st = 1; st < 8; st <<= 1) {
+    // with that of the lane `st` away
+    __device__ __forceinline__ void join(int st) {
         lo = fminf(lo, __shfl_xor(lo, st, 64));
         hi = fmaxf(hi, __shfl_xor(hi, st, 64));
-        bad |= __shfl_xor(bad, st, 64);
+        big = max(big, (unsigned)__shfl_xor((int)big, st, 64));
     }
-    const float step = fmaxf(__uint_as_float((__float_as_uint((hi - lo) / (float)TOP) + LOW) & ~LOW), 0x1p-100f);
-    const float zero = rintf(-lo / step);
+};
+
+// A group's quantiser. Quotients are rounded to fp32 before they are rounded to
+// integers: the step has so few bits that no quotient of a 24-bit number comes to
+// lie on a half, or on a step, by that. Division by a step of one bit is a product.
+// By one of four it is a product with the rounded reciprocal, and its remainder
+// times that again, which gives the rounded quotient (Markstein's theorem on
+// division by fused multiply-add).
+template <int BITS>
+struct Quantiser {
+    static constexpr unsigned TOP = BITS == 4 ? 15 : 255, LOW = BITS == 4 ? 0xfffffu : 0x7fffffu;
+    float step, inv;
+    int shift;
+    unsigned word;
+    bool bad;
+    __device__ __forceinline__ explicit Quantiser(const Range& r) {
+        bad = r.big >= 0x7e000000u;  // 2^125
+        step = fmaxf(__uint_as_float((__float_as_uint((r.hi - r.lo) / (float)TOP) + LOW) & ~LOW), 0x1p-100f);
+        inv = 1.f / step;
+        const float zero = rintf(quotient(-r.lo));
+        shift = (int)zero - 0x4b400000;
+        if constexpr (BITS == 4) word = bad ? 0x7ff0u : (__float_as_uint(step) >> 16) | (unsigned)zero;
+        else word = bad ? 0xff00u : (__float_as_uint(step) >> 23) << 8 | (unsigned)zero;
+    }
+    __device__ __forceinline__ float quotient(float x) const {
+        const float t = x * inv;
+        return BITS == 8 ? t : fmaf(fmaf(-t, step, x), inv, t);
+    }
+    __device__ __forceinline__ unsigned code(float x) const {
+        const int n = __float_as_int(quotient(x) + 12582912.f) + shift;  // (the sum with 1.5 2^23 rounds to an integer)
+        return bad ? 0 : min(max(n, 0), (int)TOP);
+    }
+};
+
+// The codes of 8 numbers of a group whose other numbers are those of the
+// lanes beside this one (8 lanes at a multiple of 8); returns the group's word.
+template <int BITS>
+__device__ __forceinline__ unsigned quantise(const float (&x)[8], unsigned (&code)[8], bool& odd) {
+    Range r;
+    r.add(x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        code[e] = bad ? 0 : (unsigned)fminf(fmaxf(rintf(x[e] / step) + zero, 0.f), (float)TOP);
-    odd = odd || bad;
-    if constexpr (BITS == 4) return bad ? 0x7ff0u : (__float_as_uint(step) >> 16) | (unsigned)zero;
-    return bad ? 0xff00u : (__float_as_uint(step) >> 23) << 8 | (unsigned)zero;
+    for (int st = 1; st < 8; st <<= 1) r.join(st);
+    const Quantiser<BITS> q(r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) code[e] = q.code(x[e]);
+    odd = odd || q.bad;
+    return q.word;
+}
+
+// A group's values as the half words that hold a position's dims (lane j of 8
+// lanes): in 4 bits those of dims 2 j and 2 j + 1 (and 16, 32 and 48 further on),
+// in 8 those of dims 32 (j / 4) + 4 (j % 4) .. + 3 (and 16 further on).
+template <int BITS>
+__device__ __forceinline__ void value_halves(const unsigned (&code)[8], int lane, unsigned (&half)[BITS / 2]) {
+    const int j = lane & 7, team = lane & ~7;
+    if constexpr (BITS == 4) {
+        unsigned w = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w |= code[e] << (4 * e);
+        half[0] = half[1] = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const unsigned v = (unsigned)__shfl((int)w, team + (j >> 2) + 2 * t, 64) >> (8 * (j & 3));
+            half[0] |= (v & 15u) << (4 * t);
+            half[1] |= (v >> 4 & 15u) << (4 * t);
+        }
+    } else {
+        const unsigned w0 = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+        const unsigned w1 = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+        unsigned v[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int from = team + (j & 4) + ((j & 3) >> 1) + 2 * t;
+            const unsigned a = __shfl((int)w0, from, 64), b = __shfl((int)w1, from, 64);
+            v[t] = j & 1 ? b : a;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) half[i] = (v[0] >> (8 * i) & 255u) | (v[1] >> (8 * i) & 255u) << 8;
+    }
+}
+// Dim, in its group, of half word i of lane j.
+template <int BITS>
+__device__ __forceinline__ int half_dim(int lane, int i) {
+    const int j = lane & 7;
+    return BITS == 4 ? 2 * j + i : (j >> 2) * 32 + (j & 3) * 4 + i;
+}
+// Keys' codes as they are held: 8 nibbles, or 4 bytes from e on.
+__device__ __forceinline__ unsigned key_word(const unsigned (&q)[8]) {
+    unsigned w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w |= q[e] << ((e >> 1) * 4 + (e & 1) * 16);
+    return w;
+}
+__device__ __forceinline__ unsigned four(const unsigned (&q)[8], int e) {
+    return q[e] | q[e + 1] << 8 | q[e + 2] << 16 | q[e + 3] << 24;
+}
+template <int BITS>
+__device__ __forceinline__ void store_key(unsigned char* dst, const unsigned (&q)[8]) {
+    if constexpr (BITS == 4) *reinterpret_cast<unsigned*>(dst) = key_word(q);
+    else *reinterpret_cast<u32x2*>(dst) = u32x2{four(q, 0), four(q, 4)};
 }
 
 // Eight numbers of a row, or into one.
 template <class T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-    if constexpr (VEC) {
+    if constexpr (VEC && sizeof(T) == 2) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? a[e >> 1] & 0xffff0000u : a[e >> 1] << 16);
+    } else if constexpr (VEC) {
         const float4 a = ld4(p), b = ld4(p + 4);
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
         x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
@@ -112,7 +206,10 @@ __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
 }
 template <class T, bool VEC>
 __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-    if constexpr (VEC) {
+    if constexpr (VEC && sizeof(T) == 2) {
+        *reinterpret_cast<u32x4*>(p) =
+            u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+    } else if constexpr (VEC) {
         st4(p, x[0], x[1], x[2], x[3]);
         st4(p + 4, x[4], x[5], x[6], x[7]);
     } else {
@@ -121,147 +218,267 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
     }
 }
 
+// What the lane 1, 2 or 4 away holds (within 8 lanes): lane permutations of the
+// vector unit itself.
+template <int ST>
+__device__ __forceinline__ unsigned lane_xor(unsigned v) {
+    if constexpr (ST == 1) return __builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true);
+    else if constexpr (ST == 2) return __builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true);
+    else return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true);  // 7, then 3
+}
+// Eight lanes' eight half words, transposed: half word e of lane j becomes half
+// word j of lane e. Three exchanges with the lanes 1, 2 and 4 away.
+__device__ __forceinline__ void transpose8(u32x4& w, int lane) {
+    const unsigned sel = lane & 1 ? 0x03020706u : 0x05040100u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(lane_xor<1>(w[i]), w[i], sel);
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const unsigned got = lane_xor<2>(lane & 2 ? w[i] : w[i + 1]);
+        w[i] = lane & 2 ? got : w[i];
+        w[i + 1] = lane & 2 ? w[i + 1] : got;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const unsigned got = lane_xor<4>(lane & 4 ? w[i] : w[i + 2]);
+        w[i] = lane & 4 ? got : w[i];
+        w[i + 2] = lane & 4 ? w[i + 2] : got;
+    }
+}
+
 // ------------------------------------------------------------------ rows in and out
 //
-// As paged_append_kernel and paged_read_kernel: a workgroup per (tile, kv head,
-// layer), rows of up to 32 positions. Eight lanes have a group. Keys are written
-// as they come; values go through LDS, so that a block's 16-byte pieces are
-// written whole where all their positions are new.
+// A wave per (tile, keys or values, head) and layer goes through the tile's block of
+// 32 positions in units of 64 dims (values) or two groups a lane (keys), entirely
+// in registers: a lane holds 32 numbers.
+//   keys    lane (position % 16, c): dims 8 c .. + 7 of each 32, its 16 bytes of
+//           the page; a group's numbers are 16 of four lanes (16 apart);
+//   values  lane (position, half): dims 8 half .. + 7 of each 16 of a group's 64,
+//           which two lanes (8 apart) share; the half words that hold a
+//           position's dims are transposed over 8 lanes, to or from the page's
+//           pieces of 8 positions.
+// Workgroups are dealt to the 8 XCDs in turn; place_of_group gives those of one
+// XCD consecutive work, so that rows of neighbouring heads meet in its L2 and
+// reach memory together.
+__device__ __forceinline__ unsigned place_of_group() {
+    const unsigned b = blockIdx.x, n = gridDim.x, x = b & 7, q = n >> 3, r = n & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+// Position, in its block of 32, and dims of a lane of the values:
+__device__ __forceinline__ int value_row(int lane) { return (lane >> 4) * 4 + (lane & 3) + (lane & 4) * 4; }
+__device__ __forceinline__ int value_dim(int lane, int i) { return i * 16 + (lane & 8); }
+// Words of a lane's key piece i (of 8 dims): its position in the block and its dim.
+// Unit n of a head's 32 positions: in D = 64 the one, in 128 the n-th 16 positions.
+template <int D>
+__device__ __forceinline__ int key_row(int n, int i, int lane) { return (D == 64 ? i / 2 : n) * 16 + (lane & 15); }
+template <int D>
+__device__ __forceinline__ int key_dim(int i, int lane) { return (D == 64 ? i & 1 : i) * 32 + (lane >> 4) * 8; }
+
 template <class T, int D, int BITS, bool VEC>
 __global__ __launch_bounds__(256) void packed_append_kernel(PagedView c, const int* __restrict__ list, int layer0,
                                                             const T* __restrict__ k, const T* __restrict__ v,
                                                             long long k_ld, long long v_ld, long long k_layer,
-                                                            long long v_layer) {
-    constexpr int CH = D / 8, LD = D + 4, TILES = 16 / BITS;
-    __shared__ __align__(16) unsigned char sv[32 * LD];
+                                                            long long v_layer, int n_layers) {
     const ListHead head = *reinterpret_cast<const ListHead*>(list);
     const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
-    const int h = blockIdx.y, layer = layer0 + blockIdx.z, tid = threadIdx.x, P = 1 << c.shift;
-    for (int it = blockIdx.x; it < head.tiles; it += gridDim.x) {
-        const PageTile t = tiles[it];
+    const int lane = threadIdx.x & 63, P = 1 << c.shift;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long all = 2LL * head.tiles * c.Hkv;  // (tile, keys or values, head) of a layer
+    for (long long u0 = place_of_group() * 4LL + wave; u0 < all * n_layers; u0 += gridDim.x * 4LL) {
+        const int z = (int)(u0 / all), layer = layer0 + z;
+        const long long w = u0 - z * all;
+        const int h = (int)(w % c.Hkv), kv = (int)(w / c.Hkv) & 1;
+        const PageTile t = tiles[w / c.Hkv >> 1];
         const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
-        const int p0 = t.pos & (P - 1);
-        unsigned char* kd = c.head<unsigned char>(page, layer, 0, h);
-        unsigned char* vd = c.head<unsigned char>(page, layer, 1, h);
-        const T* ks = k + blockIdx.z * k_layer + (long long)t.row * k_ld + h * D;
-        const T* vs = v + blockIdx.z * v_layer + (long long)t.row * v_ld + h * D;
+        const int b0 = t.pos & (P - 1) & ~31, lo = t.pos & 31, hi = lo + t.n;  // the block, and its new positions
+        const long long ld = kv ? v_ld : k_ld;
+        const T* src = (kv ? v + z * v_layer : k + z * k_layer) + t.row * ld + h * D;
+        unsigned char* dst = c.head<unsigned char>(page, layer, kv, h);
+        unsigned short* words = reinterpret_cast<unsigned short*>(dst + packed_codes<BITS>(P, D)) + b0;
+        // a position's row in the caller's; of positions that are not new, the first or last new one's
+        auto row = [&](int p) __attribute__((always_inline)) { return src + (min(max(p, lo), hi - 1) - lo) * ld; };
+        auto is_new = [&](int p) __attribute__((always_inline)) { return p >= lo && p < hi; };
         bool odd = false;
-        for (int i = tid; i < t.n * CH; i += 256) {
-            const int r = i / CH, d = (i - r * CH) * 8, p = p0 + r;
-            float x[8];
-            unsigned q[8];
-            load8<T, VEC>(ks + r * k_ld + d, x);
-            const unsigned wk = quantise<BITS>(x, q, odd);
-            unsigned char* dst = kd + pkey_off<BITS>(p, d, D);
-            if constexpr (BITS == 4) {
-                unsigned w = 0;
+#pragma unroll 1
+        for (int n = 0; n < D / 64; ++n) {
+            float x[4][8];
+            if (kv == 0) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w |= q[e] << ((e >> 1) * 4 + (e & 1) * 16);
-                *reinterpret_cast<unsigned*>(dst) = w;
+                for (int i = 0; i < 4; ++i) load8<T, VEC>(row(key_row<D>(n, i, lane)) + key_dim<D>(i, lane), x[i]);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int p = key_row<D>(n, 2 * u, lane), d = key_dim<D>(2 * u, lane);
+                    Range r;
+                    r.add(x[2 * u]);
+                    r.add(x[2 * u + 1]);
+                    r.join(16);
+                    r.join(32);
+                    const Quantiser<BITS> q(r);
+                    unsigned code[2][8];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) code[i][e] = q.code(x[2 * u + i][e]);
+                    if (!is_new(p)) continue;
+                    odd = odd || q.bad;
+                    unsigned char* to = dst + pkey_off<BITS>(b0 + p, d, D);  // (the second piece is right behind)
+                    if constexpr (BITS == 4) {
+                        *reinterpret_cast<u32x2*>(to) = u32x2{key_word(code[0]), key_word(code[1])};
+                    } else {
+                        *reinterpret_cast<u32x4*>(to) = u32x4{four(code[0], 0), four(code[0], 4), four(code[1], 0), four(code[1], 4)};
+                    }
+                    if (lane < 16) words[(d / GROUP) * P + p] = (unsigned short)q.word;
+                }
             } else {
-                *reinterpret_cast<u32x2*>(dst) = u32x2{q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24,
-                                                       q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24};
-            }
-            load8<T, VEC>(vs + r * v_ld + d, x);
-            const unsigned wv = quantise<BITS>(x, q, odd);
-            unsigned* sd = reinterpret_cast<unsigned*>(sv + (p & 31) * LD + d);
-            sd[0] = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-            sd[1] = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
-            if ((d & (GROUP - 1)) == 0) {
-                const int at = packed_codes<BITS>(P, D) + ((d / GROUP) * P + p) * 2;
-                *reinterpret_cast<unsigned short*>(kd + at) = (unsigned short)wk;
-                *reinterpret_cast<unsigned short*>(vd + at) = (unsigned short)wv;
-            }
-        }
-        if (c.odd && odd) *c.odd = 1;
-        __syncthreads();
-        const int lo = p0 & 31, hi = lo + t.n;
-        unsigned char* vb = vd + pval_off<BITS>(p0 & ~31, 0, D);
-        for (int i = tid; i < D * BITS / 4; i += 256) {  // 16-byte pieces of the block of 32 positions
-            const int ln = i & 63, dim = (i >> 6) * (256 / BITS) + (ln & 15), g = ln >> 4;
-            unsigned half[8];
-            bool all = true;
+                const int p = value_row(lane);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int pos = g * 4 + (e & 3) + (e >> 2) * 16;
-                all = all && pos >= lo && pos < hi;
-                half[e] = 0;
+                for (int i = 0; i < 4; ++i) load8<T, VEC>(row(p) + n * GROUP + value_dim(lane, i), x[i]);
+                Range r;
 #pragma unroll
-                for (int u = 0; u < TILES; ++u) half[e] |= (unsigned)sv[pos * LD + dim + u * 16] << (u * BITS);
-            }
-            unsigned char* dst = vb + i * 16;
-            if (all) {
-                *reinterpret_cast<u32x4*>(dst) =
-                    u32x4{half[0] | half[1] << 16, half[2] | half[3] << 16, half[4] | half[5] << 16, half[6] | half[7] << 16};
-            } else {
+                for (int i = 0; i < 4; ++i) r.add(x[i]);
+                r.join(8);
+                const Quantiser<BITS> q(r);
+                odd = odd || (q.bad && is_new(p));
+                if (!(lane & 8) && is_new(p)) words[n * P + p] = (unsigned short)q.word;
+                // half words of dims 8 half + j: 16 dims on in the next nibble (byte), 32 on in the next block (8 bits)
+                constexpr int BLOCKS = BITS / 4, TILES = 4 / BLOCKS;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int pos = g * 4 + (e & 3) + (e >> 2) * 16;
-                    if (pos >= lo && pos < hi) reinterpret_cast<unsigned short*>(dst)[e] = (unsigned short)half[e];
+                for (int b = 0; b < BLOCKS; ++b) {
+                    u32x4 y;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        y[j] = 0;
+#pragma unroll
+                        for (int i = 0; i < TILES; ++i)
+                            y[j] |= (q.code(x[b * TILES + i][2 * j]) | q.code(x[b * TILES + i][2 * j + 1]) << 16) << (BITS * i);
+                    }
+                    transpose8(y, lane);
+                    // now the 8 positions (lane / 16) * 4 .. + 3 and 16 on of dim lane % 16
+                    const int g = (lane >> 4) * 4;
+                    unsigned char* to = dst + pval_off<BITS>(b0, n * GROUP + b * 32, D) + lane * 16;
+                    if (g >= lo && g + 20 <= hi) {
+                        *reinterpret_cast<u32x4*>(to) = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (is_new(g + (e & 3) + (e >> 2) * 16))
+                                reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(y[e >> 1] >> (e & 1) * 16);
+                    }
                 }
             }
         }
-        __syncthreads();  // the next tile's LDS
+        if (c.odd && odd) *c.odd = 1;
+    }
+}
+
+// Tiles of few rows: a row of a head's keys, or values, per D / 8 lanes, and its
+// half words written one by one. (A workgroup per tile would have 8 of its 256
+// lanes at work on a decode step.)
+template <class T, int D, int BITS, bool VEC>
+__global__ __launch_bounds__(256) void packed_append_few_kernel(PagedView c, const int* __restrict__ list, int layer0,
+                                                                const T* __restrict__ k, const T* __restrict__ v,
+                                                                long long k_ld, long long v_ld, long long k_layer,
+                                                                long long v_layer) {
+    constexpr int CH = D / 8;
+    const ListHead head = *reinterpret_cast<const ListHead*>(list);
+    const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
+    const int layer = layer0 + blockIdx.z, tid = threadIdx.x, d = tid % CH * 8, P = 1 << c.shift;
+    const long long all = 2LL * head.tiles * c.Hkv;  // (tile, keys or values, head)
+    for (long long w = blockIdx.x * (256LL / CH) + tid / CH; w < all; w += gridDim.x * (256LL / CH)) {
+        const int h = (int)(w % c.Hkv), kv = (int)(w / c.Hkv) & 1;
+        const PageTile t = tiles[w / c.Hkv >> 1];
+        const long long ld = kv ? v_ld : k_ld;
+        const T* src = (kv ? v + blockIdx.z * v_layer : k + blockIdx.z * k_layer) + t.row * ld + h * D + d;
+        const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
+        unsigned char* dst = c.head<unsigned char>(page, layer, kv, h);
+        bool odd = false;
+        for (int r = 0; r < t.n; ++r) {
+            const int p = (t.pos & (P - 1)) + r;
+            float x[8];
+            unsigned q[8], half[BITS / 2];
+            load8<T, VEC>(src + r * ld, x);
+            const unsigned word = quantise<BITS>(x, q, odd);
+            value_halves<BITS>(q, tid, half);
+            if (kv == 0) {
+                store_key<BITS>(dst + pkey_off<BITS>(p, d, D), q);
+            } else {
+#pragma unroll
+                for (int e = 0; e < BITS / 2; ++e) {
+                    const int dim = (d & ~(GROUP - 1)) + half_dim<BITS>(tid, e);
+                    *reinterpret_cast<unsigned short*>(dst + pval_off<BITS>(p, dim, D)) = (unsigned short)half[e];
+                }
+            }
+            if ((d & (GROUP - 1)) == 0)
+                *reinterpret_cast<unsigned short*>(dst + packed_codes<BITS>(P, D) + ((d / GROUP) * P + p) * 2) = (unsigned short)word;
+        }
+        if (c.odd && odd) *c.odd = 1;
     }
 }
 
 template <class T, int D, int BITS, bool VEC>
 __global__ __launch_bounds__(256) void packed_read_kernel(PagedView c, const int* __restrict__ list, int layer0,
                                                           T* __restrict__ k, T* __restrict__ v, long long k_ld,
-                                                          long long v_ld, long long k_layer, long long v_layer) {
-    constexpr int CH = D / 8, LD = D + 4, TILES = 16 / BITS;
-    __shared__ __align__(16) unsigned char sv[32 * LD];
+                                                          long long v_ld, long long k_layer, long long v_layer,
+                                                          int n_layers) {
     const ListHead head = *reinterpret_cast<const ListHead*>(list);
     const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
-    const int h = blockIdx.y, layer = layer0 + blockIdx.z, tid = threadIdx.x, P = 1 << c.shift;
-    for (int it = blockIdx.x; it < head.tiles; it += gridDim.x) {
-        const PageTile t = tiles[it];
+    const int lane = threadIdx.x & 63, P = 1 << c.shift;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long all = 2LL * head.tiles * c.Hkv;
+    for (long long u0 = place_of_group() * 4LL + wave; u0 < all * n_layers; u0 += gridDim.x * 4LL) {
+        const int z = (int)(u0 / all), layer = layer0 + z;
+        const long long w = u0 - z * all;
+        const int h = (int)(w % c.Hkv), kv = (int)(w / c.Hkv) & 1;
+        const PageTile t = tiles[w / c.Hkv >> 1];
         const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
-        const int p0 = t.pos & (P - 1);
-        const unsigned char* kd = c.head<unsigned char>(page, layer, 0, h);
-        const unsigned char* vd = c.head<unsigned char>(page, layer, 1, h);
-        const unsigned char* vb = vd + pval_off<BITS>(p0 & ~31, 0, D);
-        T* ks = k + blockIdx.z * k_layer + (long long)t.row * k_ld + h * D;
-        T* vs = v + blockIdx.z * v_layer + (long long)t.row * v_ld + h * D;
-        for (int i = tid; i < D * BITS / 4; i += 256) {
-            const int ln = i & 63, dim = (i >> 6) * (256 / BITS) + (ln & 15), g = ln >> 4;
-            const u32x4 a = *reinterpret_cast<const u32x4*>(vb + i * 16);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int pos = g * 4 + (e & 3) + (e >> 2) * 16;
-#pragma unroll
-                for (int u = 0; u < TILES; ++u)
-                    sv[pos * LD + dim + u * 16] = (unsigned char)(a[e >> 1] >> ((e & 1) * 16 + u * BITS) & (BITS == 4 ? 15u : 255u));
-            }
-        }
-        __syncthreads();
-        for (int i = tid; i < t.n * CH; i += 256) {
-            const int r = i / CH, d = (i - r * CH) * 8, p = p0 + r;
-            const int at = packed_codes<BITS>(P, D) + ((d / GROUP) * P + p) * 2;
+        const int b0 = t.pos & (P - 1) & ~31, lo = t.pos & 31, hi = lo + t.n;
+        const long long ld = kv ? v_ld : k_ld;
+        T* dst = (kv ? v + z * v_layer : k + z * k_layer) + t.row * ld + h * D;
+        const unsigned char* src = c.head<unsigned char>(page, layer, kv, h);
+        const unsigned short* words = reinterpret_cast<const unsigned short*>(src + packed_codes<BITS>(P, D)) + b0;
+#pragma unroll 1
+        for (int n = 0; n < D / 64; ++n) {
             float x[8];
-            unsigned q[8];
-            const unsigned char* src = kd + pkey_off<BITS>(p, d, D);
-            if constexpr (BITS == 4) {
-                const unsigned w = *reinterpret_cast<const unsigned*>(src);
+            if (kv == 0) {
+                u32x4 y[BITS / 4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] = w >> ((e >> 1) * 4 + (e & 1) * 16) & 15u;
+                for (int i = 0; i < BITS / 4; ++i)  // (in 8 bits the second half of the positions, or dims, is 1 KiB on)
+                    y[i] = *reinterpret_cast<const u32x4*>(src + (b0 / 32 * (D / 64) + n) * (BITS * 256) + i * 1024 + lane * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p = key_row<D>(n, i, lane), d = key_dim<D>(i, lane);
+                    const unsigned word = words[(d / GROUP) * P + p];
+                    const float step = group_step<BITS>(word), off = -group_zero<BITS>(word) * step;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const unsigned q = BITS == 4 ? y[0][i] >> ((e >> 1) * 4 + (e & 1) * 16) & 15u
+                                                     : y[i >> 1 & (BITS == 8)][(i & 1) * 2 + (e >> 2)] >> ((e & 3) * 8) & 255u;
+                        x[e] = fmaf((float)q, step, off);
+                    }
+                    if (p >= lo && p < hi) store8<T, VEC>(dst + (p - lo) * ld + d, x);
+                }
             } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(src);
+                constexpr int BLOCKS = BITS / 4, TILES = 4 / BLOCKS;
+                const int p = value_row(lane);
+                const unsigned word = words[n * P + p];
+                const float step = group_step<BITS>(word), off = -group_zero<BITS>(word) * step;
+                u32x4 y[BLOCKS];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] = w[e >> 2] >> ((e & 3) * 8) & 255u;
+                for (int b = 0; b < BLOCKS; ++b)
+                    y[b] = *reinterpret_cast<const u32x4*>(src + pval_off<BITS>(b0, n * GROUP + b * 32, D) + lane * 16);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    transpose8(y[b], lane);
+#pragma unroll
+                    for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            x[e] = fmaf((float)(y[b][e >> 1] >> ((e & 1) * 16 + i * BITS) & (BITS == 4 ? 15u : 255u)), step, off);
+                        if (p >= lo && p < hi) store8<T, VEC>(dst + (p - lo) * ld + n * GROUP + value_dim(lane, b * TILES + i), x);
+                    }
+                }
             }
-            const unsigned wk = *reinterpret_cast<const unsigned short*>(kd + at);
-            const unsigned wv = *reinterpret_cast<const unsigned short*>(vd + at);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = ((float)q[e] - group_zero<BITS>(wk)) * group_step<BITS>(wk);
-            store8<T, VEC>(ks + r * k_ld + d, x);
-            const unsigned* sd = reinterpret_cast<const unsigned*>(sv + (p & 31) * LD + d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[e] = ((float)(sd[e >> 2] >> ((e & 3) * 8) & 255u) - group_zero<BITS>(wv)) * group_step<BITS>(wv);
-            store8<T, VEC>(vs + r * v_ld + d, x);
         }
-        __syncthreads();  // the next tile's LDS
     }
 }
 
