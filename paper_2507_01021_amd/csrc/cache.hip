@@ -38,6 +38,8 @@ constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
 // Rows of a tile, on average, up to which the packed cache's append takes the
 // kernel of few rows.
 constexpr int FEW_ROWS = 4;
+// Workgroups that the packed cache's attention of up to 4 rows is cut into.
+constexpr int FOUR_WGS = 512;
 // Most workgroups of a launch along its list (a grid holds fewer than 2^32
 // threads): the kernels go through longer lists in strides.
 constexpr int MOST_WGS = 1 << 22;
@@ -50,6 +52,7 @@ class PagedCacheT final : public PagedCache {
         G_ = p.n_head / p.n_kv_head;
         // parts of cut ranges: ATTN_WGS / n_kv_head whole ones and a partial one for each of as many ranges
         max_parts_ = 2 * (ATTN_WGS / p.n_kv_head + 1);
+        if (FOURS && bits_ && G_ <= 4) max_parts_ *= 2;  // (sequences of up to 4 rows, and those of more)
         if (big_rows(p.max_tokens)) max_parts_ += BIG_ROWS / 16 * 2 * (BIG_WGS / p.n_kv_head + 1);
         if (dev_ == WHISPER_NO_DEVICE) return;
         DeviceScope scope(dev_);
@@ -150,7 +153,7 @@ class PagedCacheT final : public PagedCache {
         need_chunk();
         DeviceScope scope(dev_);
         const bool rec = capturing(st_);
-        if (n_items_ + n_bigs_ == 0 && !rec) return;
+        if (n_items_ + n_bigs_ + n_fours_ == 0 && !rec) return;
         AttnArgs a{view(), layer, P_.n_head, G_, q, out, q_ld, out_ld, scale * 1.4426950408889634f, plan_.dev,
                    parts_};
         if (P_.head_size == 64) launch_attn<64>(a, rec);
@@ -310,7 +313,7 @@ class PagedCacheT final : public PagedCache {
     ListHead head_{};
     bool plan_ok_ = false;    // there is a chunk
     bool append_ok_ = false;  // none of its sequences was forked since
-    int tokens_ = 0, n_items_ = 0, n_bigs_ = 0, n_merges_ = 0, n_tiles_ = 0, n_wide_ = 0;
+    int tokens_ = 0, n_items_ = 0, n_bigs_ = 0, n_fours_ = 0, n_merges_ = 0, n_tiles_ = 0, n_wide_ = 0;
     int max_tiles_ = 0;
 
     template <class U>
@@ -415,6 +418,8 @@ class PagedCacheT final : public PagedCache {
         copy_pages(list_.dev + upd.size(), (int)copies.size());
     }
 
+    // Packed caches of bf16: up to 4 rows of a sequence go to a kernel of their own.
+    static constexpr bool FOURS = sizeof(T) == 2;
     // Whether a chunk's `count` tokens of one sequence go to the kernel of many rows.
     bool big_rows(int count) const { return sizeof(T) == 2 && (long long)count * G_ >= BIG_FROM; }
     bool max_bigs() const { return big_rows(P_.max_tokens); }
@@ -442,14 +447,18 @@ class PagedCacheT final : public PagedCache {
         int row = 0, np = 0;
         // items of `step` rows of the sequences that kernel `big` takes, cut
         // into about `wgs` workgroups, a part's positions a multiple of 128
-        auto plan = [&](bool big, int step, int wgs, int least) {
+        enum Kind { BIG, SOME, FOUR };
+        auto kind = [&](int count) {
+            return big_rows(count) ? BIG : FOURS && bits_ && (long long)count * G_ <= 4 ? FOUR : SOME;
+        };
+        auto plan = [&](Kind which, int step, int wgs, int least) {
             items.clear();
             cut.clear();
             long long work = 0;
             int tok0 = 0;
             for (int i = 0; i < n; tok0 += counts[i++]) {
                 const int s = seqs[i], past = book_.length(s) - counts[i], rows = counts[i] * G_;
-                if (big_rows(counts[i]) != big) continue;
+                if (kind(counts[i]) != which) continue;
                 for (int j = 0; j < rows; j += step) {
                     const int end = past + (std::min(j + step, rows) - 1) / G_ + 1;
                     items.push_back(AttnItem{s, past, counts[i], tok0, j, 0, end, -1});
@@ -481,11 +490,14 @@ class PagedCacheT final : public PagedCache {
                              [](const AttnItem& a, const AttnItem& b) { return a.kv1 - a.kv0 > b.kv1 - b.kv0; });
         };
         for (int i = 0; i < n; ++i) row = add_tiles(tiles, seqs[i], book_.length(seqs[i]) - counts[i], counts[i], row);
-        plan(true, BIG_ROWS, BIG_WGS, BIG_PART);
+        plan(BIG, BIG_ROWS, BIG_WGS, BIG_PART);
         const std::vector<AttnItem> bigs = cut;
-        plan(false, 16, ATTN_WGS, ATTN_PART);
+        plan(FOUR, 16, FOUR_WGS, ATTN_PART);
+        const std::vector<AttnItem> fours = cut;
+        plan(SOME, 16, ATTN_WGS, ATTN_PART);
         n_items_ = (int)cut.size();
         n_bigs_ = (int)bigs.size();
+        n_fours_ = (int)fours.size();
         n_merges_ = (int)merges.size();
         n_tiles_ = (int)tiles.size() / 4;
         blob_.assign(HEAD_INTS, 0);
@@ -514,7 +526,8 @@ class PagedCacheT final : public PagedCache {
         }
         n_wide_ = (int)wide.size();
         const size_t wa = add(wide.data(), wide.size());
-        head_ = ListHead{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, n_wide_, (int)wa};
+        const size_t fa = add(fours.data(), fours.size() * (sizeof(AttnItem) / sizeof(int)));
+        head_ = ListHead{n_items_, n_merges_, n_tiles_, (int)ma, (int)ta, n_bigs_, (int)ba, n_wide_, (int)wa, n_fours_, (int)fa};
         memcpy(blob_.data(), &head_, sizeof(head_));
     }
 
@@ -522,6 +535,7 @@ class PagedCacheT final : public PagedCache {
     void launch_attn(const AttnArgs& a, bool rec) {
         // a recorded launch may meet a longer list at its replay: the kernels go through it in strides
         const unsigned ni = rec ? 2 * ATTN_WGS : std::min(n_items_ * P_.n_kv_head, MOST_WGS);
+        const unsigned nf = !FOURS || !bits_ ? 0 : rec ? 2 * ATTN_WGS : std::min(n_fours_ * P_.n_kv_head, MOST_WGS);
         const unsigned nm = rec ? ATTN_WGS : (unsigned)n_merges_ * P_.n_kv_head;
         if constexpr (sizeof(T) == 2) {
             const unsigned nb = rec ? (max_bigs() ? 2 * BIG_WGS : 0) : (unsigned)n_bigs_ * P_.n_kv_head;
@@ -536,6 +550,10 @@ class PagedCacheT final : public PagedCache {
                 w.layer = 0;
             }
             if (nb) hipLaunchKernelGGL(paged_attn_big_kernel<D>, dim3(nb), dim3(BIG_THREADS), 0, st_, w);
+        }
+        if constexpr (FOURS) {
+            if (nf && bits_ == 4) hipLaunchKernelGGL((packed_attn_four_kernel<D, 4>), dim3(nf), dim3(256), 0, st_, a);
+            else if (nf) hipLaunchKernelGGL((packed_attn_four_kernel<D, 8>), dim3(nf), dim3(256), 0, st_, a);
         }
         if (ni) {
             if (bits_ == 4) hipLaunchKernelGGL((packed_attn_kernel<T, D, 4>), dim3(ni), dim3(256), 0, st_, a);

@@ -54,12 +54,11 @@ __device__ __forceinline__ int pval_off(int p, int d, int D) {
            ((p & 3) + ((p & 16) >> 2)) * 2;
 }
 
-// Step and zero from a group's word. CHECK: 8-bit words may be NaN's.
-template <int BITS, bool CHECK = true>
+// Step and zero from a group's word. A group of NaN has code and zero 0 throughout
+// and NaN, or (8 bits) +inf, as its step: 0 times either is NaN.
+template <int BITS>
 __device__ __forceinline__ float group_step(unsigned w) {
-    if constexpr (BITS == 4) return __uint_as_float((w & 0x7ff0u) << 16);
-    const float s = __uint_as_float((w & 0xff00u) << 15);
-    return CHECK && (w & 0xff00u) == 0xff00u ? NAN : s;
+    return __uint_as_float(BITS == 4 ? (w & 0x7ff0u) << 16 : (w & 0xff00u) << 15);
 }
 template <int BITS>
 __device__ __forceinline__ float group_zero(unsigned w) {
@@ -494,7 +493,10 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <class T> struct Codes;
 template <> struct Codes<bf16> {
     typedef mfma_bf16x8 V;
-    __device__ static __forceinline__ unsigned pair4(unsigned w) { return (w & 0x000f000fu) | 0x43004300u; }
+    unsigned mask = 0x000f000fu, exponent = 0x43004300u;
+    // (in vector registers, an instruction takes both; of constants it takes one)
+    __device__ __forceinline__ Codes() { asm volatile("" : "+v"(mask), "+v"(exponent)); }
+    __device__ __forceinline__ unsigned pair4(unsigned w) const { return (w & mask) | exponent; }
     __device__ static __forceinline__ unsigned pair8(unsigned a, unsigned b) {  // two numbers up to 255
         return __builtin_amdgcn_perm(__float_as_uint((float)b), __float_as_uint((float)a), 0x07060302u);
     }
@@ -502,21 +504,21 @@ template <> struct Codes<bf16> {
         return __builtin_bit_cast(V, (u32x4{a, b, c, d}));
     }
     template <int BITS>
-    __device__ static __forceinline__ V key(const unsigned* w) {  // one word, or two
+    __device__ __forceinline__ V key(const unsigned* w) const {  // one word, or two
         if constexpr (BITS == 4) return of(pair4(w[0]), pair4(w[0] >> 4), pair4(w[0] >> 8), pair4(w[0] >> 12));
         else
             return of(pair8(w[0] & 255u, w[0] >> 8 & 255u), pair8(w[0] >> 16 & 255u, w[0] >> 24),
                       pair8(w[1] & 255u, w[1] >> 8 & 255u), pair8(w[1] >> 16 & 255u, w[1] >> 24));
     }
     template <int BITS>
-    __device__ static __forceinline__ V val(u32x4 w, int u) {  // the u-th of the dims that are 16 apart
+    __device__ __forceinline__ V val(u32x4 w, int u) const {  // the u-th of the dims that are 16 apart
         if constexpr (BITS == 4) return of(pair4(w[0] >> 4 * u), pair4(w[1] >> 4 * u), pair4(w[2] >> 4 * u), pair4(w[3] >> 4 * u));
         else
             return of(pair8(w[0] >> 8 * u & 255u, w[0] >> (8 * u + 16) & 255u), pair8(w[1] >> 8 * u & 255u, w[1] >> (8 * u + 16) & 255u),
                       pair8(w[2] >> 8 * u & 255u, w[2] >> (8 * u + 16) & 255u), pair8(w[3] >> 8 * u & 255u, w[3] >> (8 * u + 16) & 255u));
     }
     template <int BITS>
-    __device__ static __forceinline__ V zeros(u32x4 w) {  // of 8 positions' words, the codes' offset added
+    __device__ __forceinline__ V zeros(u32x4 w) const {  // of 8 positions' words, the codes' offset added
         if constexpr (BITS == 4) return of(pair4(w[0]), pair4(w[1]), pair4(w[2]), pair4(w[3]));
         else return val<8>(w, 0);
     }
@@ -527,7 +529,7 @@ template <> struct Codes<bf16> {
 template <> struct Codes<float> {
     typedef f32x8 V;
     template <int BITS>
-    __device__ static __forceinline__ V key(const unsigned* w) {
+    __device__ __forceinline__ V key(const unsigned* w) const {
         V x;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -535,14 +537,14 @@ template <> struct Codes<float> {
         return x;
     }
     template <int BITS>
-    __device__ static __forceinline__ V val(u32x4 w, int u) {
+    __device__ __forceinline__ V val(u32x4 w, int u) const {
         V x;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (float)(w[e >> 1] >> ((e & 1) * 16 + u * BITS) & (BITS == 4 ? 15u : 255u));
         return x;
     }
     template <int BITS>
-    __device__ static __forceinline__ V zeros(u32x4 w) { return val<BITS>(w, 0); }
+    __device__ __forceinline__ V zeros(u32x4 w) const { return val<BITS>(w, 0); }
     __device__ static __forceinline__ mfma_f32x4 mul(V a, V b, mfma_f32x4 c) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
@@ -567,7 +569,6 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
     constexpr int NK = D / 32, ND = D / 16, NG = D / GROUP;
     constexpr int NB = D * BITS / 256;  // 16-byte pieces per lane of 32 positions' codes
     constexpr int PER = 16 / BITS;      // dim tiles of a value piece
-    constexpr float OFF = CODE_OFF<T, BITS>;
     constexpr bool TWO = sizeof(T) == 2;
     __shared__ float so[4][16][D + 4];
     __shared__ float sm[4][16], sl[4][16];
@@ -576,6 +577,7 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int P = 1 << a.c.shift;
+    const C codes{};
     for (int w0 = blockIdx.x; w0 < head.items * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const AttnItem t = items[it];
@@ -599,6 +601,20 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
             qs[i] += __shfl_xor(qs[i], 16, 64);
             qs[i] += __shfl_xor(qs[i], 32, 64);
         }
+        // bf16: the zeros' term of the scores as a product too, of -(zero + offset) and
+        // the sums as three bf16 numbers each, which leave 2^-24 of them
+        V qz[NG];
+        if constexpr (TWO) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                float left = fc == 0 ? qs[i] : 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    qz[i][e] = (__bf16)(e < 3 ? left : 0.f);
+                    left -= (float)qz[i][e];
+                }
+            }
+        }
         mfma_f32x4 o[ND], oz[NG];
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -615,20 +631,24 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
             const int at = (p0 >> 5) * (NB * 1024) + lane * 16, ws = packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
             u32x4 kw[NB], vw[NB];
             u32x2 ks[NG][2], vs[NG][2];  // words of positions b * 16 + fc * 4 .. + 3
+            unsigned kz[NG][2];          // and of position b * 16 + fr
 #pragma unroll
             for (int i = 0; i < NB; ++i) kw[i] = *reinterpret_cast<const u32x4*>(kb + at + i * 1024);
 #pragma unroll
             for (int i = 0; i < NG; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) ks[i][b] = *reinterpret_cast<const u32x2*>(kb + ws + (i * P + b * 16) * 2);
+                for (int b = 0; b < 2; ++b) {
+                    ks[i][b] = *reinterpret_cast<const u32x2*>(kb + ws + (i * P + b * 16) * 2);
+                    if constexpr (TWO)
+                        kz[i][b] = *reinterpret_cast<const unsigned short*>(kb + packed_codes<BITS>(P, D) + (i * P + p0 + b * 16 + fr) * 2);
+                }
 #pragma unroll
             for (int i = 0; i < NB; ++i) vw[i] = *reinterpret_cast<const u32x4*>(vb + at + i * 1024);
 #pragma unroll
             for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) vs[i][b] = *reinterpret_cast<const u32x2*>(vb + ws + (i * P + b * 16) * 2);
-            const bool edge = p + 32 > all;
-            auto hidden = [&](int b, int r) { return edge && p + b * 16 + fc * 4 + r >= lim; };
+            const int end = p + 32 > all ? lim - p - fc * 4 : 32;  // positions of the block, from this lane's first, that it sees
             mfma_f32x4 sc[2];
             float mx = -INFINITY;
 #pragma unroll
@@ -637,13 +657,20 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
 #pragma unroll
                 for (int i = 0; i < NG; ++i) {
                     x[i] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+                    if constexpr (TWO) {
+                        unsigned z;  // -(zero + offset), twice
+                        if constexpr (BITS == 4) z = (kz[i][b] & 15u) | 0xc300u;
+                        else z = __float_as_uint(-(float)(kz[i][b] & 255u)) >> 16;
+                        z |= z << 16;
+                        x[i] = C::mul(C::of(z, z, z, z), qz[i], x[i]);
+                    }
 #pragma unroll
                     for (int s = 2 * i; s < 2 * i + 2; ++s) {
                         const int n = b * NK + s;
                         unsigned w[2];
                         if constexpr (BITS == 4) w[0] = w[1] = kw[n >> 2][n & 3];
                         else w[0] = kw[n >> 1][(n & 1) * 2], w[1] = kw[n >> 1][(n & 1) * 2 + 1];
-                        x[i] = C::mul(C::template key<BITS>(w), qf[s], x[i]);
+                        x[i] = C::mul(codes.template key<BITS>(w), qf[s], x[i]);
                     }
                 }
 #pragma unroll
@@ -652,10 +679,11 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
 #pragma unroll
                     for (int i = 0; i < NG; ++i) {
                         const unsigned w = ks[i][b][r >> 1] >> (r & 1) * 16;
-                        y += fmaf(-(group_zero<BITS>(w) + OFF), qs[i], x[i][r]) * group_step<BITS>(w);
+                        if constexpr (TWO) y = fmaf(x[i][r], group_step<BITS>(w), y);
+                        else y += fmaf(-group_zero<BITS>(w), qs[i], x[i][r]) * group_step<BITS>(w);
                     }
                     y *= a.scale;
-                    if (hidden(b, r)) y = -INFINITY;
+                    y = b * 16 + r >= end ? -INFINITY : y;
                     sc[b][r] = y;
                     mx = fmaxf(mx, y);
                 }
@@ -693,7 +721,7 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float st = group_step<BITS>(vs[i][b][r >> 1] >> (r & 1) * 16);
-                        const float y = hidden(b, r) ? 0.f : sc[b][r] * st;
+                        const float y = sc[b][r] * (b * 16 + r >= end ? 0.f : st);
                         if constexpr (TWO) {
                             const __bf16 w = (__bf16)y;
                             pf[b * 4 + r] = w;
@@ -704,12 +732,12 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
                             pf[b * 4 + r] = y;
                         }
                     }
-                const V z = C::template zeros<BITS>(u32x4{vs[i][0][0], vs[i][0][1], vs[i][1][0], vs[i][1][1]});
+                const V z = codes.template zeros<BITS>(u32x4{vs[i][0][0], vs[i][0][1], vs[i][1][0], vs[i][1][1]});
                 if constexpr (TWO) oz[i] = C::mul(z, pl, oz[i]);
                 oz[i] = C::mul(z, pf, oz[i]);
 #pragma unroll
                 for (int d = i * (GROUP / 16); d < (i + 1) * (GROUP / 16); ++d) {
-                    const V vf = C::template val<BITS>(vw[d / PER], d % PER);
+                    const V vf = codes.template val<BITS>(vw[d / PER], d % PER);
                     if constexpr (TWO) o[d] = C::mul(vf, pl, o[d]);
                     o[d] = C::mul(vf, pf, o[d]);
                 }
@@ -767,6 +795,241 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
     }
 }
 
+// Up to 4 rows in bf16 (a decode step of up to 4 query heads per kv head): 16 columns of a
+// product would hold them four times. Here 64 positions at once make use of the
+// 16: column 4 b + g is row g over the b-th 16 positions, so the softmax of 64
+// positions takes as many instructions as that of 16 rows over 16 positions. The
+// four blocks' scores are products with the same queries in all columns, of which
+// each column keeps its own block's; the weights enter the product with a value
+// block of 32 positions in the columns of its two blocks, zeros in the others, and
+// a row's four columns are added up at the end.
+template <int D, int BITS>
+__global__ __launch_bounds__(256) void packed_attn_four_kernel(AttnArgs a) {
+    typedef bf16 T;
+    typedef Codes<T> C;
+    typedef C::V V;
+    constexpr int NK = D / 32, ND = D / 16, NG = D / GROUP;
+    constexpr int NB = D * BITS / 256;  // 16-byte pieces per lane of 32 positions' codes
+    constexpr int PER = 16 / BITS;      // dim tiles of a value piece
+    constexpr float OFF = CODE_OFF<T, BITS>;
+    __shared__ float so[4][4][D + 4];
+    __shared__ float sm[4][4], sl[4][4];
+    const ListHead head = *reinterpret_cast<const ListHead*>(a.plan);
+    const AttnItem* items = reinterpret_cast<const AttnItem*>(a.plan + head.fours_at);
+    const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4, g = fr & 3, blk = fr >> 2;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int P = 1 << a.c.shift;
+    const C codes{};
+    for (int w0 = blockIdx.x; w0 < head.fours * a.c.Hkv; w0 += gridDim.x) {
+        const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
+        const AttnItem t = items[it];
+        const int rows = t.count * a.G;
+        const int j = min(t.j0 + g, rows - 1), tok = j / a.G;
+        const int lim = t.past + tok + 1;         // positions this lane's row sees
+        const int all = t.past + t.j0 / a.G + 1;  // positions every row sees
+        const T* q = static_cast<const T*>(a.q) + (long long)(t.tok0 + tok) * a.q_ld + (h * a.G + j - tok * a.G) * D + fc * 8;
+        V qf[NK];
+        float qs[NG];  // the row's sums
+#pragma unroll
+        for (int i = 0; i < NG; ++i) qs[i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+            qf[s] = *reinterpret_cast<const V*>(q + s * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) qs[s / 2] += (float)qf[s][e];
+        }
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            qs[i] += __shfl_xor(qs[i], 16, 64);
+            qs[i] += __shfl_xor(qs[i], 32, 64);
+        }
+        mfma_f32x4 o[ND], oz[NG];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NG; ++i) oz[i] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        const int* table = a.c.table + (long long)t.seq * a.c.ld;
+        // 32 positions from p, or (where the range ends before) its last 32 again, hidden
+        const int last = (t.kv1 - 1) & ~31;
+        auto place = [&](int p) __attribute__((always_inline)) { return min(p, last); };
+        auto page_of = [&](int p) __attribute__((always_inline)) { return list_at(table, place(p) >> a.c.shift); };
+        int next[2];  // pages are looked up a block ahead
+#pragma unroll
+        for (int i = 0; i < 2; ++i) next[i] = page_of(t.kv0 + wave * 64 + i * 32);
+        for (int p = t.kv0 + wave * 64; p < t.kv1; p += 256) {
+            u32x4 kw[2][NB], vw[2][NB];
+            u32x2 vs[NG][2][2];  // words of the halves' positions b * 16 + fc * 4 .. + 3
+            u32x2 ks[NG], vo[NG];  // of positions blk * 16 + fc * 4 .. + 3, this column's
+            const unsigned char *kb[2], *vb[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int p0 = place(p + 32 * i) & (P - 1);
+                kb[i] = a.c.head<unsigned char>(next[i], a.layer, 0, h);
+                vb[i] = a.c.head<unsigned char>(next[i], a.layer, 1, h);
+                next[i] = page_of(p + 256 + 32 * i);
+                const int at = (p0 >> 5) * (NB * 1024) + lane * 16;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) kw[i][n] = *reinterpret_cast<const u32x4*>(kb[i] + at + n * 1024);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) vw[i][n] = *reinterpret_cast<const u32x4*>(vb[i] + at + n * 1024);
+                kb[i] += packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
+                vb[i] += packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
+            }
+            const unsigned char *kc = (blk & 2 ? kb[1] : kb[0]) + (blk & 1) * 32, *vc = (blk & 2 ? vb[1] : vb[0]) + (blk & 1) * 32;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                ks[i] = *reinterpret_cast<const u32x2*>(kc + i * P * 2);
+                vo[i] = *reinterpret_cast<const u32x2*>(vc + i * P * 2);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) vs[i][n][b] = *reinterpret_cast<const u32x2*>(vb[n] + i * P * 2 + b * 32);
+            }
+            mfma_f32x4 x[NG];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    mfma_f32x4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 2 * i; s < 2 * i + 2; ++s) {
+                        const int n = (b & 1) * NK + s;
+                        unsigned w[2];
+                        if constexpr (BITS == 4) w[0] = w[1] = kw[b >> 1][n >> 2][n & 3];
+                        else w[0] = kw[b >> 1][n >> 1][(n & 1) * 2], w[1] = kw[b >> 1][n >> 1][(n & 1) * 2 + 1];
+                        y = C::mul(codes.key<BITS>(w), qf[s], y);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[i][r] = b == 0 || blk == b ? y[r] : x[i][r];
+                }
+            // of this lane's 4 positions, those it sees
+            const int end = p + 64 > min(all, t.kv1) ? min(lim, t.kv1) - (p + blk * 16 + fc * 4) : 4;
+            float sc[4], mx = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float y = 0.f;
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    const unsigned w = ks[i][r >> 1] >> (r & 1) * 16;
+                    y = fmaf(fmaf(-(group_zero<BITS>(w) + OFF), qs[i], x[i][r]), group_step<BITS>(w), y);
+                }
+                y *= a.scale;
+                y = r >= end ? -INFINITY : y;
+                sc[r] = y;
+                mx = fmaxf(mx, y);
+            }
+            mx = fmaxf(mx, __uint_as_float(lane_xor<4>(__float_as_uint(mx))));
+            mx = fmaxf(mx, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(mx), 0x128, 0xf, 0xf, true)));  // 8 lanes on
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float mn = fmaxf(m, mx);
+            const float mu = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing, or only -inf
+            if (__any(mn > m)) {
+                const float alpha = exp2_softmax(m - mu);
+                l *= alpha;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
+#pragma unroll
+                for (int i = 0; i < NG; ++i) oz[i][0] *= alpha;
+                m = mn;
+            }
+            {
+#pragma clang fp contract(off)  // mu is a rounded product, and so is what it is taken from
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sc[r] = exp2_softmax(sc[r] - mu);
+                    l += sc[r];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                float y[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float st = group_step<BITS>(vo[i][r >> 1] >> (r & 1) * 16);
+                    y[r] = sc[r] * (r >= end ? 0.f : st);
+                }
+                V pf[2], pl[2];
+                unsigned hi[2], lo[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    hi[u] = pack_bf16x2(y[2 * u], y[2 * u + 1]);
+                    lo[u] = pack_bf16x2(y[2 * u] - __uint_as_float(hi[u] << 16), y[2 * u + 1] - __uint_as_float(hi[u] & 0xffff0000u));
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const bool one = blk == 2 * n, two = blk == 2 * n + 1;
+                    pf[n] = C::of(one ? hi[0] : 0, one ? hi[1] : 0, two ? hi[0] : 0, two ? hi[1] : 0);
+                    pl[n] = C::of(one ? lo[0] : 0, one ? lo[1] : 0, two ? lo[0] : 0, two ? lo[1] : 0);
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const V z = codes.zeros<BITS>(u32x4{vs[i][n][0][0], vs[i][n][0][1], vs[i][n][1][0], vs[i][n][1][1]});
+                    oz[i] = C::mul(z, pl[n], oz[i]);
+                    oz[i] = C::mul(z, pf[n], oz[i]);
+#pragma unroll
+                    for (int d = i * (GROUP / 16); d < (i + 1) * (GROUP / 16); ++d) {
+                        const V vf = codes.val<BITS>(vw[n][d / PER], d % PER);
+                        o[d] = C::mul(vf, pl[n], o[d]);
+                        o[d] = C::mul(vf, pf[n], o[d]);
+                    }
+                }
+            }
+        }
+        // a row's columns 4 and 8 lanes away, the lanes' weights
+        auto add_blocks = [&](float v) __attribute__((always_inline)) {
+            v += __uint_as_float(lane_xor<4>(__float_as_uint(v)));
+            return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x128, 0xf, 0xf, true));
+        };
+        l = add_blocks(l);
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (lane < 4) {
+            sm[wave][g] = m;
+            sl[wave][g] = l;
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float y = add_blocks(o[d][r] - oz[d * 16 / GROUP][0]);
+                if (blk == 0) so[wave][g][d * 16 + fc * 4 + r] = y;
+            }
+        __syncthreads();
+        // thread: row tid / (D / 4), 4 dims
+        const int row = threadIdx.x / (D / 4), d = (threadIdx.x % (D / 4)) * 4;
+        if (row < 4 && t.j0 + row < rows) {
+            const float mt = fmaxf(fmaxf(sm[0][row], sm[1][row]), fmaxf(sm[2][row], sm[3][row]));
+            const float mu = mt == -INFINITY ? 0.f : mt;
+            float w[4], lt = 0.f, y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = exp2_softmax(sm[i][row] - mu);
+                lt += sl[i][row] * w[i];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                y[e] = so[0][row][d + e] * w[0] + so[1][row][d + e] * w[1] + so[2][row][d + e] * w[2] + so[3][row][d + e] * w[3];
+            if (t.part < 0) {
+                const int jr = t.j0 + row, tk = jr / a.G, gg = jr - tk * a.G;
+                const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+                attn_store<T, false>(a, t.tok0 + tk, h * a.G + gg, D, d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+            } else {
+                float* ps = a.parts + ((long long)t.part * a.c.Hkv + h) * (16 * (D + 2));
+                st4(ps + row * D + d, y[0], y[1], y[2], y[3]);
+                if (d == 0) {
+                    ps[16 * D + row] = mt;
+                    ps[16 * D + 16 + row] = lt;
+                }
+            }
+        }
+        __syncthreads();  // the next item's LDS
+    }
+}
+
 // ------------------------------------------------------------------ attention of many rows
 //
 // The 128-row kernel goes through a sequence's positions once for every 128
@@ -807,12 +1070,12 @@ __global__ __launch_bounds__(256) void packed_unpack_kernel(PagedView c, int lay
                     unsigned x[2];
                     if constexpr (BITS == 4) x[0] = x[1] = w[f >> 2][f & 3];
                     else x[0] = w[f >> 1][(f & 1) * 2], x[1] = w[f >> 1][(f & 1) * 2 + 1];
-                    put(f, (Codes<float>::key<BITS>(x) - group_zero<BITS>(m)) * group_step<BITS>(m));
+                    put(f, (Codes<float>{}.key<BITS>(x) - group_zero<BITS>(m)) * group_step<BITS>(m));
                 }
         } else {
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
-                f32x8 y = Codes<float>::val<BITS>(w[d / PER], d % PER);
+                f32x8 y = Codes<float>{}.val<BITS>(w[d / PER], d % PER);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const unsigned m = words[d / 4 * P + fc * 4 + (e & 3) + (e >> 2) * 16];

@@ -79,7 +79,8 @@ struct PageTile {
 // grid, so a recorded launch serves whatever list is current at its replay.
 struct ListHead {
     int items, merges, tiles, merges_at, tiles_at, bigs, bigs_at;
-    int pages, pages_at;  // of a packed cache: pages to unpack for the bigs
+    // of a packed cache: pages to unpack for the bigs, items of up to 4 rows
+    int pages, pages_at, fours, fours_at;
 };
 constexpr int HEAD_INTS = sizeof(ListHead) / sizeof(int);
 
