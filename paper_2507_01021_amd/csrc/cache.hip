@@ -179,7 +179,7 @@ class PagedCacheT final : public PagedCache {
         plan_ok_ = false;
         if (dev_ == WHISPER_NO_DEVICE) return;
         DeviceScope scope(dev_);
-        end_chunk(false);
+        end_chunk(ALL);
     }
 
     void fork(int src, const int* dst, int n) override {
@@ -206,7 +206,7 @@ class PagedCacheT final : public PagedCache {
         if (n == 0 || !open || !plan_ok_ || !append_ok_) return;
         append_ok_ = false;
         DeviceScope scope(dev_);
-        end_chunk(true);
+        end_chunk(KEEP);
     }
 
     void reorder(const int* seqs, const int* from, int n) override {
@@ -242,11 +242,13 @@ class PagedCacheT final : public PagedCache {
             for (size_t k = 0; k < pg.size(); ++k)
                 if (k >= before[i].size() || pg[k] != before[i][k]) add_update(upd, to[i], (int)k, pg[k]);
         }
-        if (gone || shared) {
+        const End end = gone ? ALL : shared ? KEEP : NO;
+        if (!upd.empty()) {
+            apply(upd, {}, end);
+        } else if (end) {
             DeviceScope scope(dev_);
-            end_chunk(!gone);
+            end_chunk(end);
         }
-        apply(upd, {});
     }
 
     void compact() override {
@@ -336,22 +338,27 @@ class PagedCacheT final : public PagedCache {
         if (dev_ == WHISPER_NO_DEVICE) throw ArgError(WHISPER_E_STATE, "the cache has no device");
         if (!plan_ok_) throw ArgError(WHISPER_E_STATE, "no chunk: call whisper_cache_extend first");
     }
-    // What a replay finds from now on: no rows, or rows to attend to but none to append.
-    void end_chunk(bool attend) {
-        ListHead head = attend ? head_ : ListHead{};
-        head.tiles = 0;
-        std::vector<int> h(HEAD_INTS);
-        memcpy(h.data(), &head, sizeof(head));
-        put(plan_, h, 0, 0);
+    // What a replay finds from now on: no rows (ALL), or rows to attend to but none to append.
+    enum End { NO, KEEP, ALL };
+    void end_chunk(End how) {
+        put_some<PUT_FEW>(nullptr, 0, nullptr, 0, 0, reinterpret_cast<ListHead*>(plan_.dev), how == KEEP);
+        WMI_HIP(hipGetLastError());
     }
     PagedView view() const {
         return PagedView{pages_, table_, book_.max_list(), shift_, P_.n_layer, P_.n_kv_head, head_elems_, odd_};
     }
 
+    template <int N>
+    void put_some(const int* v, int m, int* dst, size_t upd, int n, ListHead* head, bool keep) {
+        PutInts<N> a;
+        a.n = m;
+        if (m) memcpy(a.v, v, m * sizeof(int));
+        hipLaunchKernelGGL(put_ints_kernel<N>, dim3(1), dim3(256), 0, st_, a, dst, (int)upd, n, table_, head, (int)keep);
+    }
     // Copies a list to the device, as a kernel argument if it is short, else
-    // through pinned memory (a ring, so that the host rarely waits), and makes
-    // the n changes of page lists that begin at upd.
-    void put(DevList& d, const std::vector<int>& v, size_t upd, int n) {
+    // through pinned memory (a ring, so that the host rarely waits), makes
+    // the n changes of page lists that begin at upd, and ends the chunk if told to.
+    void put(DevList& d, const std::vector<int>& v, size_t upd, int n, End end = NO) {
         if (&d == &plan_ && v.size() > d.cap) throw DeviceError("paged cache: a longer plan than planned for");
         if (v.size() > d.cap) {
             WMI_HIP(hipStreamSynchronize(st_));
@@ -366,12 +373,13 @@ class PagedCacheT final : public PagedCache {
         if (v.size() <= 2 * PUT_INTS) {
             const bool once = v.size() <= PUT_INTS;
             for (size_t i = 0; i < v.size(); i += PUT_INTS) {
-                PutInts a;
-                a.n = (int)std::min<size_t>(PUT_INTS, v.size() - i);
-                memcpy(a.v, v.data() + i, a.n * sizeof(int));
-                hipLaunchKernelGGL(put_ints_kernel, dim3(1), dim3(256), 0, st_, a, d.dev + i, (int)upd, once ? n : 0, table_);
+                const int m = (int)std::min<size_t>(PUT_INTS, v.size() - i), un = once ? n : 0;
+                ListHead* head = once && end ? reinterpret_cast<ListHead*>(plan_.dev) : nullptr;
+                if (m <= PUT_FEW) put_some<PUT_FEW>(v.data() + i, m, d.dev + i, upd, un, head, end == KEEP);
+                else put_some<PUT_INTS>(v.data() + i, m, d.dev + i, upd, un, head, end == KEEP);
             }
             WMI_HIP(hipGetLastError());
+            if (!once && end) end_chunk(end);
             if (!once) update_table(d.dev + upd, n);
             return;
         }
@@ -391,6 +399,7 @@ class PagedCacheT final : public PagedCache {
         WMI_HIP(hipMemcpyAsync(d.dev, s.host, v.size() * sizeof(int), hipMemcpyHostToDevice, st_));
         WMI_HIP(hipEventRecord(s.ev, st_));
         update_table(d.dev + upd, n);
+        if (end) end_chunk(end);
     }
 
     void add_update(std::vector<int>& upd, int seq, int k, int page) const {
@@ -409,12 +418,12 @@ class PagedCacheT final : public PagedCache {
             WMI_HIP(hipGetLastError());
         }
     }
-    void apply(const std::vector<int>& upd, const std::vector<PageCopy>& copies) {
+    void apply(const std::vector<int>& upd, const std::vector<PageCopy>& copies, End end = NO) {
         std::vector<int> v = upd;
         for (auto& c : copies) v.insert(v.end(), {c.src, c.dst});
         if (v.empty()) return;
         DeviceScope scope(dev_);
-        put(list_, v, 0, (int)upd.size() / 2);
+        put(list_, v, 0, (int)upd.size() / 2, end);
         copy_pages(list_.dev + upd.size(), (int)copies.size());
     }
 
@@ -596,7 +605,7 @@ class PagedCacheT final : public PagedCache {
         };
         // packed: a wave per (tile, keys or values, head) and layer
         auto go_flat = [&](auto kernel, auto* kk, auto* vv) {
-            const long long wgs = (2LL * n * P_.n_kv_head * nl + 3) / 4;
+            const long long wgs = (2LL * n * P_.n_kv_head * nl + 31) / 32 * 8;
             hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<long long>(wgs, MOST_WGS)), block, 0, st_, view(), list, l0, kk, vv,
                                k_ld, v_ld, kl, vl, nl);
         };

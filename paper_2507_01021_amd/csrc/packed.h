@@ -258,11 +258,8 @@ __device__ __forceinline__ void transpose8(u32x4& w, int lane) {
 //           pieces of 8 positions.
 // Workgroups are dealt to the 8 XCDs in turn; place_of_group gives those of one
 // XCD consecutive work, so that rows of neighbouring heads meet in its L2 and
-// reach memory together.
-__device__ __forceinline__ unsigned place_of_group() {
-    const unsigned b = blockIdx.x, n = gridDim.x, x = b & 7, q = n >> 3, r = n & 7;
-    return x * q + min(x, r) + (b >> 3);
-}
+// reach memory together (grids are multiples of 8).
+__device__ __forceinline__ unsigned place_of_group() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
 // Position, in its block of 32, and dims of a lane of the values:
 __device__ __forceinline__ int value_row(int lane) { return (lane >> 4) * 4 + (lane & 3) + (lane & 4) * 4; }
 __device__ __forceinline__ int value_dim(int lane, int i) { return i * 16 + (lane & 8); }
@@ -282,12 +279,13 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PagedView c, const i
     const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
     const int lane = threadIdx.x & 63, P = 1 << c.shift;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long all = 2LL * head.tiles * c.Hkv;  // (tile, keys or values, head) of a layer
-    for (long long u0 = place_of_group() * 4LL + wave; u0 < all * n_layers; u0 += gridDim.x * 4LL) {
-        const int z = (int)(u0 / all), layer = layer0 + z;
-        const long long w = u0 - z * all;
-        const int h = (int)(w % c.Hkv), kv = (int)(w / c.Hkv) & 1;
-        const PageTile t = tiles[w / c.Hkv >> 1];
+    const unsigned all = 2u * head.tiles * c.Hkv;  // (tile, keys or values, head) of a layer; less than 2^30
+    for (long long u0 = place_of_group() * 4LL + wave; u0 < (long long)all * n_layers; u0 += gridDim.x * 4LL) {
+        const int z = u0 >> 32 ? (int)(u0 / all) : (int)((unsigned)u0 / all), layer = layer0 + z;
+        const unsigned w = (unsigned)(u0 - (long long)z * all);
+        const unsigned wt = w / c.Hkv;
+        const int h = w - wt * c.Hkv, kv = wt & 1;
+        const PageTile t = tiles[wt >> 1];
         const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
         const int b0 = t.pos & (P - 1) & ~31, lo = t.pos & 31, hi = lo + t.n;  // the block, and its new positions
         const long long ld = kv ? v_ld : k_ld;
@@ -382,10 +380,11 @@ __global__ __launch_bounds__(256) void packed_append_few_kernel(PagedView c, con
     const ListHead head = *reinterpret_cast<const ListHead*>(list);
     const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
     const int layer = layer0 + blockIdx.z, tid = threadIdx.x, d = tid % CH * 8, P = 1 << c.shift;
-    const long long all = 2LL * head.tiles * c.Hkv;  // (tile, keys or values, head)
-    for (long long w = blockIdx.x * (256LL / CH) + tid / CH; w < all; w += gridDim.x * (256LL / CH)) {
-        const int h = (int)(w % c.Hkv), kv = (int)(w / c.Hkv) & 1;
-        const PageTile t = tiles[w / c.Hkv >> 1];
+    const unsigned all = 2u * head.tiles * c.Hkv;  // (tile, keys or values, head); less than 2^30
+    for (unsigned w = blockIdx.x * (256u / CH) + tid / CH; w < all; w += gridDim.x * (256u / CH)) {
+        const unsigned wt = w / c.Hkv;
+        const int h = w - wt * c.Hkv, kv = wt & 1;
+        const PageTile t = tiles[wt >> 1];
         const long long ld = kv ? v_ld : k_ld;
         const T* src = (kv ? v + blockIdx.z * v_layer : k + blockIdx.z * k_layer) + t.row * ld + h * D + d;
         const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
@@ -423,12 +422,13 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PagedView c, const int
     const PageTile* tiles = reinterpret_cast<const PageTile*>(list + head.tiles_at);
     const int lane = threadIdx.x & 63, P = 1 << c.shift;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long all = 2LL * head.tiles * c.Hkv;
-    for (long long u0 = place_of_group() * 4LL + wave; u0 < all * n_layers; u0 += gridDim.x * 4LL) {
-        const int z = (int)(u0 / all), layer = layer0 + z;
-        const long long w = u0 - z * all;
-        const int h = (int)(w % c.Hkv), kv = (int)(w / c.Hkv) & 1;
-        const PageTile t = tiles[w / c.Hkv >> 1];
+    const unsigned all = 2u * head.tiles * c.Hkv;
+    for (long long u0 = place_of_group() * 4LL + wave; u0 < (long long)all * n_layers; u0 += gridDim.x * 4LL) {
+        const int z = u0 >> 32 ? (int)(u0 / all) : (int)((unsigned)u0 / all), layer = layer0 + z;
+        const unsigned w = (unsigned)(u0 - (long long)z * all);
+        const unsigned wt = w / c.Hkv;
+        const int h = w - wt * c.Hkv, kv = wt & 1;
+        const PageTile t = tiles[wt >> 1];
         const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
         const int b0 = t.pos & (P - 1) & ~31, lo = t.pos & 31, hi = lo + t.n;
         const long long ld = kv ? v_ld : k_ld;
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PagedView c, const int
                 const int p = value_row(lane);
                 const unsigned word = words[n * P + p];
                 const float step = group_step<BITS>(word), off = -group_zero<BITS>(word) * step;
-                u32x4 y[BLOCKS];
+                u32x4 y[BLOCKS], r[4];
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
                     y[b] = *reinterpret_cast<const u32x4*>(src + pval_off<BITS>(b0, n * GROUP + b * 32, D) + lane * 16);
@@ -473,7 +473,30 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PagedView c, const int
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             x[e] = fmaf((float)(y[b][e >> 1] >> ((e & 1) * 16 + i * BITS) & (BITS == 4 ? 15u : 255u)), step, off);
-                        if (p >= lo && p < hi) store8<T, VEC>(dst + (p - lo) * ld + n * GROUP + value_dim(lane, b * TILES + i), x);
+                        if constexpr (VEC && sizeof(T) == 2)
+                            r[b * TILES + i] = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                                     pack_bf16x2(x[6], x[7])};
+                        else if (p >= lo && p < hi) store8<T, VEC>(dst + (p - lo) * ld + n * GROUP + value_dim(lane, b * TILES + i), x);
+                    }
+                }
+                if constexpr (VEC && sizeof(T) == 2) {
+                    // neighbouring lanes have neighbouring rows: they swap halves, so that a
+                    // store's segments are 64 bytes long instead of 32
+                    const bool second = lane & 1;
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const unsigned got = lane_xor<1>(second ? r[i][j] : r[i + 1][j]);
+                            r[i][j] = second ? got : r[i][j];
+                            r[i + 1][j] = second ? r[i + 1][j] : got;
+                        }
+                        const int d = n * GROUP + value_dim(lane, i + second);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int q = (p & ~1) + j;
+                            if (q >= lo && q < hi) *reinterpret_cast<u32x4*>(dst + (q - lo) * ld + d) = r[i + j];
+                        }
                     }
                 }
             }

@@ -87,18 +87,26 @@ constexpr int HEAD_INTS = sizeof(ListHead) / sizeof(int);
 // ------------------------------------------------------------------ small lists
 //
 // Lists of up to PUT_INTS numbers reach the device as a kernel argument: no
-// copy engine, nothing to wait for, and the host may go on at once.
-constexpr int PUT_INTS = 960;
+// copy engine, nothing to wait for, and the host may go on at once. (Short ones
+// as a shorter argument.)
+constexpr int PUT_INTS = 960, PUT_FEW = 224;
+template <int N>
 struct PutInts {
     int n;
-    int v[PUT_INTS];
+    int v[N];
 };
 // The list's numbers upd .. upd + 2 n - 1 are changes of page lists as well
-// (table[first] = second), made at once.
-static __global__ __launch_bounds__(256) void put_ints_kernel(PutInts a, int* __restrict__ dst, int upd, int n,
-                                                              int* __restrict__ table) {
+// (table[first] = second), made at once. `head`, if not null, is that of a list that
+// ends: of the whole of it, or (keep) of its tiles.
+template <int N>
+static __global__ __launch_bounds__(256) void put_ints_kernel(PutInts<N> a, int* __restrict__ dst, int upd, int n,
+                                                              int* __restrict__ table, ListHead* head, int keep) {
     for (int i = threadIdx.x; i < a.n; i += 256) dst[i] = a.v[i];
     for (int i = threadIdx.x; i < n; i += 256) table[a.v[upd + 2 * i]] = a.v[upd + 2 * i + 1];
+    if (head && threadIdx.x == 0) {
+        if (keep) head->tiles = 0;
+        else *head = ListHead{};
+    }
 }
 // table[at[2 i]] = at[2 i + 1]
 static __global__ __launch_bounds__(256) void table_update_kernel(const int* __restrict__ at, int n, int* __restrict__ table) {
