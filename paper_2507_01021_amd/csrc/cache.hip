@@ -35,10 +35,32 @@ constexpr int ATTN_PART = 512;
 // some 7 us where it is faster (few sequences, short contexts) and lose several
 // times the time where it is not; below, it loses with many sequences too.
 constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
+// The same for a packed cache, whose pages are unpacked before that kernel reads
+// them. us of the 16-row kernel and of the two, per rows:
+//                                          128        192        256        384
+//    1 sequence  over  200, 20 of 64, 4 b.   6  15      7  16      7  18     12  22
+//    1           over 4000                  20  28     26  34     31  34     44  41
+//    9 sequences over 1000                  32  45     46  54     60  55     88  67
+//   32           over 1000                  97 104    145 137    196 141    305 189
+//    9           over 1000, 32 / 8 of 128   32  35     43  42     47  45     65  51
+//   32           over 1000                  78  70    114  79    152  83    229 113
+//   32           over 1000, 8 bits         113  74    166  82    220  86    328 117
+constexpr int BIG_FROM_PACKED = 192;
 // Rows of a tile, on average, up to which the packed cache's append takes the
-// kernel of few rows.
+// kernel of few rows. us of the other kernel and of this one, all of 32 layers, 20
+// heads of 64, 4 bits, per rows of a sequence:
+//                     1            4           8          16
+//    1 sequence    4.1  3.2    4.2  5.4    4.3  8.4    4.6 14.4
+//    9            11.7  4.0   12.0  6.8   12.5 11.0   14.2 20.1
+//   32            34.0  6.3   34.1 12.5   35.1 27.0   39.3 52.8
+// (32 sequences with 8 heads of 128: 28.2 5.7, 28.3 10.0, 28.1 16.5, 30.5 28.6; with
+// 20 of 64 in 8 bits: 32.2 9.1, 32.3 20.9, 33.4 36.7, 37.6 65.8.)
 constexpr int FEW_ROWS = 4;
-// Workgroups that the packed cache's attention of up to 4 rows is cut into.
+// Workgroups that the packed cache's attention of up to 4 rows is cut into (4
+// sequences of one token over 60001 positions at most, 32 / 8 heads of 128: 37.4 us,
+// 39.9 with 1024). The kernel of 16 rows and this one with the merge, one token, 4
+// bits, us: 20 heads of 64, 1 sequence over 4000 10.5 9.2, 32 over 200 6.9 6.2, 32
+// over 1000 22.2 14.7; 32 / 8 heads of 128 12.5 11.5, 6.5 6.5, 17.9 16.8.
 constexpr int FOUR_WGS = 512;
 // Most workgroups of a launch along its list (a grid holds fewer than 2^32
 // threads): the kernels go through longer lists in strides.
@@ -430,7 +452,7 @@ class PagedCacheT final : public PagedCache {
     // Packed caches of bf16: up to 4 rows of a sequence go to a kernel of their own.
     static constexpr bool FOURS = sizeof(T) == 2;
     // Whether a chunk's `count` tokens of one sequence go to the kernel of many rows.
-    bool big_rows(int count) const { return sizeof(T) == 2 && (long long)count * G_ >= BIG_FROM; }
+    bool big_rows(int count) const { return sizeof(T) == 2 && (long long)count * G_ >= (bits_ ? BIG_FROM_PACKED : BIG_FROM); }
     bool max_bigs() const { return big_rows(P_.max_tokens); }
     bool unpacks() const { return bits_ && max_bigs(); }
 
