@@ -635,7 +635,7 @@ whisper_status whisper_cache_create(const whisper_cache_params* params, int devi
  * below 2^125 in magnitude (infinities and NaN among them) stands for NaN
  * throughout; a position that is not visible does not enter all the same.
  * Queries are taken to be below 2^100 in magnitude.
- * In bf16, a cache whose max_tokens times query heads of a kv head is 128 or more
+ * In bf16, a cache whose max_tokens times query heads of a kv head is 192 or more
  * also holds one layer's keys and values of all its pages in bf16: attention of
  * sequences with that many rows unpacks their pages there first.
  * Errors: as whisper_cache_create.

@@ -144,6 +144,68 @@ def test_many_groups():
     assert all(torch.equal(x, y) for x, y in zip(again, got))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_rows_of_equal_logits(dtype):
+    """More equal logits than any list holds, in every piece of a row and over all of
+    them; runs of equal ones among others."""
+    V, width, n = 200003, 4, 64
+    logits, scores = make(dtype, 4 * width, V, 11)
+    logits[:width] = -2.0
+    scores[:width] = -3.0
+    logits[width: 2 * width] = torch.tensor([0.0, 1.0, 1.0, 0.0], device="cuda")[:, None]
+    scores[width: 2 * width] = torch.tensor([-1.0, -1.0, -7.0, -1.0])
+    logits[2 * width: 3 * width, 150000:199000] = 30.0  # all in some pieces
+    logits[3 * width, ::3], logits[3 * width + 1, 1::5] = 9.0, 30.0
+    b = binding.Beam(V, 4 * width)
+    check(run(b, dtype, logits, scores, width, n), logits, scores, width, n)
+    b.options([0, 1, V - 1, 150000])
+    check(run(b, dtype, logits, scores, width, n), logits, scores, width, n, [0, 1, V - 1, 150000])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_widest_call(dtype):
+    """32 beams of 2^20 ids; then more groups than one launch takes of such rows."""
+    V = 1 << 20
+    logits, scores = make(dtype, 32, V, 12)
+    b = binding.Beam(V, 70)
+    check(run(b, dtype, logits, scores, 32, 64), logits, scores, 32, 64)
+    logits = torch.cat([logits, logits.flip(0), logits[:6] + 1]).contiguous()
+    scores = torch.rand(70, device="cuda") * -20
+    got = run(b, dtype, logits, scores, 2, 5)
+    for g in (0, 15, 16, 31, 32, 34):
+        rows = slice(2 * g, 2 * g + 2)
+        check([x[g: g + 1] for x in got], logits[rows], scores[rows], 2, 5)
+
+
+def test_two_handles_at_once():
+    """Graphs of two handles, replayed on two streams beside each other."""
+    made = []
+    for V, width, n, dtype in ((50001, 5, 10, "bf16"), (20000, 8, 16, "f32")):
+        b = binding.Beam(V, 3 * width)
+        logits, scores = make(dtype, 3 * width, V, V)
+        out = [torch.zeros(3, n, dtype=t, device="cuda") for t in (torch.int32, torch.int32, torch.float32)]
+        st = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        b.set_stream(st.cuda_stream)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            b.run(logits.data_ptr(), DT[dtype][1], 3, width, n, scores.data_ptr(), *(x.data_ptr() for x in out))
+        made.append((b, logits, scores, out, st, g, width, n, dtype, V))
+    for i in range(4):
+        for b, logits, scores, out, st, g, width, n, dtype, V in made:
+            new, sc = make(dtype, 3 * width, V, i)
+            logits.copy_(new)
+            scores.copy_(sc)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for b, logits, scores, out, st, g, width, n, dtype, V in made:
+                with torch.cuda.stream(st):
+                    g.replay()
+        torch.cuda.synchronize()
+        for b, logits, scores, out, st, g, width, n, dtype, V in made:
+            check(out, logits, scores, width, n)
+
+
 def test_close_scores():
     """Continuations of different beams that differ by a few 2^-40 of a score: far
     less than fp32 tells apart."""

@@ -204,6 +204,24 @@ def test_chunks(dtype, bits, H, Hkv, D, P):
     p.attend([3, 1], [7, 333])
 
 
+@BOTH
+@pytest.mark.parametrize("H,Hkv,D", [(4, 4, 64), (8, 2, 128)])
+def test_chunks_on_either_side_of_a_choice_of_kernel(dtype, bits, H, Hkv, D):
+    """Rows of a sequence and kv head around 4, 16, 32 and 192; tokens around 4 a
+    tile, whose mean decides how a chunk is appended."""
+    p = Pair(dtype, bits, H, Hkv, D, 64, 6, 1500, seed=3)
+    p.add([0, 1, 2, 3, 4, 5], [700, 1, 33, 31, 64, 255])
+    G = H // Hkv
+    for rows in ([192, 188, 196, 4, 8, 16], [4, 8, 12, 16, 20, 32], [4, 4, 4, 4, 4, 4], [36, 128, 124, 64, 4, 192]):
+        counts = [r // G for r in rows]
+        p.add(list(range(6)), counts)
+        p.attend(list(range(6)), counts)
+    for counts in ([1, 2, 3, 4, 5, 6], [4, 4, 4, 4, 4, 4], [5, 5, 5, 5, 5, 5], [191, 193, 1, 1, 1, 1], [0, 0, 33, 0, 0, 0]):
+        p.add(list(range(6)), counts)
+        p.attend(list(range(6)), counts)
+    p.check_rows(list(range(6)))
+
+
 @pytest.mark.parametrize("dtype,bits,H,Hkv,D,lens", [
     ("bf16", 4, 8, 2, 128, [20000, 1, 4097]), ("bf16", 8, 20, 20, 64, [9000]), ("bf16", 4, 8, 8, 64, [7001, 3000]),
     ("f32", 4, 4, 1, 64, [12345, 700]), ("f32", 8, 2, 2, 128, [5000]), ("bf16", 4, 1, 1, 64, [50000])])
@@ -440,6 +458,40 @@ def test_recorded_step_serves_later_chunks(dtype, bits):
         p.c.set_stream(st.cuda_stream)
         p.check_rows(seqs)
         (torch.randn(64, 64, device="cuda") @ torch.randn(64, 64, device="cuda")).sum().item()
+
+
+def test_two_recorded_caches_at_once():
+    """Graphs of two caches, one of 4 and one of 8 bits, replayed on two streams beside
+    each other for chunks of few and of many rows (200 and more of a sequence and kv
+    head): neither's workspaces are the other's."""
+    n, made = 130, []
+    for bits in (4, 8):
+        p = Pair("bf16", bits, 8, 4, 64, 64, 4, 3000, max_tokens=12000, seed=bits)
+        p.add([0, 1, 2, 3], [100, 2500, 7, 1000])
+        k, v = (torch.zeros(1, n, 4, 64, dtype=p.t, device="cuda") for _ in range(2))
+        q, out = (torch.zeros(n, 8, 64, dtype=p.t, device="cuda") for _ in range(2))
+        st = torch.cuda.Stream()
+        p.c.set_stream(st.cuda_stream)
+        p.c.extend([0], [0])
+        g = record(p, st, lambda: p.c.append(0, k.data_ptr(), v.data_ptr()), lambda: p.c.attend(0, q.data_ptr(), out.data_ptr()))
+        made.append((p, st, g, k, v, q, out))
+    for seqs, counts in (([0, 2], [120, 10]), ([1, 3, 0], [101, 2, 20]), ([3, 2, 1, 0], [1, 1, 1, 1])):
+        for p, st, g, k, v, q, out in made:
+            for x in (k, v, q):
+                x.copy_(torch.randn(x.shape, generator=p.g, device="cuda"))
+        torch.cuda.synchronize()
+        for p, st, g, k, v, q, out in made:
+            p.c.extend(seqs, counts)
+        for _ in range(3):
+            for p, st, g, k, v, q, out in made:
+                with torch.cuda.stream(st):
+                    g.replay()
+        torch.cuda.synchronize()
+        m = sum(counts)
+        for p, st, g, k, v, q, out in made:
+            p.note(seqs, counts, k[:, :m], v[:, :m])
+            p.check(out[:m], q[:m], seqs, counts)
+            p.check_rows([0, 1, 2, 3])
 
 
 @pytest.mark.parametrize("bits", [0, 4])
