@@ -13,7 +13,7 @@
 // pieces' sums and picks from their lists. (As one kernel, whose last workgroup of
 // a group goes on with the choice, the fences that make the others' lists visible
 // cost more than the launch: 1, 64 and 16 groups of 5, 5 and 12 beams of 51865, 51866
-// and 151937 ids took 20, 107 and 165 us instead of 12.5, 32 and 48.)
+// and 151937 ids took 20, 107 and 165 us, as two 12.5, 32 and 45.)
 // The n largest of many numbers: the n-th largest of the lanes' maxima is a
 // bound that at least n numbers reach, and few more than n; those are listed, and
 // put in order by counting for each the larger ones.
@@ -54,7 +54,7 @@ struct BeamPiece {
     float ref;
 };
 // Rows a launch takes at most, pieces that they are cut into, pieces of a group.
-constexpr int BEAM_ROWS = 512, BEAM_PIECES = 1024, BEAM_LISTS = 1024;
+constexpr int BEAM_ROWS = 512, BEAM_PIECES = 1280, BEAM_LISTS = 1024;
 constexpr int BEAM_BATCHES = 16;  // batches of a piece
 
 namespace bm {
@@ -153,6 +153,9 @@ __device__ __forceinline__ void in_order(int n, int best, L&& larger, F&& f) {
 // suppressed. Ids are counted from the row's first wherever that lies (16-byte
 // loads need no alignment here), so that a row's sums are the same at every
 // address: beams that are alike stay equal to the last bit.
+// Bound by the issue of fp64 (30 vector instructions per 64 ids, 55 % of the cycles,
+// 64 groups of 5 beams of 51866 ids in bf16: 26.2 us, 1.3 TB/s) and by the waits around
+// it: first loads, joined bounds, what is read again.
 template <class T, int U, bool NEVER>
 __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
     using namespace bm;
@@ -213,6 +216,9 @@ __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
         }
         return mx;
     };
+    // a wave's batches that are not all behind the row (and one for the ids behind the last 16 bytes)
+    const int ids = whole - start(wave * 64, 0), tail = blockIdx.x == gridDim.x - 1 && wave == 0;
+    const int batches = min(a.batches, max(tail, ids > 0 ? (ids + U * 64 - 1) / (U * 64) : 0));
     u32x4 x[U];
     unsigned m[U];
     float l[U][EL];
@@ -220,14 +226,14 @@ __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
     float ref = -INFINITY, all_most = lx;
     double sum = 0.0;
 #pragma unroll 1
-    for (int bt = 0; bt < a.batches; ++bt) {
+    for (int bt = 0; bt < batches; ++bt) {
         const int v0 = start(tid, bt);
-        const float last = bt == a.batches - 1 ? lx : -INFINITY;
+        const float last = bt == batches - 1 ? lx : -INFINITY;
         float mx = unpack(v0, x, m, l);
         most[bt][tid] = mx;
         mx = fmaxf(mx, last);
         all_most = fmaxf(all_most, mx);
-        if (bt + 1 < a.batches) fetch(v0 + U * 64, x, m);
+        if (bt + 1 < batches) fetch(v0 + U * 64, x, m);
         // (fp64 has room for exponents up to there)
         if (__any(mx > ref + 500.f)) {
             const float t = wave_max(mx);
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) bound = fmaxf(bound, wbound[0][w]);
     bound = fmaxf(bound, -FLT_MAX);
-    for (int bt = 0; bt < a.batches; ++bt)
+    for (int bt = 0; bt < batches; ++bt)
         if (most[bt][tid] >= bound) {
             const int p = atomicAdd(&pairs, 1);
             if (p < THREADS) pair[p] = bt << 8 | tid;
@@ -339,7 +345,7 @@ __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
             n += __popcll(in);
         };
 #pragma unroll 1
-        for (int bt = 0; bt < a.batches; ++bt) {
+        for (int bt = 0; bt < batches; ++bt) {
             if (!__any(most[bt][tid] >= bound)) continue;
             const int v0 = start(tid, bt);
             fetch(v0, x, m);
@@ -378,7 +384,8 @@ __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
 // j-th entry is some score has j + 1 continuations no worse, so the k-th largest of
 // the lists' j-th entries, k (j + 1) >= n, is a bound that n continuations reach
 // (rounded down to fp32, it still is). What reaches it is put in order by counting.
-// Bound by the latency of two rounds of loads and of the counting.
+// Bound by the latency of two rounds of loads and of the counting: 5.5 us for one
+// group of 5 beams, 7.6 for 64, 9.5 for 16 of 12.
 static __global__ __launch_bounds__(bm::THREADS) void beam_pick_kernel(BeamArgs a) {
     using namespace bm;
     constexpr int CAP = 1024, PER = BEAM_LISTS / 256, FEW = BEAM_BEST;
@@ -601,8 +608,10 @@ static __global__ __launch_bounds__(bm::THREADS) void beam_pick_kernel(BeamArgs 
     }
 }
 
-// A launch's pieces: what 1024 workgroups (four per CU) take in batches of 16 ids a
-// thread, or, where that gives fewer than one per CU, in batches of 8 ids.
+// A launch's pieces: what 1280 workgroups (five per CU) take in batches of 16 ids a
+// thread, or, where that gives fewer than one per CU, in batches of 8 ids. (16 groups
+// of 12 beams of 151937 ids: 36.8 us, 40.3 with 1024 pieces; 64 of 5 beams of 51866
+// in bf16: 26.2 both.)
 template <class T, int U>
 inline void beam_launch(BeamArgs a, int n, int groups, int loads, hipStream_t st) {
     const int most = (loads + U * bm::THREADS - 1) / (U * bm::THREADS);
@@ -634,7 +643,8 @@ inline void beam_rows(BeamArgs a, int groups, hipStream_t st) {
         else beam_launch<T, U / 2>(b, n, m, loads, st);
     }
 }
-// the widest group over the widest vocabulary (2^20 ids of 4 bytes) fits a launch, and so its pieces' lists
-static_assert(BEAM_PIECES / ((1 << 18) / (BEAM_BATCHES * 4 * bm::THREADS)) >= BEAM_WIDTH && BEAM_PIECES <= BEAM_LISTS, "");
+// the widest group over the widest vocabulary (2^20 ids of 4 bytes) fits a launch, and its pieces the lists of a group
+constexpr int BEAM_LEAST = (1 << 18) / (BEAM_BATCHES * 4 * bm::THREADS);
+static_assert(BEAM_PIECES / BEAM_LEAST >= BEAM_WIDTH && BEAM_LISTS / BEAM_WIDTH >= BEAM_LEAST, "");
 
 }  // namespace wmi
