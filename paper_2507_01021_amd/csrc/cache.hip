@@ -163,7 +163,8 @@ class PagedCacheT final : public PagedCache {
     void append(int layer, const void* k, const void* v, int64_t k_ld, int64_t v_ld) override {
         need_chunk();
         if (!append_ok_)
-            throw ArgError(WHISPER_E_STATE, "a sequence of the chunk was forked: its rows cannot be written any more");
+            throw ArgError(WHISPER_E_STATE, "a sequence of the chunk was forked or is continued by others: its rows "
+                                            "cannot be written any more");
         DeviceScope scope(dev_);
         // a recorded launch goes through whatever list is current at its replay in strides
         const int n = capturing(st_) ? std::min(max_tiles_, ATTN_WGS) : n_tiles_;

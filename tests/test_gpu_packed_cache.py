@@ -410,6 +410,32 @@ def test_reorder_and_the_chunk():
     p.check_rows([0, 1, 2, 3, 4])
 
 
+@pytest.mark.parametrize("n", [3, 12, 24, 64])
+@pytest.mark.parametrize("bits", [0, 8])
+def test_reorders_of_many_pages(bits, n):
+    """Lists of changed pages of any length, with a chunk that they end: all sequences
+    in a circle, then all but two as one."""
+    p = Pair("bf16", bits, 2, 1, 64, 32, n, 800, n_pages=n * 26, seed=n)
+    lens = [600 + 11 * (i % 10) for i in range(n)]
+    p.add(list(range(n)), lens)
+    p.add([0, 1], [1, 2])  # a chunk
+    p.reorder(list(range(n)), [(i + 1) % n for i in range(n)])
+    x = p.rows(4, 2)[0]
+    for f in (lambda: p.c.append(-1, x.data_ptr(), x.data_ptr()), lambda: p.c.attend(0, x.data_ptr(), x.data_ptr())):
+        with pytest.raises(binding.WhisperError) as e:
+            f()
+        assert e.value.status == binding.E_STATE
+    p.check_rows(list(range(n)))
+    p.add(list(range(n)), [1] * n)
+    p.attend(list(range(n)), [1] * n)
+    p.reorder(list(range(2, n)), [1] * (n - 2))
+    p.check_rows(list(range(n)))
+    for _ in range(2):
+        p.add(list(range(n)), [3] * n)
+        p.attend(list(range(n)), [3] * n)
+    p.check_rows(list(range(n)))
+
+
 def record(p, st, *calls):
     torch.cuda.synchronize()
     p.c.set_stream(st.cuda_stream)
