@@ -40,11 +40,11 @@ constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
 //                                          128        192        256        384
 //    1 sequence  over  200, 20 of 64, 4 b.   6  15      7  16      7  18     12  22
 //    1           over 4000                  20  28     26  34     31  34     44  41
-//    9 sequences over 1000                  32  45     46  54     60  55     88  67
-//   32           over 1000                  97 104    145 137    196 141    305 189
-//    9           over 1000, 32 / 8 of 128   32  35     43  42     47  45     65  51
-//   32           over 1000                  78  70    114  79    152  83    229 113
-//   32           over 1000, 8 bits         113  74    166  82    220  86    328 117
+//    9 sequences over 1000                  31  45     45  54     59  55     87  67
+//   32           over 1000                  95 104    145 137    194 141    303 189
+//    9           over 1000, 32 / 8 of 128   32  35     43  42     48  45     66  51
+//   32           over 1000                  74  70    110  79    146  83    218 113
+//   32           over 1000, 8 bits          93  74    136  82    180  86    266 117
 constexpr int BIG_FROM_PACKED = 192;
 // Rows of a tile, on average, up to which the packed cache's append takes the
 // kernel of few rows. us of the other kernel and of this one, all of 32 layers, 20

@@ -591,12 +591,14 @@ template <> struct Codes<float> {
 // zeros are one rank-1 term of the scores and one more "dim" of the values (a
 // fragment whose 16 rows are all z). In fp32 the operands are c - z itself: terms
 // that leave again would cost bits of a result of 24 (one token over 37 positions, 6
-// heads of 64, 4 bits: 1.1e-6 off instead of 3.3e-7, and 4.9 us instead of 4.6).
+// heads of 64, 4 bits: 1.1e-6 off instead of 3.3e-7, and no slower).
 // Codes are finite whatever was there before; hidden positions' steps are taken as
 // 0, so no value of theirs enters.
 // Bound by the chain list - page - codes where contexts are short, else by unpacking:
 // 5 tokens each of 16 sequences over 4001 positions at most, 16 / 4 heads of 64 in 8
-// bits, 10.9 us.
+// bits, 10.6 us. (With all of a block's reads before it 10.9, and 113 instead of 93
+// for 32 tokens with 4 query heads each of 32 sequences over 1000 positions, 8 heads of
+// 128 in 8 bits.)
 template <class T, int D, int BITS>
 __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
     typedef Codes<T> C;
@@ -652,31 +654,47 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
         for (int i = 0; i < NG; ++i) oz[i] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
         const int* table = a.c.table + (long long)t.seq * a.c.ld;
-        int next = list_at(table, min(t.kv0 + wave * 32, t.kv1 - 1) >> a.c.shift);  // pages are looked up a block ahead
-        for (int p = t.kv0 + wave * 32; p < t.kv1; p += 128) {
-            const int page = next, p0 = p & (P - 1);
-            next = list_at(table, min(p + 128, t.kv1 - 1) >> a.c.shift);
+        // pages are looked up a block ahead, a block's codes read when the former's have been used
+        auto page_of = [&](int p) __attribute__((always_inline)) { return list_at(table, min(p, t.kv1 - 1) >> a.c.shift); };
+        u32x4 kw[NB], vw[NB];
+        u32x2 ks[NG][2], vs[NG][2];  // words of positions b * 16 + fc * 4 .. + 3
+        unsigned kz[NG][2];          // and of position b * 16 + fr
+        auto read_keys = [&](int page, int p) __attribute__((always_inline)) {
+            const int p0 = p & (P - 1);
             const unsigned char* kb = a.c.head<unsigned char>(page, a.layer, 0, h);
-            const unsigned char* vb = a.c.head<unsigned char>(page, a.layer, 1, h);
-            const int at = (p0 >> 5) * (NB * 1024) + lane * 16, ws = packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
-            u32x4 kw[NB], vw[NB];
-            u32x2 ks[NG][2], vs[NG][2];  // words of positions b * 16 + fc * 4 .. + 3
-            unsigned kz[NG][2];          // and of position b * 16 + fr
+            const unsigned char* words = kb + packed_codes<BITS>(P, D) + p0 * 2;
 #pragma unroll
-            for (int i = 0; i < NB; ++i) kw[i] = *reinterpret_cast<const u32x4*>(kb + at + i * 1024);
+            for (int i = 0; i < NB; ++i) kw[i] = *reinterpret_cast<const u32x4*>(kb + (p0 >> 5) * (NB * 1024) + lane * 16 + i * 1024);
 #pragma unroll
             for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    ks[i][b] = *reinterpret_cast<const u32x2*>(kb + ws + (i * P + b * 16) * 2);
-                    kz[i][b] = *reinterpret_cast<const unsigned short*>(kb + packed_codes<BITS>(P, D) + (i * P + p0 + b * 16 + fr) * 2);
+                    ks[i][b] = *reinterpret_cast<const u32x2*>(words + (i * P + b * 16 + fc * 4) * 2);
+                    kz[i][b] = *reinterpret_cast<const unsigned short*>(words + (i * P + b * 16 + fr) * 2);
                 }
+        };
+        auto read_values = [&](int page, int p) __attribute__((always_inline)) {
+            const int p0 = p & (P - 1);
+            const unsigned char* vb = a.c.head<unsigned char>(page, a.layer, 1, h);
+            const unsigned char* words = vb + packed_codes<BITS>(P, D) + p0 * 2;
 #pragma unroll
-            for (int i = 0; i < NB; ++i) vw[i] = *reinterpret_cast<const u32x4*>(vb + at + i * 1024);
+            for (int i = 0; i < NB; ++i) vw[i] = *reinterpret_cast<const u32x4*>(vb + (p0 >> 5) * (NB * 1024) + lane * 16 + i * 1024);
 #pragma unroll
             for (int i = 0; i < NG; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) vs[i][b] = *reinterpret_cast<const u32x2*>(vb + ws + (i * P + b * 16) * 2);
+                for (int b = 0; b < 2; ++b) vs[i][b] = *reinterpret_cast<const u32x2*>(words + (i * P + b * 16 + fc * 4) * 2);
+        };
+        const int p1 = t.kv0 + wave * 32;
+        int next = page_of(p1);
+        if (p1 < t.kv1) {
+            read_keys(next, p1);
+            read_values(next, p1);
+        }
+        next = page_of(p1 + 128);
+        for (int p = p1; p < t.kv1; p += 128) {
+            const int page = next;
+            const bool more = p + 128 < t.kv1;
+            next = page_of(p + 256);
             const int end = p + 32 > all ? lim - p - fc * 4 : 32;  // positions of the block, from this lane's first, that it sees
             mfma_f32x4 sc[2];
             float mx = -INFINITY;
@@ -718,6 +736,7 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
                     mx = fmaxf(mx, y);
                 }
             }
+            if (more) read_keys(page, p + 128);
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             const float mn = fmaxf(m, mx);
@@ -775,6 +794,7 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
                     o[d] = C::mul(vf, pf, o[d]);
                 }
             }
+            if (more) read_values(page, p + 128);
         }
 #pragma unroll
         for (int d = 0; d < ND; ++d)
