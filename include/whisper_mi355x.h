@@ -577,6 +577,11 @@ whisper_status whisper_test_kernel_choice(int32_t choice_of, int32_t dtype, cons
  * it; a layer = -1 append as many tokens as at its recording) and does nothing
  * if there is none. The other calls that change the cache or enqueue work
  * refuse a recording stream (WHISPER_E_STATE).
+ * No handle is created or destroyed while any stream of the process records a
+ * graph: allocating, waiting and freeing break that recording, and what could not
+ * be freed is lost. (In Python: close a handle, or drop a recorded graph, by
+ * itself; one that is part of a reference cycle goes when the collector runs,
+ * which may be then.)
  * All calls on one cache, replays too, share its workspace: order them on one
  * stream.
  * Device: calls run on the cache's device and leave the current device as it
