@@ -639,7 +639,9 @@ whisper_status whisper_cache_create(const whisper_cache_params* params, int devi
  * bytes for 64 numbers in 4 bits, 66 in 8. A group with a number that is not
  * below 2^125 in magnitude (infinities and NaN among them) stands for NaN
  * throughout; a position that is not visible does not enter all the same.
- * Queries are taken to be below 2^100 in magnitude.
+ * Queries are taken to be below 2^100 in magnitude, and q . k[t] to fit fp32. (A cache
+ * that was given values of some 2^80 or more computes with smaller weights from
+ * then on, whose products with values below some 2^-46 lose bits.)
  * In bf16, a cache whose max_tokens times query heads of a kv head is 192 or more
  * also holds one layer's keys and values of all its pages in bf16: attention of
  * sequences with that many rows unpacks their pages there first.

@@ -82,7 +82,7 @@ class PagedCacheT final : public PagedCache {
         page_bytes_ = 2LL * p.n_layer * p.n_kv_head * head_elems_ * (bits_ ? 1 : sizeof(T));
         while ((1 << shift_) < p.page_size) ++shift_;
         pages_ = dalloc<unsigned char>((size_t)p.n_pages * page_bytes_);
-        table_ = dalloc<int>((size_t)p.max_seqs * book_.max_list() + 1);
+        table_ = dalloc<int>((size_t)p.max_seqs * book_.max_list() + 2);
         odd_ = table_ + (size_t)p.max_seqs * book_.max_list();  // (the pages are cleared: all finite)
         // room for the longest plan, so that recorded launches keep their addresses
         const long long T0 = p.max_tokens, S0 = p.max_seqs;
@@ -581,7 +581,8 @@ class PagedCacheT final : public PagedCache {
                 w.c.head_elems = (long long)P_.page_size * D;
                 w.layer = 0;
             }
-            if (nb) hipLaunchKernelGGL(paged_attn_big_kernel<D>, dim3(nb), dim3(BIG_THREADS), 0, st_, w);
+            if (nb && bits_) hipLaunchKernelGGL((paged_attn_big_kernel<D, true>), dim3(nb), dim3(BIG_THREADS), 0, st_, w);
+            else if (nb) hipLaunchKernelGGL((paged_attn_big_kernel<D, false>), dim3(nb), dim3(BIG_THREADS), 0, st_, w);
         }
         if constexpr (FOURS) {
             if (nf && bits_ == 4) hipLaunchKernelGGL((packed_attn_four_kernel<D, 4>), dim3(nf), dim3(256), 0, st_, a);

@@ -34,6 +34,18 @@
 namespace wmi {
 
 constexpr int GROUP = 64;
+// Attention adds up weighted codes before it divides by the weights: numbers of up to
+// 143 steps in 4 bits (128 + 15), 255 in 8, for each of up to 2^24 positions, in the
+// kernel of many rows up to 2^8 times that. From steps of 2^80 on, fp32 might not hold
+// such sums (a step is below 2^123). Once values with such a step have been appended
+// to a cache, its attention multiplies all weights, or unpacked values, by SHRINK,
+// 2^-36, so that a sum is below 2^122; the division takes it back. Products with
+// steps below 2^-50 or so then lose bits, among values of 2^80 and more.
+// (Other caches run the code they would run without it: a loop of its own in the
+// kernel of 4 rows, where a branch in the loop took 7.38 instead of 7.19 us for 32 tokens
+// over 447 positions at most; in that of 16 rows a branch, 13.8 us for 16 drafts of 5
+// tokens either way, where a second loop takes 17 to 54 registers more.)
+constexpr float LARGE_STEP = 0x1p80f;
 
 // Bytes of a head's codes and of all it holds.
 template <int BITS> constexpr int packed_codes(int P, int D) { return P * D * BITS / 8; }
@@ -109,6 +121,7 @@ struct Quantiser {
         if constexpr (BITS == 4) word = bad ? 0x7ff0u : (__float_as_uint(step) >> 16) | (unsigned)zero;
         else word = bad ? 0xff00u : (__float_as_uint(step) >> 23) << 8 | (unsigned)zero;
     }
+    __device__ __forceinline__ bool large() const { return step >= LARGE_STEP && !bad; }
     __device__ __forceinline__ float quotient(float x) const {
         const float t = x * inv;
         return BITS == 8 ? t : fmaf(fmaf(-t, step, x), inv, t);
@@ -122,7 +135,7 @@ struct Quantiser {
 // The codes of 8 numbers of a group whose other numbers are those of the
 // lanes beside this one (8 lanes at a multiple of 8); returns the group's word.
 template <int BITS>
-__device__ __forceinline__ unsigned quantise(const float (&x)[8], unsigned (&code)[8], bool& odd) {
+__device__ __forceinline__ unsigned quantise(const float (&x)[8], unsigned (&code)[8], bool& odd, bool& large) {
     Range r;
     r.add(x);
 #pragma unroll
@@ -131,6 +144,7 @@ __device__ __forceinline__ unsigned quantise(const float (&x)[8], unsigned (&cod
 #pragma unroll
     for (int e = 0; e < 8; ++e) code[e] = q.code(x[e]);
     odd = odd || q.bad;
+    large = large || q.large();
     return q.word;
 }
 
@@ -300,7 +314,7 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PagedView c, const i
         // a position's row in the caller's; of positions that are not new, the first or last new one's
         auto row = [&](int p) __attribute__((always_inline)) { return src + (min(max(p, lo), hi - 1) - lo) * ld; };
         auto is_new = [&](int p) __attribute__((always_inline)) { return p >= lo && p < hi; };
-        bool odd = false;
+        bool odd = false, large = false;
 #pragma unroll 1
         for (int n = 0; n < D / 64; ++n) {
             float x[4][8];
@@ -341,6 +355,7 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PagedView c, const i
                 r.join(8);
                 const Quantiser<BITS> q(r);
                 odd = odd || (q.bad && is_new(p));
+                large = large || (q.large() && is_new(p));
                 if (!(lane & 8) && is_new(p)) words[n * P + p] = (unsigned short)q.word;
                 // half words of dims 8 half + j: 16 dims on in the next nibble (byte), 32 on in the next block (8 bits)
                 constexpr int BLOCKS = BITS / 4, TILES = 4 / BLOCKS;
@@ -370,6 +385,7 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PagedView c, const i
             }
         }
         if (c.odd && odd) *c.odd = 1;
+        if (c.odd && large) c.odd[1] = 1;
     }
 }
 
@@ -395,13 +411,13 @@ __global__ __launch_bounds__(256) void packed_append_few_kernel(PagedView c, con
         const T* src = (kv ? v + blockIdx.z * v_layer : k + blockIdx.z * k_layer) + t.row * ld + h * D + d;
         const int page = c.table[(long long)t.seq * c.ld + (t.pos >> c.shift)];
         unsigned char* dst = c.head<unsigned char>(page, layer, kv, h);
-        bool odd = false;
+        bool odd = false, large = false;
         for (int r = 0; r < t.n; ++r) {
             const int p = (t.pos & (P - 1)) + r;
             float x[8];
             unsigned q[8], half[BITS / 2];
             load8<T, VEC>(src + r * ld, x);
-            const unsigned word = quantise<BITS>(x, q, odd);
+            const unsigned word = quantise<BITS>(x, q, odd, large);
             value_halves<BITS>(q, tid, half);
             if (kv == 0) {
                 store_key<BITS>(dst + pkey_off<BITS>(p, d, D), q);
@@ -416,6 +432,7 @@ __global__ __launch_bounds__(256) void packed_append_few_kernel(PagedView c, con
                 *reinterpret_cast<unsigned short*>(dst + packed_codes<BITS>(P, D) + ((d / GROUP) * P + p) * 2) = (unsigned short)word;
         }
         if (c.odd && odd) *c.odd = 1;
+        if (c.odd && large && kv) c.odd[1] = 1;
     }
 }
 
@@ -614,6 +631,7 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int P = 1 << a.c.shift;
+    const bool large = a.c.large();
     const C codes{};
     for (int w0 = blockIdx.x; w0 < head.items * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
@@ -757,10 +775,12 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        sc[b][r] = exp2_softmax(sc[b][r] - mu);
-                        l += sc[b][r];
-                    }
+                    for (int r = 0; r < 4; ++r) sc[b][r] = exp2_softmax(sc[b][r] - mu);
+                if (large) sc[0] *= SHRINK, sc[1] *= SHRINK;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) l += sc[b][r];
             }
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
@@ -875,6 +895,7 @@ __global__ __launch_bounds__(256) void packed_attn_four_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4, g = fr & 3, blk = fr >> 2;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int P = 1 << a.c.shift;
+    const bool large = a.c.large();
     const C codes{};
     for (int w0 = blockIdx.x; w0 < head.fours * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
@@ -913,128 +934,134 @@ __global__ __launch_bounds__(256) void packed_attn_four_kernel(AttnArgs a) {
         int next[2];  // pages are looked up a block ahead
 #pragma unroll
         for (int i = 0; i < 2; ++i) next[i] = page_of(t.kv0 + wave * 64 + i * 32);
-        for (int p = t.kv0 + wave * 64; p < t.kv1; p += 256) {
-            u32x4 kw[2][NB], vw[2][NB];
-            u32x2 vs[NG][2][2];  // words of the halves' positions b * 16 + fc * 4 .. + 3
-            u32x2 ks[NG], vo[NG];  // of positions blk * 16 + fc * 4 .. + 3, this column's
-            const unsigned char *kb[2], *vb[2];
+        auto blocks = [&](auto is_large) __attribute__((always_inline)) {
+            for (int p = t.kv0 + wave * 64; p < t.kv1; p += 256) {
+                u32x4 kw[2][NB], vw[2][NB];
+                u32x2 vs[NG][2][2];  // words of the halves' positions b * 16 + fc * 4 .. + 3
+                u32x2 ks[NG], vo[NG];  // of positions blk * 16 + fc * 4 .. + 3, this column's
+                const unsigned char *kb[2], *vb[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int p0 = place(p + 32 * i) & (P - 1);
-                kb[i] = a.c.head<unsigned char>(next[i], a.layer, 0, h);
-                vb[i] = a.c.head<unsigned char>(next[i], a.layer, 1, h);
-                next[i] = page_of(p + 256 + 32 * i);
-                const int at = (p0 >> 5) * (NB * 1024) + lane * 16;
+                for (int i = 0; i < 2; ++i) {
+                    const int p0 = place(p + 32 * i) & (P - 1);
+                    kb[i] = a.c.head<unsigned char>(next[i], a.layer, 0, h);
+                    vb[i] = a.c.head<unsigned char>(next[i], a.layer, 1, h);
+                    next[i] = page_of(p + 256 + 32 * i);
+                    const int at = (p0 >> 5) * (NB * 1024) + lane * 16;
 #pragma unroll
-                for (int n = 0; n < NB; ++n) kw[i][n] = *reinterpret_cast<const u32x4*>(kb[i] + at + n * 1024);
+                    for (int n = 0; n < NB; ++n) kw[i][n] = *reinterpret_cast<const u32x4*>(kb[i] + at + n * 1024);
 #pragma unroll
-                for (int n = 0; n < NB; ++n) vw[i][n] = *reinterpret_cast<const u32x4*>(vb[i] + at + n * 1024);
-                kb[i] += packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
-                vb[i] += packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
-            }
-            const unsigned char *kc = (blk & 2 ? kb[1] : kb[0]) + (blk & 1) * 32, *vc = (blk & 2 ? vb[1] : vb[0]) + (blk & 1) * 32;
-#pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                ks[i] = *reinterpret_cast<const u32x2*>(kc + i * P * 2);
-                vo[i] = *reinterpret_cast<const u32x2*>(vc + i * P * 2);
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) vs[i][n][b] = *reinterpret_cast<const u32x2*>(vb[n] + i * P * 2 + b * 32);
-            }
-            mfma_f32x4 x[NG];
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
+                    for (int n = 0; n < NB; ++n) vw[i][n] = *reinterpret_cast<const u32x4*>(vb[i] + at + n * 1024);
+                    kb[i] += packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
+                    vb[i] += packed_codes<BITS>(P, D) + (p0 + fc * 4) * 2;
+                }
+                const unsigned char *kc = (blk & 2 ? kb[1] : kb[0]) + (blk & 1) * 32, *vc = (blk & 2 ? vb[1] : vb[0]) + (blk & 1) * 32;
 #pragma unroll
                 for (int i = 0; i < NG; ++i) {
-                    mfma_f32x4 y{0.f, 0.f, 0.f, 0.f};
+                    ks[i] = *reinterpret_cast<const u32x2*>(kc + i * P * 2);
+                    vo[i] = *reinterpret_cast<const u32x2*>(vc + i * P * 2);
 #pragma unroll
-                    for (int s = 2 * i; s < 2 * i + 2; ++s) {
-                        const int n = (b & 1) * NK + s;
-                        unsigned w[2];
-                        if constexpr (BITS == 4) w[0] = w[1] = kw[b >> 1][n >> 2][n & 3];
-                        else w[0] = kw[b >> 1][n >> 1][(n & 1) * 2], w[1] = kw[b >> 1][n >> 1][(n & 1) * 2 + 1];
-                        y = C::mul(codes.key<BITS>(w), qf[s], y);
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) vs[i][n][b] = *reinterpret_cast<const u32x2*>(vb[n] + i * P * 2 + b * 32);
+                }
+                mfma_f32x4 x[NG];
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) {
+                        mfma_f32x4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 2 * i; s < 2 * i + 2; ++s) {
+                            const int n = (b & 1) * NK + s;
+                            unsigned w[2];
+                            if constexpr (BITS == 4) w[0] = w[1] = kw[b >> 1][n >> 2][n & 3];
+                            else w[0] = kw[b >> 1][n >> 1][(n & 1) * 2], w[1] = kw[b >> 1][n >> 1][(n & 1) * 2 + 1];
+                            y = C::mul(codes.key<BITS>(w), qf[s], y);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[i][r] = b == 0 || blk == b ? y[r] : x[i][r];
                     }
+                // of this lane's 4 positions, those it sees
+                const int end = p + 64 > min(all, t.kv1) ? min(lim, t.kv1) - (p + blk * 16 + fc * 4) : 4;
+                float sc[4], mx = -INFINITY;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[i][r] = b == 0 || blk == b ? y[r] : x[i][r];
+                for (int r = 0; r < 4; ++r) {
+                    float y = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) {
+                        const unsigned w = ks[i][r >> 1] >> (r & 1) * 16;
+                        y = fmaf(fmaf(-(group_zero<BITS>(w) + OFF), qs[i], x[i][r]), group_step<BITS>(w), y);
+                    }
+                    y *= a.scale;
+                    y = r >= end ? -INFINITY : y;
+                    sc[r] = y;
+                    mx = fmaxf(mx, y);
                 }
-            // of this lane's 4 positions, those it sees
-            const int end = p + 64 > min(all, t.kv1) ? min(lim, t.kv1) - (p + blk * 16 + fc * 4) : 4;
-            float sc[4], mx = -INFINITY;
+                mx = fmaxf(mx, __uint_as_float(lane_xor<4>(__float_as_uint(mx))));
+                mx = fmaxf(mx, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(mx), 0x128, 0xf, 0xf, true)));  // 8 lanes on
+                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                const float mn = fmaxf(m, mx);
+                const float mu = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing, or only -inf
+                if (__any(mn > m)) {
+                    const float alpha = exp2_softmax(m - mu);
+                    l *= alpha;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float y = 0.f;
+                    for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int i = 0; i < NG; ++i) {
-                    const unsigned w = ks[i][r >> 1] >> (r & 1) * 16;
-                    y = fmaf(fmaf(-(group_zero<BITS>(w) + OFF), qs[i], x[i][r]), group_step<BITS>(w), y);
+                        for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) oz[i][0] *= alpha;
+                    m = mn;
                 }
-                y *= a.scale;
-                y = r >= end ? -INFINITY : y;
-                sc[r] = y;
-                mx = fmaxf(mx, y);
-            }
-            mx = fmaxf(mx, __uint_as_float(lane_xor<4>(__float_as_uint(mx))));
-            mx = fmaxf(mx, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(mx), 0x128, 0xf, 0xf, true)));  // 8 lanes on
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float mn = fmaxf(m, mx);
-            const float mu = mn == -INFINITY ? 0.f : mn;  // a row that has seen nothing, or only -inf
-            if (__any(mn > m)) {
-                const float alpha = exp2_softmax(m - mu);
-                l *= alpha;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
-#pragma unroll
-                for (int i = 0; i < NG; ++i) oz[i][0] *= alpha;
-                m = mn;
-            }
-            {
+                {
 #pragma clang fp contract(off)  // mu is a rounded product, and so is what it is taken from
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    sc[r] = exp2_softmax(sc[r] - mu);
-                    l += sc[r];
-                }
-            }
+                    for (int r = 0; r < 4; ++r) sc[r] = exp2_softmax(sc[r] - mu);
+                    if constexpr (decltype(is_large)::value)
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                float y[4];
+                        for (int r = 0; r < 4; ++r) sc[r] *= SHRINK;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float st = group_step<BITS>(vo[i][r >> 1] >> (r & 1) * 16);
-                    y[r] = sc[r] * (r >= end ? 0.f : st);
-                }
-                V pf[2], pl[2];
-                unsigned hi[2], lo[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    hi[u] = pack_bf16x2(y[2 * u], y[2 * u + 1]);
-                    lo[u] = pack_bf16x2(y[2 * u] - __uint_as_float(hi[u] << 16), y[2 * u + 1] - __uint_as_float(hi[u] & 0xffff0000u));
+                    for (int r = 0; r < 4; ++r) l += sc[r];
                 }
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const bool one = blk == 2 * n, two = blk == 2 * n + 1;
-                    pf[n] = C::of(one ? hi[0] : 0, one ? hi[1] : 0, two ? hi[0] : 0, two ? hi[1] : 0);
-                    pl[n] = C::of(one ? lo[0] : 0, one ? lo[1] : 0, two ? lo[0] : 0, two ? lo[1] : 0);
-                }
+                for (int i = 0; i < NG; ++i) {
+                    float y[4];
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const V z = codes.zeros<BITS>(u32x4{vs[i][n][0][0], vs[i][n][0][1], vs[i][n][1][0], vs[i][n][1][1]});
-                    oz[i] = C::mul(z, pl[n], oz[i]);
-                    oz[i] = C::mul(z, pf[n], oz[i]);
+                    for (int r = 0; r < 4; ++r) {
+                        const float st = group_step<BITS>(vo[i][r >> 1] >> (r & 1) * 16);
+                        y[r] = sc[r] * (r >= end ? 0.f : st);
+                    }
+                    V pf[2], pl[2];
+                    unsigned hi[2], lo[2];
 #pragma unroll
-                    for (int d = i * (GROUP / 16); d < (i + 1) * (GROUP / 16); ++d) {
-                        const V vf = codes.val<BITS>(vw[n][d / PER], d % PER);
-                        o[d] = C::mul(vf, pl[n], o[d]);
-                        o[d] = C::mul(vf, pf[n], o[d]);
+                    for (int u = 0; u < 2; ++u) {
+                        hi[u] = pack_bf16x2(y[2 * u], y[2 * u + 1]);
+                        lo[u] = pack_bf16x2(y[2 * u] - __uint_as_float(hi[u] << 16), y[2 * u + 1] - __uint_as_float(hi[u] & 0xffff0000u));
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const bool one = blk == 2 * n, two = blk == 2 * n + 1;
+                        pf[n] = C::of(one ? hi[0] : 0, one ? hi[1] : 0, two ? hi[0] : 0, two ? hi[1] : 0);
+                        pl[n] = C::of(one ? lo[0] : 0, one ? lo[1] : 0, two ? lo[0] : 0, two ? lo[1] : 0);
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const V z = codes.zeros<BITS>(u32x4{vs[i][n][0][0], vs[i][n][0][1], vs[i][n][1][0], vs[i][n][1][1]});
+                        oz[i] = C::mul(z, pl[n], oz[i]);
+                        oz[i] = C::mul(z, pf[n], oz[i]);
+#pragma unroll
+                        for (int d = i * (GROUP / 16); d < (i + 1) * (GROUP / 16); ++d) {
+                            const V vf = codes.val<BITS>(vw[n][d / PER], d % PER);
+                            o[d] = C::mul(vf, pl[n], o[d]);
+                            o[d] = C::mul(vf, pf[n], o[d]);
+                        }
                     }
                 }
             }
-        }
+        };
+        if (large) blocks(std::true_type{});
+        else blocks(std::false_type{});
         // a row's columns 4 and 8 lanes away, the lanes' weights
         auto add_blocks = [&](float v) __attribute__((always_inline)) {
             v += __uint_as_float(lane_xor<4>(__float_as_uint(v)));
@@ -1102,6 +1129,7 @@ __global__ __launch_bounds__(256) void packed_unpack_kernel(PagedView c, int lay
     const int* pages = list + head.pages_at;  // as places in the page lists, which may change while the list is current
     const int P = 1 << c.shift, lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
     constexpr int NB = D * BITS / 256, NK = D / 32, PER = 16 / BITS;
+    const float shrink = c.large() ? SHRINK : 1.f;  // (the attention's weights take it back)
     // a wave per 32 positions of a head's keys or values
     const int blocks = P / 32, n = head.pages * c.Hkv * 2 * blocks;
     for (int i = blockIdx.x * 4 + (threadIdx.x >> 6); i < n; i += gridDim.x * 4) {
@@ -1137,7 +1165,7 @@ __global__ __launch_bounds__(256) void packed_unpack_kernel(PagedView c, int lay
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const unsigned m = words[d / 4 * P + fc * 4 + (e & 3) + (e >> 2) * 16];
-                    y[e] = (y[e] - group_zero<BITS>(m)) * group_step<BITS>(m);
+                    y[e] = (y[e] - group_zero<BITS>(m)) * (group_step<BITS>(m) * shrink);
                 }
                 put(d, y);
             }

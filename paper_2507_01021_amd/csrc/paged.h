@@ -45,9 +45,11 @@ struct PagedView {
     int n_layer, Hkv;
     long long head_elems;  // P * D
     // 1 once a value that is not finite was appended: attention then takes care
-    // of 0 * inf at hidden positions. Null: it always does.
+    // of 0 * inf at hidden positions. Null: it always does. (Packed caches: behind it, 1
+    // once values were appended whose sums fp32 might not hold, see LARGE_STEP.)
     int* odd;
     __device__ __forceinline__ bool may_be_odd() const { return !odd || list_at(odd, 0) != 0; }
+    __device__ __forceinline__ bool large() const { return odd && list_at(odd, 1) != 0; }
     template <class T>
     __device__ T* head(int page, int layer, int kv, int h) const {
         return reinterpret_cast<T*>(pages) + (((long long)page * n_layer + layer) * 2 + kv) * Hkv * head_elems +
@@ -646,14 +648,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(AttnArgs a) {
 // and took 1040.
 // An item's rows may be fewer than 128 (its waves and tiles without rows do
 // nothing but help loading) and its positions a part of a cut range; slot
-// part + i then holds the i-th 16 rows.
+// part + i then holds the i-th 16 rows. PACKED: keys and values were unpacked from
+// codes, large ones times SHRINK.
 __device__ __forceinline__ void load_to_lds(const bf16* src, unsigned char* dst) {
     __builtin_amdgcn_global_load_lds(src, dst, 16, 0, 0);
 }
+constexpr float SHRINK = 0x1p-36f;  // what weights, or unpacked values, of a cache of large values are multiplied by
 constexpr int BIG_ROWS = 128;
 constexpr int BIG_TILES = 2;  // tiles of 16 rows per wave
 constexpr int BIG_THREADS = BIG_ROWS / 16 / BIG_TILES * 64;
-template <int D>
+template <int D, bool PACKED>
 __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs a) {
     typedef mfma_bf16x8 V;
     constexpr int NK = D / 32, ND = D / 16, UT = BIG_TILES, NW = BIG_THREADS / 64;
@@ -667,6 +671,7 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pmask = (1 << a.c.shift) - 1;
     const bool check = a.c.may_be_odd();
+    const float shrunk = PACKED && a.c.large() ? SHRINK : 1.f;  // what unpacked values were multiplied by
     for (int w0 = blockIdx.x; w0 < head.bigs * a.c.Hkv; w0 += gridDim.x) {
         const int it = w0 / a.c.Hkv, h = w0 - it * a.c.Hkv;
         const AttnItem t = items[it];
@@ -875,6 +880,7 @@ __global__ __launch_bounds__(BIG_THREADS, 2) void paged_attn_big_kernel(AttnArgs
             float lt = l[u];
             lt += __shfl_xor(lt, 16, 64);
             lt += __shfl_xor(lt, 32, 64);
+            if constexpr (PACKED) lt *= shrunk;
             const int j = r0 + u * 16 + fr;
             if (u >= nu || j >= rows) continue;
             if (t.part < 0) {
