@@ -539,6 +539,7 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <class T> struct Codes;
 template <> struct Codes<bf16> {
     typedef mfma_bf16x8 V;
+    __device__ static __forceinline__ V load(const bf16* p) { return *reinterpret_cast<const V*>(p); }
     unsigned mask = 0x000f000fu, exponent = 0x43004300u;
     // (in vector registers, an instruction takes both; of constants it takes one)
     __device__ __forceinline__ Codes() { asm volatile("" : "+v"(mask), "+v"(exponent)); }
@@ -574,6 +575,10 @@ template <> struct Codes<bf16> {
 };
 template <> struct Codes<float> {
     typedef f32x8 V;
+    __device__ static __forceinline__ V load(const float* p) {  // (16-byte aligned, V is 32)
+        const mfma_f32x4 a = *reinterpret_cast<const mfma_f32x4*>(p), b = *reinterpret_cast<const mfma_f32x4*>(p + 4);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
     template <int BITS>
     __device__ __forceinline__ V key(const unsigned* w) const {
         V x;
@@ -643,7 +648,7 @@ __global__ __launch_bounds__(256) void packed_attn_kernel(AttnArgs a) {
         const T* q = static_cast<const T*>(a.q) + (long long)(t.tok0 + tok) * a.q_ld + (h * a.G + g) * D + fc * 8;
         V qf[NK];
 #pragma unroll
-        for (int s = 0; s < NK; ++s) qf[s] = *reinterpret_cast<const V*>(q + s * 32);
+        for (int s = 0; s < NK; ++s) qf[s] = C::load(q + s * 32);
         // bf16: the zeros' term of the scores as a product too, of -(zero + offset) and
         // the row's sums as three bf16 numbers each, which leave 2^-24 of them
         V qz[NG];
@@ -911,7 +916,7 @@ __global__ __launch_bounds__(256) void packed_attn_four_kernel(AttnArgs a) {
         for (int i = 0; i < NG; ++i) qs[i] = 0.f;
 #pragma unroll
         for (int s = 0; s < NK; ++s) {
-            qf[s] = *reinterpret_cast<const V*>(q + s * 32);
+            qf[s] = C::load(q + s * 32);
 #pragma unroll
             for (int e = 0; e < 8; ++e) qs[s / 2] += (float)qf[s][e];
         }
