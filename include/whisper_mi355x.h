@@ -575,7 +575,10 @@ whisper_status whisper_test_kernel_choice(int32_t choice_of, int32_t dtype, cons
  * attend may be recorded into a graph, after an extend; each replay takes the
  * chunk that is current when it runs (k, v, q and out need a row per token of
  * it; a layer = -1 append as many tokens as at its recording) and does nothing
- * if there is none. The other calls that change the cache or enqueue work
+ * if there is none. (A packed cache's append keeps the kernel that the chunk of its
+ * recording calls for, one for up to 4 tokens of a block of 32 positions on average
+ * and one for more: right for all chunks, but several times as long for the other
+ * kind.) The other calls that change the cache or enqueue work
  * refuse a recording stream (WHISPER_E_STATE).
  * No handle is created or destroyed while any stream of the process records a
  * graph: allocating, waiting and freeing break that recording, and what could not
@@ -644,7 +647,10 @@ whisper_status whisper_cache_create(const whisper_cache_params* params, int devi
  * then on, whose products with values below some 2^-46 lose bits.)
  * In bf16, a cache whose max_tokens times query heads of a kv head is 192 or more
  * also holds one layer's keys and values of all its pages in bf16: attention of
- * sequences with that many rows unpacks their pages there first.
+ * sequences with that many new tokens times query heads of a kv head unpacks their
+ * pages there first, and its weights are rounded to one bf16 number (2^-8, others to
+ * two), so results depend by as much on how a prompt is cut into chunks.
+ * In 8 bits a step is up to twice what a range needs, 1.44 times on average.
  * Errors: as whisper_cache_create.
  */
 whisper_status whisper_cache_create_packed(const whisper_cache_params* params, int32_t bits, int device,

@@ -19,8 +19,9 @@
 // put in order by counting for each the larger ones.
 // Scores of different beams may lie close together, so sums, logarithms and
 // scores are fp64: exponentials of fp32 would be off by 2^-23 of a weight, and
-// one choice in some thousands would be another. An fp64 exponential is 15 of some
-// 20 instructions per id.
+// one choice in some thousands would be another. An fp64 exponential, with its
+// conversion, difference and sum, is 16 of some 22 vector instructions per id of the
+// pass over a row, half of all that a launch takes (see beam_rows_kernel).
 #pragma once
 
 #include <cfloat>
@@ -153,9 +154,10 @@ __device__ __forceinline__ void in_order(int n, int best, L&& larger, F&& f) {
 // suppressed. Ids are counted from the row's first wherever that lies (16-byte
 // loads need no alignment here), so that a row's sums are the same at every
 // address: beams that are alike stay equal to the last bit.
-// Bound by the issue of fp64 (30 vector instructions per 64 ids, 55 % of the cycles,
-// 64 groups of 5 beams of 51866 ids in bf16: 26.2 us, 1.3 TB/s) and by the waits around
-// it: first loads, joined bounds, what is read again.
+// Bound by the issue of vector instructions (64 groups of 5 beams of 51866 ids in bf16:
+// 26.2 us, 1.3 TB/s; 33 are counted per id of a lane, 55 % of the cycles, 16 of them the
+// exponentials', 6 unpacking and maxima, the others bounds and lists) and by the waits
+// around it: first loads, joined bounds, what is read again.
 template <class T, int U, bool NEVER>
 __global__ __launch_bounds__(bm::THREADS, 4) void beam_rows_kernel(BeamArgs a) {
     using namespace bm;

@@ -45,6 +45,9 @@ constexpr int BIG_FROM = 128, BIG_WGS = 256, BIG_PART = 512;
 //    9           over 1000, 32 / 8 of 128   32  35     43  42     48  45     66  51
 //   32           over 1000                  74  70    110  79    146  83    218 113
 //   32           over 1000, 8 bits          93  74    136  82    180  86    266 117
+// Rows alone do not say which is faster here either. From 192 on, the 16-row kernel would
+// save some 10 us where it is faster (one sequence, short contexts) and lose up to
+// 150; below, it loses some 20 of 93 with many sequences of 8 bits, 4 of 74 of 4 bits.
 constexpr int BIG_FROM_PACKED = 192;
 // Rows of a tile, on average, up to which the packed cache's append takes the
 // kernel of few rows. us of the other kernel and of this one, all of 32 layers, 20

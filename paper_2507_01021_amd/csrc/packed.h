@@ -15,7 +15,9 @@
 //   4 bits: the step as bf16, whose low 4 bits are free, with zero in them
 //   8 bits: the step's exponent in the high byte, zero in the low one
 // so a number takes 4.25 or 8.25 bits. A step of any 8 bits would be 3 % finer on
-// average in 4 bits, but its values would need 12 bits and be rounded in bf16.
+// average in 4 bits, but its values would need 12 bits and be rounded in bf16. (In 8
+// bits a step of one bit is up to twice what the range needs, 1.44 times on average
+// over ranges of all sizes: half a bit of the 8.)
 //
 // Memory: pages [page][layer][K, V][kv head], each head P * D codes and behind
 // them the groups' words [D / 64][P]. The codes are in the order in which
@@ -274,7 +276,7 @@ __device__ __forceinline__ void transpose8(u32x4& w, int lane) {
 // XCD consecutive work, so that rows of neighbouring heads meet in its L2 and
 // reach memory together (grids are multiples of 8).
 // Bound by memory, in rows and pages of 64-byte segments: 40 sequences of 62 positions,
-// 32 layers, 20 heads of 64 in 4 bits are read out in 111 us (397 MB written; 4.7 TB/s
+// 32 layers, 20 heads of 64 in 4 bits are read out in 111 us (406 MB written; 4.6 TB/s
 // read and written; 121 to 160 with nontemporal stores, with keys and values in one
 // wave, or persistent and reading ahead); up to 224 new tokens of 16 sequences, 12
 // layers, 12 heads of 64 are appended in 28 us (41 through LDS, a workgroup per tile).
@@ -392,7 +394,9 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PagedView c, const i
 // Tiles of few rows: a row of a head's keys, or values, per D / 8 lanes, and its
 // half words written one by one. (A workgroup per tile would have 8 of its 256
 // lanes at work on a decode step.) Bound by the latency of the list, the page and the
-// row: 32 tokens, 32 layers, 20 heads of 64 in 8 bits 10.7 us, 32 with a wave per tile.
+// row, and by the values' half words, stores of 2 bytes that lie 16 apart: 32 tokens, 32
+// layers, 20 heads of 64 take 9.1 us in 8 bits and 6.3 in 4, which have half as many of
+// them for the same rows (32 with a wave per tile).
 template <class T, int D, int BITS, bool VEC>
 __global__ __launch_bounds__(256) void packed_append_few_kernel(PagedView c, const int* __restrict__ list, int layer0,
                                                                 const T* __restrict__ k, const T* __restrict__ v,
